@@ -446,6 +446,102 @@ at_status at_sa_set_profiling(at_chains_t chains, int enable);
 at_status at_sa_kernel_times(at_chains_t chains, double* tree_ms, int64_t* tree_launches, double* chain_ms,
                              int64_t* chain_launches);
 
+/* --------------------------------------------------------------------------
+ * Operators of sequence models over schedule tokens: embedding, log
+ * probabilities and the update of hidden matrices, for a program that learns
+ * proposals from the configurations its searches kept (Section 3.1's second
+ * cost model embeds the program's symbols and is trained as the search goes
+ * on; Appendix A.3 gives it 128-wide embeddings and hidden states).
+ *
+ * They take plain device tensors, run on the current device and enqueue on
+ * `stream`.  A tensor is a pointer, an element type and, where it has rows, the
+ * distance between them in elements (for an output at least the row's length;
+ * an input's rows may overlap or, at distance 0, be one row); pointers are
+ * aligned to an element, nothing more.  Arithmetic and sums are fp32; a result is
+ * rounded to its element type once.  Results do not depend on the order in which
+ * workgroups run.  A workspace is caller-owned device memory of at least the
+ * bytes the matching call states, 16-byte aligned, which may be reused by
+ * later calls on the same stream; NULL is fine where that is 0.  Outputs must
+ * not overlap inputs unless a call says so.
+ * -------------------------------------------------------------------------- */
+
+typedef enum { AT_F32 = 0, AT_BF16 = 1, AT_F16 = 2 } at_dtype;
+typedef enum { AT_I32 = 0, AT_I64 = 1 } at_itype;
+
+/* Embedding lookup with scaling: out[i, :] = round(scale * weight[tokens[i], :]).
+ * A token outside [0, vocab) (padding) gives a row of zeros.
+ * weight: device [vocab][dim] wtype, rows ldw apart; tokens: device [n] itype;
+ * out: device [n][dim] otype, rows ldo apart.  n == 0 or dim == 0 is a no-op.
+ * AT_E_UNSUPPORTED for n, vocab or dim of 2^31 or more. */
+at_status at_embed(const void* weight, int wtype, int64_t ldw, int64_t vocab, int64_t dim, const void* tokens, int itype,
+                   int64_t n, float scale, void* out, int otype, int64_t ldo, at_stream_t stream);
+
+/* Gradient of at_embed: dweight[v, :] = round(scale * sum of dout[i, :] over the i
+ * with tokens[i] == v), added up in fp32 in an order that depends on the
+ * sizes alone.  Tokens outside [0, vocab) take no part.  With accumulate == 0
+ * every row is written (zeros for rows that no token names); otherwise the
+ * sum is added to what dweight holds, in fp32, and other rows are untouched.
+ * dout: device [n][dim] dtype, rows ldd apart; dweight: device [vocab][dim]
+ * gtype, rows ldg apart.  The tokens are sorted by value, stably, in the workspace
+ * (at_embed_grad_workspace bytes). */
+at_status at_embed_grad_workspace(int64_t n, int64_t vocab, int64_t dim, int64_t* bytes);
+at_status at_embed_grad(const void* dout, int dtype, int64_t ldd, const void* tokens, int itype, int64_t n, float scale,
+                        int accumulate, void* dweight, int gtype, int64_t ldg, int64_t vocab, int64_t dim,
+                        void* workspace, int64_t workspace_bytes, at_stream_t stream);
+
+/* Log probabilities of given tokens, entropies and the most likely
+ * alternatives.  Row i holds logits x_j for j < valid[i] (clamped to [0,
+ * vocab]; every column when valid is NULL); with z_j = scale * x_j and p =
+ * softmax(z):
+ *   lse[i] = log sum exp z_j,  logp[i] = z_t - lse,  entropy[i] = -sum p_j log p_j,
+ *   top_idx[i, r], top_logp[i, r]: the column of the r-th largest logit (the
+ *   lowest one first among equals) and its log probability, r < k <= 64.
+ * Logits of -inf are ruled out: probability 0, never an alternative; columns
+ * from valid[i] on are not read.  Alternatives that a row does not have get
+ * index -1 and -inf.  A row with nothing left has lse and logp -inf, entropy
+ * 0.  A token that is ruled out, or not below valid[i], has logp -inf; a
+ * negative one is no token: logp 0.  A NaN or +inf among a row's logits makes
+ * its outputs NaN and its indices -1.
+ * logits: device [n][vocab] type, rows ld apart; valid: device [n] int32 or
+ * NULL; tokens: device [n] itype, or NULL for none; logp, entropy, lse: device [n]
+ * float, top_logp: device [n][k] float, top_idx: device [n][k] int32, each
+ * of them NULL when not wanted.  scale must be positive and finite.
+ * Few rows are split over workgroups and joined: at_logprobs_workspace bytes. */
+at_status at_logprobs_workspace(int64_t n, int64_t vocab, int k, int64_t* bytes);
+at_status at_logprobs(const void* logits, int type, int64_t ld, int64_t n, int64_t vocab, const int32_t* valid,
+                      const void* tokens, int itype, float scale, int k, float* logp, float* entropy, float* lse,
+                      float* top_logp, int32_t* top_idx, void* workspace, int64_t workspace_bytes, at_stream_t stream);
+
+/* Gradient of at_logprobs: with g = dlogp[i] and h = dentropy[i],
+ *   dlogits[i, j] = round(scale * (g * (1[j = t] - p_j) - h * p_j * (log p_j + entropy[i])))
+ * and 0 in ruled-out columns, columns from valid[i] on and rows with nothing in
+ * them or with an lse below -1e30 (nothing but a mask's lowest value).  g counts as 0 for a row without a token or whose token is ruled
+ * out.  lse, entropy: the forward call's (device [n] float; entropy may be
+ * NULL without dentropy); dlogp, dentropy: device [n] float, or NULL for zero.
+ * dlogits: device [n][vocab] of the logits' type, rows ldd apart. */
+at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, int64_t vocab, const int32_t* valid,
+                           const void* tokens, int itype, float scale, const float* lse, const float* entropy,
+                           const float* dlogp, const float* dentropy, void* dlogits, int64_t ldd, at_stream_t stream);
+
+/* Orthogonalises a batch of equal matrices by Newton-Schulz steps, as an
+ * update of hidden matrices wants it (singular values driven towards 1):
+ *   X = x / (|x|_F + eps);  steps times:  A = X X^T, B = b A + c A A, X = a X + B X
+ *   out = round(scale * X)
+ * (on the transpose when rows > cols).  x: device [batch][rows][cols] xtype,
+ * matrices xbatch and rows ldx elements apart; out: device, bf16 or fp32
+ * (otype), obatch and ldo apart; out may be x, of the same type.  The products
+ * run on the matrix cores with fp16 operands and fp32 sums while X keeps 22
+ * bits.  fp32 outputs, and matrices whose shorter side is at most 256, have
+ * fp32's accuracy before the result is rounded; other bf16 outputs are within
+ * about 2e-3 of their norm (bf16's own rounding is 1.7e-3 of it).
+ * A matrix of zeros gives zeros.  1 <= steps <= 64; batch <= 65535, rows and cols
+ * <= 65536, AT_E_UNSUPPORTED beyond; coefficients that let singular values
+ * grow past 8 overflow.  Workspace: at_orthogonalize_workspace bytes. */
+at_status at_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int otype, int64_t* bytes);
+at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx, int64_t batch, int64_t rows,
+                           int64_t cols, int steps, float a, float b, float c, float eps, float scale, void* out,
+                           int otype, int64_t obatch, int64_t ldo, void* workspace, int64_t workspace_bytes, at_stream_t stream);
+
 /* Thread-local description of the last non-OK status ("" if none). */
 const char* at_last_error(void);
 

@@ -37,6 +37,8 @@ EXPORTED = [
     "at_gbt_predict", "at_gbt_predict_global_local", "at_chains_create", "at_chains_destroy", "at_chains_step",
     "at_sa_thresholds", "at_sa_run", "at_sa_run_traced", "at_sa_run_global_local", "at_chains_export", "at_sa_set_profiling",
     "at_sa_kernel_times", "at_chains_set_path", "at_chains_last_path", "at_chains_last_plan", "at_select_batch", "at_select_batch_noalloc", "at_last_error",
+    "at_embed", "at_embed_grad_workspace", "at_embed_grad", "at_logprobs_workspace", "at_logprobs",
+    "at_logprobs_grad", "at_orthogonalize_workspace", "at_orthogonalize",
 ]
 
 # at_sa_path
@@ -59,7 +61,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} was built from other sources than those under csrc/; "
                           "run __graft_entry__.build() again")
     L = ctypes.CDLL(LIB_PATH)
-    vp, i32, i64, u64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint64
+    vp, i32, i64, u64, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
     sig = {
         "at_space_create": [i32, vp, i32, vp],
         "at_space_info": [vp, vp, vp, vp, vp, vp],
@@ -93,6 +95,15 @@ def _load():
         "at_select_batch": [vp, vp, i64, i32, i32, ctypes.c_float, i32, u64, vp, vp],
         "at_select_batch_noalloc": [vp, vp, i64, i32, i32, ctypes.c_float, i32, u64, vp, vp],
         "at_last_error": [],
+        "at_embed": [vp, i32, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp],
+        "at_embed_grad_workspace": [i64, i64, i64, vp],
+        "at_embed_grad": [vp, i32, i64, vp, i32, i64, f32, i32, vp, i32, i64, i64, i64, vp, i64, vp],
+        "at_logprobs_workspace": [i64, i64, i32, vp],
+        "at_logprobs": [vp, i32, i64, i64, i64, vp, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp, i64, vp],
+        "at_logprobs_grad": [vp, i32, i64, i64, i64, vp, vp, i32, f32, vp, vp, vp, vp, vp, i64, vp],
+        "at_orthogonalize_workspace": [i64, i64, i64, i32, vp],
+        "at_orthogonalize": [vp, i32, i64, i64, i64, i64, i64, i32, f32, f32, f32, f32, f32, vp, i32, i64, i64, vp,
+                             i64, vp],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -490,3 +501,223 @@ def entries(t) -> np.ndarray:
     """Host structured view (cfg, score, flag) of a device at_entry tensor [..., 4] int32."""
     a = t.detach().cpu().contiguous().numpy()
     return a.view(ENTRY_DTYPE).reshape(a.shape[:-1])
+
+
+# --------------------------------------------------------------------------
+# Operators of sequence models over schedule tokens.  Tensors with rows may have
+# any row stride (a last stride of 1); vectors are contiguous.  Outputs are
+# the caller's; a workspace may be given as a uint8 tensor (the *_workspace
+# functions say how many bytes), else one is taken from torch's allocator on the
+# call's stream.
+# --------------------------------------------------------------------------
+AT_F32, AT_BF16, AT_F16 = 0, 1, 2
+AT_I32, AT_I64 = 0, 1
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+_TYPES = None
+
+
+def _type(t, name):
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: AT_F32, torch.bfloat16: AT_BF16, torch.float16: AT_F16}
+    c = _TYPES.get(t.dtype)
+    if c is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return c
+
+
+def _rows(t, name, rows=None, cols=None):
+    """(pointer, element type, row stride) of a device tensor [rows, cols]."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    sh, st = t.shape, t.stride()
+    if len(sh) != 2 or (rows is not None and sh[0] != rows) or (cols is not None and sh[1] != cols):
+        raise ValueError(f"{name} must be [{'n' if rows is None else rows}, {'n' if cols is None else cols}], "
+                         f"got {list(sh)}")
+    if sh[1] > 1 and st[1] != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), _type(t, name), (st[0] if sh[0] > 1 else max(st[0], sh[1]))
+
+
+def _vec(t, n, dtype, name):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n:
+        raise ValueError(f"{name} must hold {n} values of {dtype}")
+    return _dev(t, None, name)
+
+
+def _tokens(t, n=None):
+    """(pointer, token type, count) of an int32 or int64 device tensor."""
+    import torch
+    if t.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"tokens must be int32 or int64, got {t.dtype}")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"tokens must hold {n} values")
+    return _dev(t, None, "tokens"), (AT_I64 if t.dtype == torch.int64 else AT_I32), t.numel()
+
+
+class _on:
+    """The call's device made current, and its stream: `stream`, or the current
+    one of that device.  Every tensor must be on the first one's device."""
+
+    def __init__(self, stream, *tensors):
+        import torch
+        self.dev = tensors[0].device
+        for t in tensors:
+            if t is not None and t.device != self.dev:
+                raise ValueError("tensors are on different devices")
+        self.stream = torch.cuda.current_stream(self.dev) if stream is None else stream
+        self.guard = None
+
+    def __enter__(self):
+        import torch
+        if torch.cuda.current_device() != self.dev.index:
+            self.guard = torch.cuda.device(self.dev)
+            self.guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+        return False
+
+    def workspace(self, given, nbytes):
+        """(tensor kept alive, pointer, bytes)."""
+        import torch
+        if given is None:
+            if not nbytes:
+                return None, None, 0
+            with torch.cuda.stream(self.stream):
+                given = torch.empty(nbytes, dtype=torch.uint8, device=self.dev)
+        elif given.device != self.dev:
+            raise ValueError("workspace is on another device")
+        return given, _dev(given, torch.uint8, "workspace"), given.numel()
+
+
+def _bytes(func, *sizes) -> int:
+    v = ctypes.c_int64()
+    _check(func, getattr(_lib, func)(*sizes, ctypes.byref(v)))
+    return v.value
+
+
+def at_embed(weight, tokens, out, scale: float = 1.0, stream=None):
+    """out[i, :] = scale * weight[tokens[i], :]; zeros for tokens outside
+    [0, vocab).  weight: [vocab, dim]; tokens: int32 or int64 [n]; out: [n, dim];
+    weight and out each float32, bfloat16 or float16."""
+    tp, ti, n = _tokens(tokens)
+    wp, wt, lw = _rows(weight, "weight")
+    op, ot, lo = _rows(out, "out", n, weight.shape[1])
+    with _on(stream, weight, tokens, out) as on:
+        _check("at_embed", _lib.at_embed(wp, wt, lw, weight.shape[0], weight.shape[1], tp, ti, n, scale, op, ot, lo,
+                                         on.stream.cuda_stream))
+
+
+def at_embed_grad_workspace(n: int, vocab: int, dim: int) -> int:
+    return _bytes("at_embed_grad_workspace", n, vocab, dim)
+
+
+def at_embed_grad(dout, tokens, dweight, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None):
+    """dweight[v, :] = scale * the sum of dout[i, :] with tokens[i] == v, or
+    added to dweight with accumulate.  dout: [n, dim]; tokens: int32 or int64
+    [n]; dweight: [vocab, dim]."""
+    tp, ti, n = _tokens(tokens)
+    vocab, dim = dweight.shape
+    dp, dt, ld = _rows(dout, "dout", n, dim)
+    gp, gt, lg = _rows(dweight, "dweight")
+    with _on(stream, dout, tokens, dweight) as on:
+        need = _bytes("at_embed_grad_workspace", n, vocab, dim) if workspace is None else 0
+        keep, wp, wb = on.workspace(workspace, need)
+        _check("at_embed_grad", _lib.at_embed_grad(dp, dt, ld, tp, ti, n, scale, 1 if accumulate else 0, gp, gt, lg,
+                                                   vocab, dim, wp, wb, on.stream.cuda_stream))
+
+
+def at_logprobs_workspace(n: int, vocab: int, k: int) -> int:
+    return _bytes("at_logprobs_workspace", n, vocab, k)
+
+
+def at_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_logp=None, top_idx=None, valid=None,
+                scale: float = 1.0, workspace=None, stream=None):
+    """Log probabilities of tokens under softmax(scale * logits), entropies, log
+    sums, and the k largest logits' columns and log probabilities.  logits:
+    [n, vocab]; tokens: int32 or int64 [n] (negative: none) or None; valid:
+    int32 [n], the columns that each row has, or None; logp, entropy, lse:
+    float32 [n]; top_logp: float32 [n, k]; top_idx: int32 [n, k]; an output
+    that is None is not computed."""
+    import torch
+    n, vocab = logits.shape
+    xp, xt, ld = _rows(logits, "logits")
+    tp, ti, _ = _tokens(tokens, n) if tokens is not None else (None, AT_I32, n)
+    k = 0
+    for t in (top_logp, top_idx):
+        if t is not None:
+            if t.dim() != 2 or t.shape[0] != n or (k and t.shape[1] != k):
+                raise ValueError("top_logp and top_idx must be [n, k]")
+            k = t.shape[1]
+    f32 = torch.float32
+    with _on(stream, logits, tokens, logp, entropy, lse, top_logp, top_idx, valid) as on:
+        need = _bytes("at_logprobs_workspace", n, vocab, k) if workspace is None else 0
+        keep, wp, wb = on.workspace(workspace, need)
+        _check("at_logprobs", _lib.at_logprobs(
+            xp, xt, ld, n, vocab, _vec(valid, n, torch.int32, "valid"), tp, ti, scale, k, _vec(logp, n, f32, "logp"),
+            _vec(entropy, n, f32, "entropy"), _vec(lse, n, f32, "lse"), _vec(top_logp, n * k, f32, "top_logp"),
+            _vec(top_idx, n * k, torch.int32, "top_idx"), wp, wb, on.stream.cuda_stream))
+
+
+def at_logprobs_grad(logits, tokens, lse, entropy, dlogp, dlogits, dentropy=None, valid=None, scale: float = 1.0,
+                     stream=None):
+    """Gradient of at_logprobs with respect to its logits, from those of logp and
+    entropy (float32 [n], or None for zero) and the forward call's lse and
+    entropy.  dlogits: [n, vocab] of the logits' type."""
+    import torch
+    n, vocab = logits.shape
+    xp, xt, ld = _rows(logits, "logits")
+    dp, dt, ldd = _rows(dlogits, "dlogits", n, vocab)
+    if dt != xt:
+        raise ValueError("dlogits must have the logits' type")
+    tp, ti, _ = _tokens(tokens, n) if tokens is not None else (None, AT_I32, n)
+    f32 = torch.float32
+    with _on(stream, logits, tokens, lse, entropy, dlogp, dlogits, dentropy, valid) as on:
+        _check("at_logprobs_grad", _lib.at_logprobs_grad(
+            xp, xt, ld, n, vocab, _vec(valid, n, torch.int32, "valid"), tp, ti, scale, _vec(lse, n, f32, "lse"),
+            _vec(entropy, n, f32, "entropy"), _vec(dlogp, n, f32, "dlogp"), _vec(dentropy, n, f32, "dentropy"), dp, ldd,
+            on.stream.cuda_stream))
+
+
+def _matrices(t, name):
+    """(pointer, matrix stride, row stride) of a device tensor [batch, rows, cols] or [rows, cols]."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be [rows, cols] or [batch, rows, cols]")
+    sh, st = t.shape, t.stride()
+    if sh[-1] > 1 and st[-1] != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    ld = st[-2] if sh[-2] > 1 else max(st[-2], sh[-1])
+    return t.data_ptr(), (st[0] if len(sh) == 3 else 0), ld
+
+
+def at_orthogonalize_workspace(batch: int, rows: int, cols: int, otype: int = AT_BF16) -> int:
+    return _bytes("at_orthogonalize_workspace", batch, rows, cols, otype)
+
+
+def at_orthogonalize(x, out, steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e-7, scale: float = 1.0, workspace=None,
+                     stream=None):
+    """Newton-Schulz steps on each matrix of x ([rows, cols] or [batch, rows,
+    cols]; float32, bfloat16 or float16), normalised first, into out (bfloat16
+    or float32, the same shape), times scale."""
+    if out.shape != x.shape:
+        raise ValueError("out must have x's shape")
+    xp, xb, ldx = _matrices(x, "x")
+    op, ob, ldo = _matrices(out, "out")
+    batch = x.shape[0] if x.dim() == 3 else 1
+    rows, cols = x.shape[-2:]
+    a, b, c = coef
+    ot = _type(out, "out")
+    with _on(stream, x, out) as on:
+        need = _bytes("at_orthogonalize_workspace", batch, rows, cols, ot) if workspace is None else 0
+        keep, wp, wb = on.workspace(workspace, need)
+        _check("at_orthogonalize", _lib.at_orthogonalize(xp, _type(x, "x"), xb, ldx, batch, rows, cols, steps, a, b, c,
+                                                         eps, scale, op, ot, ob, ldo, wp, wb,
+                                                         on.stream.cuda_stream))

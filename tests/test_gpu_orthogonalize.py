@@ -1,0 +1,195 @@
+"""Newton-Schulz steps on the GPU against the recurrence in 64 bits on the CPU.
+
+Tolerances, relative to the result's Frobenius norm.  fp32 outputs: every
+product is exact to about 2^-21 of its operands' norms, and a step enlarges
+an error by at most a = 3.4445, so five steps stay below 2^-21 * (1 + a + .. + a^4)
+* 3 < 4e-4 in the worst case, an error entirely in the smallest directions; for the
+matrices here errors spread over all directions: 1e-4.  bf16 outputs add the
+rounding, 2^-9 at most for each value.  bf16 outputs of larger matrices use
+fp16 operands: 2^-12 a rounding, three of them a step on values of about
+2.7, enlarged by about 1.5 a step near convergence and averaged over many singular
+directions: 3e-3 and the rounding."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+def say(msg):
+    print(f"[gpu-orthogonalize] {msg}", flush=True)
+
+
+@pytest.fixture(scope="module")
+def P():
+    import torch
+    torch.cuda.set_device(0)
+    import paper_1805_08166_amd
+    return paper_1805_08166_amd
+
+
+def types():
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def reference(g, steps, coef=COEF, eps=1e-7):
+    import torch
+    a, b, c = coef
+    x = g.double()
+    tall = x.shape[0] > x.shape[1]
+    if tall:
+        x = x.T
+    x = x / (torch.linalg.norm(x) + eps)
+    for _ in range(steps):
+        m = x @ x.T
+        x = a * x + (b * m + c * (m @ m)) @ x
+    return x.T if tall else x
+
+
+def make(batch, rows, cols, kind, dtype, gen):
+    import torch
+    g = torch.randn(batch, rows, cols, generator=gen)
+    if kind == "strong":    # a few strong directions over noise
+        r = min(4, rows, cols)
+        g = g * 0.3 + torch.randn(batch, rows, r, generator=gen) @ torch.randn(batch, r, cols, generator=gen)
+    elif kind == "low":     # rank 2 exactly, up to the type's rounding
+        r = min(2, rows, cols)
+        g = torch.randn(batch, rows, r, generator=gen) @ torch.randn(batch, r, cols, generator=gen)
+    elif kind == "tiny":
+        g = g * 1e-12
+    elif kind == "huge":
+        g = g * 1e25
+    return g.to(dtype)
+
+
+@pytest.mark.parametrize("batch,rows,cols,dt,ot,steps,kind", [
+    (1, 1, 1, "f32", "f32", 5, "plain"),
+    (1, 1, 9, "bf16", "bf16", 5, "plain"),
+    (2, 7, 3, "f32", "f32", 4, "plain"),
+    (3, 16, 16, "f16", "bf16", 5, "plain"),
+    (1, 64, 64, "f32", "f32", 6, "strong"),
+    (2, 65, 63, "bf16", "bf16", 5, "strong"),
+    (5, 128, 128, "f32", "bf16", 5, "strong"),
+    (1, 128, 128, "f32", "f32", 5, "low"),
+    (2, 128, 129, "f32", "f32", 5, "plain"),
+    (1, 300, 33, "f16", "f32", 5, "plain"),
+    (2, 100, 1000, "bf16", "bf16", 5, "strong"),
+    (1, 256, 256, "f32", "f32", 5, "tiny"),
+    (1, 256, 300, "f32", "bf16", 5, "huge"),
+    (1, 257, 500, "bf16", "bf16", 5, "strong"),
+    (2, 700, 321, "f32", "bf16", 5, "plain"),
+    (1, 512, 512, "bf16", "bf16", 5, "low"),
+    (1, 600, 400, "f32", "f32", 5, "strong"),
+    (1, 1000, 1100, "bf16", "bf16", 1, "plain"),
+])
+def test_steps(P, batch, rows, cols, dt, ot, steps, kind):
+    import torch
+    say(f"{batch} x {rows} x {cols} {dt} -> {ot} {kind}")
+    T = types()
+    gen = torch.Generator().manual_seed(rows * 3 + cols)
+    g = make(batch, rows, cols, kind, T[dt], gen)
+    out = torch.full((batch, rows, cols), 9.0, dtype=T[ot], device=DEV)
+    eps = 1e-20 if kind == "tiny" else 1e-7
+    P.at_orthogonalize(g.to(DEV), out, steps=steps, eps=eps)
+    small = min(rows, cols) <= 256
+    for k in range(batch):
+        want = reference(g[k], steps, eps=eps)
+        err = float((out[k].cpu().double() - want).norm() / want.norm())
+        tol = 1e-4 if ot == "f32" else (1e-4 if small else 3e-3) + 2.0 ** -8
+        assert err < tol, (k, err)
+
+
+def test_strides_scale_and_neighbours(P):
+    """Views with gaps between rows and matrices, a scale; nothing outside the
+    output's rows is touched, and what lies between the input's rows is not read."""
+    import torch
+    gen = torch.Generator().manual_seed(1)
+    for rows, cols in ((40, 90), (90, 40), (300, 280)):
+        xb = torch.full((3, rows + 2, cols + 5), float("nan"))
+        xb[:, :rows, :cols] = torch.randn(3, rows, cols, generator=gen)
+        ob = torch.full((3, rows + 1, cols + 3), 7.0, dtype=torch.float32, device=DEV)
+        x, o = xb.to(DEV)[:, :rows, :cols], ob[:, :rows, :cols]
+        P.at_orthogonalize(x, o, scale=0.25)
+        for k in range(3):
+            want = reference(xb[k, :rows, :cols], 5) * 0.25
+            assert float((o[k].cpu().double() - want).norm() / want.norm()) < 1e-4
+        rest = ob.clone()
+        rest[:, :rows, :cols] = 7.0
+        assert bool((rest == 7.0).all())
+
+
+def test_batch_equals_single_and_repeats(P):
+    import torch
+    gen = torch.Generator().manual_seed(2)
+    for rows, cols in ((128, 128), (200, 333), (400, 270)):
+        g = torch.randn(3, rows, cols, generator=gen).to(DEV)
+        a, b = (torch.empty(3, rows, cols, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        P.at_orthogonalize(g, a)
+        ws = torch.full((P.at_orthogonalize_workspace(1, rows, cols),), 0xFF, dtype=torch.uint8, device=DEV)
+        for k in range(3):
+            P.at_orthogonalize(g[k], b[k], workspace=ws)
+        assert torch.equal(a, b)
+
+
+def test_in_place(P):
+    import torch
+    gen = torch.Generator().manual_seed(3)
+    for rows, cols in ((60, 70), (300, 400)):
+        g = torch.randn(2, rows, cols, generator=gen).to(torch.bfloat16).to(DEV)
+        out = torch.empty_like(g)
+        P.at_orthogonalize(g, out)
+        P.at_orthogonalize(g, g)
+        assert torch.equal(g, out)
+
+
+def test_zeros_and_poison(P):
+    """A matrix of zeros gives zeros; a NaN spoils its own matrix only."""
+    import torch
+    gen = torch.Generator().manual_seed(4)
+    for rows, cols in ((50, 60), (270, 260)):
+        g = torch.randn(3, rows, cols, generator=gen)
+        g[0] = 0.0
+        g[2, 3, 5] = float("nan")
+        out = torch.empty(3, rows, cols, dtype=torch.float32, device=DEV)
+        P.at_orthogonalize(g.to(DEV), out)
+        out = out.cpu()
+        assert bool((out[0] == 0).all())
+        want = reference(g[1], 5)
+        assert float((out[1].double() - want).norm() / want.norm()) < 1e-4
+        assert bool(torch.isnan(out[2]).any())
+
+
+def test_other_coefficients(P):
+    """The cubic Newton-Schulz iteration (3/2, -1/2, 0), which converges to an
+    orthogonal matrix: many steps make X X^T the identity."""
+    import torch
+    gen = torch.Generator().manual_seed(5)
+    for rows, cols in ((24, 80), (260, 700)):
+        g = torch.randn(rows, cols, generator=gen)
+        out = torch.empty(rows, cols, device=DEV)
+        P.at_orthogonalize(g.to(DEV), out, steps=20, coef=(1.5, -0.5, 0.0))
+        x = out.cpu().double()
+        assert float((x @ x.T - torch.eye(rows, dtype=torch.float64)).norm() / rows ** 0.5) < 1e-4
+
+
+def test_graph_replays(P):
+    import torch
+    gen = torch.Generator().manual_seed(6)
+    for rows, cols in ((128, 128), (320, 290)):
+        g = torch.randn(2, rows, cols, generator=gen).to(DEV)
+        out = torch.empty(2, rows, cols, dtype=torch.bfloat16, device=DEV)
+        ws = torch.empty(P.at_orthogonalize_workspace(2, rows, cols), dtype=torch.uint8, device=DEV)
+        P.at_orthogonalize(g, out, workspace=ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            P.at_orthogonalize(g, out, workspace=ws)
+        for _ in range(3):
+            g.copy_(torch.randn(2, rows, cols, generator=gen))
+            want = torch.empty_like(out)
+            P.at_orthogonalize(g, want)
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
