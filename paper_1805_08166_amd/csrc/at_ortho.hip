@@ -21,6 +21,8 @@
 //     operands.
 // A and B are symmetric: only tiles on and below the diagonal are computed,
 // and each is written twice.
+#include <atomic>
+
 #include "at_ops.h"
 
 namespace at {
@@ -30,85 +32,123 @@ namespace {
 using half_t = _Float16;
 typedef half_t half8 __attribute__((ext_vector_type(8)));
 typedef half_t half4 __attribute__((ext_vector_type(4)));
+typedef float float8 __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr int TILE = 64;      // sizes are padded to multiples of it, with zeros
 constexpr int BK = 64;        // depth of one staged tile: 128 bytes a row
-constexpr int GEMM_THREADS = 256;
 constexpr float A_SCALE = 256.0f;
 
-// Each matrix is two: its words rounded to fp16, and what that left.
+// Each matrix is two: its words rounded to fp16, and what that left.  X is kept by
+// rows, the operand of A, and transposed, the operand of the update and
+// what it adds to; without split products the rest is needed in the latter
+// only, and each word of it by one workgroup only, so that it stays in place.
 struct OrthoBufs {
     half_t* X[2];         // [batch][sp][lp]
     half_t* XT[2][2];     // [step & 1]: X transposed, [batch][lp][sp]
     half_t *A[2], *B[2];  // [batch][sp][sp]
     double* part;         // [batch][NORM_BLOCKS]
 };
-constexpr int NORM_BLOCKS = 64;
+constexpr int NORM_BLOCKS = 256;
 constexpr int NORM_THREADS = 256;
 
 // --------------------------------------------------------------------------
 // Norm and layout
 // --------------------------------------------------------------------------
+// Sum over a workgroup, in every thread.
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v, double* scratch) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+    for (int w = 0; w < THREADS / 64; ++w) v += scratch[w];
+    return v;
+}
+
+// Partial sums of squares, in 64 bits: squares of what fp32 holds overflow it.
 template <int DT>
 __global__ __launch_bounds__(NORM_THREADS) void k_norm(OrthoArgs a, double* part) {
     using T = typename Elem<DT>::T;
+    constexpr int VEC = 16 / sizeof(T);
     __shared__ double s_sum[NORM_THREADS / 64];
     const T* x = static_cast<const T*>(a.x) + blockIdx.y * a.xbatch;
+    const uint32_t packs = (uint32_t)((a.cols + VEC - 1) / VEC);
+    const uint64_t all = (uint64_t)packs * (uint32_t)a.rows;
     double sum = 0.0;
-    for (int64_t r = blockIdx.x; r < a.rows; r += NORM_BLOCKS) {
-        for (int64_t c = threadIdx.x; c < a.cols; c += NORM_THREADS) {
-            const double v = (double)(float)x[r * a.ldx + c];
-            sum += v * v;
+    for (uint64_t k = blockIdx.x * NORM_THREADS + threadIdx.x; k < all; k += NORM_BLOCKS * NORM_THREADS) {
+        const int64_t r = (int64_t)((uint32_t)k / packs), c = (int64_t)((uint32_t)k % packs) * VEC;   // k < 2^32
+        const T* p = x + r * a.ldx + c;
+        if (c + VEC <= a.cols) {
+            const Pack<T, VEC> w = load_pack<T, VEC>(p);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const double v = (double)(float)w.v[e];
+                sum = __builtin_fma(v, v, sum);
+            }
+        } else {
+            for (int e = 0; c + e < a.cols; ++e) {
+                const double v = (double)(float)p[e];
+                sum = __builtin_fma(v, v, sum);
+            }
         }
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < NORM_THREADS / 64; ++w) sum += s_sum[w];
-        part[blockIdx.y * NORM_BLOCKS + blockIdx.x] = sum;
-    }
+    sum = block_sum<NORM_THREADS>(sum, s_sum);
+    if (threadIdx.x == 0) part[blockIdx.y * NORM_BLOCKS + blockIdx.x] = sum;
 }
 
-// xs * G / (|G| + eps) and its transpose, zero padded; one 64 x 64 tile of X a
-// workgroup.
+// xs * G / (|G| + eps) and its transpose, zero padded: one 64 x 64 tile of G a
+// workgroup, sixteen values of a row a thread.
 template <int DT, bool SPLIT>
 __global__ __launch_bounds__(256) void k_layout(OrthoArgs a, OrthoBufs b, int sp, int lp, int tall, float xs) {
     using T = typename Elem<DT>::T;
-    __shared__ half_t s_hi[TILE][TILE + 2], s_lo[TILE][TILE + 2];
-    __shared__ float s_f;
-    if (threadIdx.x < 64) {
-        double sum = threadIdx.x < NORM_BLOCKS ? b.part[blockIdx.z * NORM_BLOCKS + threadIdx.x] : 0.0;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        if (threadIdx.x == 0) s_f = (float)((double)xs / (sqrt(sum) + (double)a.eps));
-    }
-    __syncthreads();
-    const float f = s_f;
+    constexpr int LD = TILE + 8;   // 16-byte aligned rows
+    __shared__ half_t s_w[2][TILE][LD];
+    __shared__ double s_sum[4];
+    static_assert(NORM_BLOCKS == 256, "one partial sum a thread");
+    const double norm = sqrt(block_sum<256>(b.part[blockIdx.z * NORM_BLOCKS + threadIdx.x], s_sum));
+    const float f = (float)((double)xs / (norm + (double)a.eps));
     const T* x = static_cast<const T*>(a.x) + blockIdx.z * a.xbatch;
-    // rows and columns of X; G has them swapped when tall
-    const int64_t i0 = (int64_t)blockIdx.y * TILE, j0 = (int64_t)blockIdx.x * TILE;
-    const int64_t s = tall ? a.cols : a.rows, l = tall ? a.rows : a.cols;
-    const int u = threadIdx.x & 63;
-    for (int v = threadIdx.x >> 6; v < TILE; v += 4) {
-        // u runs along G's rows
-        const int ti = tall ? u : v, tj = tall ? v : u;
-        const int64_t i = i0 + ti, j = j0 + tj;
-        float y = 0.0f;
-        if (i < s && j < l) y = (float)(tall ? x[j * a.ldx + i] : x[i * a.ldx + j]) * f;
-        const half_t h = (half_t)y;
-        s_hi[ti][tj] = h;
-        s_lo[ti][tj] = (half_t)(y - (float)h);
+    const int line = threadIdx.x >> 2, seg = (threadIdx.x & 3) * 16;
+    const int64_t r0 = (int64_t)blockIdx.y * TILE, c0 = (int64_t)blockIdx.x * TILE, row = r0 + line, col = c0 + seg;
+    float v[16];
+    if (row < a.rows && col + 16 <= a.cols) {
+        const Pack<T, 16> w = load_pack<T, 16>(x + row * a.ldx + col);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = (float)w.v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = row < a.rows && col + e < a.cols ? (float)x[row * a.ldx + col + e] : 0.0f;
+    }
+    half8 w[2][2];   // word, half of the segment
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const float y = v[e] * f;
+        const half_t h = (half_t)y, l = (half_t)(y - (float)h);
+        w[0][e >> 3][e & 7] = h;
+        w[1][e >> 3][e & 7] = l;
+        s_w[0][seg + e][line] = h;
+        s_w[1][seg + e][line] = l;
     }
     __syncthreads();
+    // along G's rows: X when wide, X transposed when tall
     const int64_t xo = (int64_t)blockIdx.z * sp * lp;
-    for (int v = threadIdx.x >> 6; v < TILE; v += 4) {
-        b.X[0][xo + (i0 + v) * lp + j0 + u] = s_hi[v][u];
-        b.X[1][xo + (i0 + v) * lp + j0 + u] = s_lo[v][u];
-        b.XT[0][0][xo + (j0 + v) * sp + i0 + u] = s_hi[u][v];
-        if (SPLIT) b.XT[0][1][xo + (j0 + v) * sp + i0 + u] = s_lo[u][v];
+    half_t* const* along = tall ? b.XT[0] : b.X;
+    half_t* const* across = tall ? b.X : b.XT[0];
+    const int64_t ld = tall ? sp : lp, ldt = tall ? lp : sp;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (h == 0 || SPLIT || tall) {
+            half8* o = reinterpret_cast<half8*>(along[h] + xo + row * ld + col);
+            o[0] = w[h][0];
+            o[1] = w[h][1];
+        }
+        if (h == 0 || SPLIT || !tall) {
+            half8* o = reinterpret_cast<half8*>(across[h] + xo + (c0 + line) * ldt + r0 + seg);
+            o[0] = *reinterpret_cast<const half8*>(&s_w[h][line][seg]);
+            o[1] = *reinterpret_cast<const half8*>(&s_w[h][line][seg + 8]);
+        }
     }
 }
 
@@ -122,11 +162,13 @@ struct GemmArgs {
     int64_t pbatch, qbatch;      // between matrices of the batch
     int depth, ldp, ldq;
     int ti, tj;                  // tiles along i and j
-    const half_t* S[2];          // added: A (POLY) or X (UPDATE, FINAL)
-    half_t *C[2], *T[2];         // A, B or X, and X transposed
+    // all by rows j of C transposed: what is added (A for POLY, X transposed for
+    // UPDATE and FINAL), and C transposed; C itself by rows i
+    const half_t* S[2];
+    half_t *T[2], *C[2];
     int64_t cbatch;
-    int ldc, ldt;
-    float mul, add;              // of the product, and of S
+    int ldt, ldc;
+    float mul, add;              // C = mul * product + add * S
     float diag;                  // added to the diagonal (POLY)
     void* out;                   // FINAL
     int otype;
@@ -134,48 +176,164 @@ struct GemmArgs {
     int rows, cols, tall;
 };
 
+// A fragment in LDS: rows of 36 floats, 16-byte aligned.
+constexpr int FRAG_LD = 36, FRAG_FLOATS = 32 * FRAG_LD;
+
+// Eight values rounded to fp16, and what that left.
+template <bool BOTH>
+__device__ __forceinline__ void put_words(half_t* const (&to)[2], int64_t at, float8 v) {
+    half8 h, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        h[e] = (half_t)v[e];
+        if (BOTH) l[e] = (half_t)(v[e] - (float)h[e]);
+    }
+    *reinterpret_cast<half8*>(to[0] + at) = h;
+    if (BOTH) *reinterpret_cast<half8*>(to[1] + at) = l;
+}
+
+// Eight values of the output's row, from column c on.
+__device__ __forceinline__ void put_out(const GemmArgs& a, int64_t z, int64_t row, int64_t c, int rows, int cols, float8 v) {
+    if (row >= rows || c >= cols) return;
+    const int64_t at = z * a.obatch + row * a.ldo + c;
+    const bool whole = c + 8 <= cols;
+    if (a.otype == AT_F32) {
+        float* o = static_cast<float*>(a.out) + at;
+        if (whole) {
+            store_pack<float, 4>(o, Pack<float, 4>{{v[0], v[1], v[2], v[3]}});
+            store_pack<float, 4>(o + 4, Pack<float, 4>{{v[4], v[5], v[6], v[7]}});
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < cols) o[e] = v[e];
+        }
+        return;
+    }
+    __bf16* o = static_cast<__bf16*>(a.out) + at;
+    if (whole) {
+        Pack<__bf16, 8> w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w.v[e] = (__bf16)v[e];
+        store_pack<__bf16, 8>(o, w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < cols) o[e] = (__bf16)v[e];
+    }
+}
+
 // A staged tile is rows of eight 16-byte chunks; chunk c of row r lies in
 // slot c ^ (r >> 1 & 7).  A wave's fragment read takes one chunk of 32 rows;
 // two rows span all banks, so every 16 lanes touch each bank once.
 __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
 
-// Rows row0 .. row0 + ROWS - 1 at depth k0 into LDS, by direct moves of
-// 16 bytes a lane.
-template <int ROWS>
-__device__ __forceinline__ void stage(const half_t* src, int ld, int64_t row0, int k0, half_t* lds) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr int MOVES = ROWS / 8 / (GEMM_THREADS / 64);
-#pragma unroll
-    for (int q = 0; q < MOVES; ++q) {
-        const int r0 = (wave * MOVES + q) * 8, r = r0 + (lane >> 3);
-        const half_t* g = src + (row0 + r) * ld + k0 + slot_of(r, lane & 7) * 8;
-        __builtin_amdgcn_global_load_lds(g, lds + r0 * BK, 16, 0, 0);
+// Eight rows of 128 bytes into LDS, 16 bytes a lane, in lane order.
+__device__ __forceinline__ void move_rows(const char* src, half_t* lds) {
+    __builtin_amdgcn_global_load_lds(src, lds, 16, 0, 0);
+}
+
+// Waits until at most N of this wave's moves are under way and its own LDS
+// reads have returned, then for the workgroup.
+template <int N>
+__device__ __forceinline__ void wait_moves() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// One tile shape: WR x WC waves, each FR x FC fragments of 32 x 32, times WK
+// that share out a staged tile's depth and add up at the end; STAGES staged
+// tiles in LDS.
+template <int WR_, int WC_, int WK_, int FR_, int FC_, int STAGES_>
+struct Shape {
+    static constexpr int WR = WR_, WC = WC_, WK = WK_, FR = FR_, FC = FC_, STAGES = STAGES_;
+    static constexpr int WAVES = WR * WC * WK, THREADS = WAVES * 64;
+    static constexpr int ROWS = WR * FR * 32, COLS = WC * FC * 32;
+    static constexpr int MOVES = (ROWS + COLS) / 8 / WAVES;   // of a wave and stage
+    static constexpr int LDS = STAGES * (ROWS + COLS) * BK * 2;
+};
+
+// Tile of this workgroup.  Workgroups go to the eight XCDs in turn, so each
+// XCD takes a run of consecutive tiles, and consecutive tiles are eight (four for
+// the symmetric products) deep in i: an XCD's tiles share their operands' rows
+// in its L2.
+constexpr int XCDS = 8;
+template <bool SYM>
+__device__ __forceinline__ void tile_of(const GemmArgs& a, int& z, int& bi, int& bj) {
+    const int n = gridDim.x, xcd = blockIdx.x % XCDS, each = n / XCDS, more = n % XCDS;
+    int t = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / XCDS;
+    const int tiles = SYM ? a.ti * (a.ti + 1) / 2 : a.ti * a.tj;
+    z = t / tiles;
+    t -= z * tiles;
+    if (SYM) {
+        // lower triangle, four rows at a time
+        int r = 0, h, c;
+        for (;; r += 4) {
+            h = a.ti - r < 4 ? a.ti - r : 4;
+            c = h * r + h * (h + 1) / 2;
+            if (t < c) break;
+            t -= c;
+        }
+        if (t < h * r) {
+            bi = r + t % h;
+            bj = t / h;
+        } else {
+            t -= h * r;
+            bi = 0;
+            while (t > bi) t -= ++bi;
+            bj = r + t;
+            bi += r;
+        }
+    } else {
+        const int g = t / (8 * a.tj), h = a.ti - g * 8 < 8 ? a.ti - g * 8 : 8;
+        t -= g * 8 * a.tj;
+        bi = g * 8 + t % h;
+        bj = t / h;
     }
 }
 
 // SPLIT: the product of (P + p)(Q + q)^T without p q^T, three passes over the
 // depth into the same sums: fp32 results to about 2^-22.
-template <int ROWS, int COLS, int MODE, bool SPLIT>
-__global__ __launch_bounds__(GEMM_THREADS) void k_gemm(GemmArgs a) {
-    constexpr int WR = ROWS / 2, WC = COLS / 2;      // of a wave
-    constexpr int FR = WR / 32, FC = WC / 32;        // fragments of 32 x 32
-    __shared__ half_t s_p[2][ROWS * BK], s_q[2][COLS * BK];
+template <class S, int MODE, bool SPLIT>
+__global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
+    constexpr int ROWS = S::ROWS, COLS = S::COLS, FR = S::FR, FC = S::FC, STAGES = S::STAGES;
+    extern __shared__ half_t s_tiles[];   // [STAGES][ROWS + COLS][BK]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t z = blockIdx.y;
-    int bi, bj;
-    if (MODE == GRAM || MODE == POLY) {
-        // lower triangle, row by row
-        const int t = blockIdx.x;
-        bi = (int)((__builtin_sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-        while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
-        while (bi * (bi + 1) / 2 > t) --bi;
-        bj = t - bi * (bi + 1) / 2;
-    } else {
-        bi = blockIdx.x % a.ti;
-        bj = blockIdx.x / a.ti;
+    int bi, bj, z;
+    tile_of<MODE == GRAM || MODE == POLY>(a, z, bi, bj);
+    const int i0 = bi * ROWS, j0 = bj * COLS;
+    const int wk = wave / (S::WR * S::WC), wq = wave % (S::WR * S::WC);
+    const int wr = wq / S::WC * FR * 32, wc = wq % S::WC * FC * 32;
+    const int steps = a.depth / BK, total = steps * (SPLIT ? 3 : 1);
+    // A tile goes to LDS by direct moves of 16 bytes a lane, eight rows each:
+    // first P's rows, then Q's; this lane's bytes lie at at_row from the tile's start.
+    constexpr int MOVES = S::MOVES;
+    uint32_t at_row[MOVES];
+#pragma unroll
+    for (int q = 0; q < MOVES; ++q) {
+        int r = (wave * MOVES + q) * 8 + (lane >> 3);
+        const bool second = r >= ROWS;
+        if (second) r -= ROWS;
+        at_row[q] = (uint32_t)((r * (second ? a.ldq : a.ldp) + slot_of(r, lane & 7) * 8) * 2);
     }
-    const int64_t i0 = (int64_t)bi * ROWS, j0 = (int64_t)bj * COLS;
-    const int wr = (wave >> 1) * WR, wc = (wave & 1) * WC;
+    int pass = 0, ks = 0;   // of the tile staged next
+    const char *srcP = nullptr, *srcQ = nullptr;
+    auto next_tile = [&]() {
+        srcP = reinterpret_cast<const char*>(a.P[SPLIT && pass == 2] + z * a.pbatch + (int64_t)i0 * a.ldp + ks * BK);
+        srcQ = reinterpret_cast<const char*>(a.Q[SPLIT && pass == 1] + z * a.qbatch + (int64_t)j0 * a.ldq + ks * BK);
+        if (++ks == steps) {
+            ks = 0;
+            ++pass;
+        }
+    };
+    auto move = [&](int q, int buf) {
+        const int r = (wave * MOVES + q) * 8;
+        const char* src = r < ROWS ? srcP : srcQ;
+        move_rows(src + at_row[q], s_tiles + (buf * (ROWS + COLS) + r) * BK);
+    };
+    for (int k = 0; k < STAGES && k < total; ++k) {
+        next_tile();
+#pragma unroll
+        for (int q = 0; q < MOVES; ++q) move(q, k);
+    }
     float16v acc[FR][FC];
 #pragma unroll
     for (int r = 0; r < FR; ++r)
@@ -183,107 +341,308 @@ __global__ __launch_bounds__(GEMM_THREADS) void k_gemm(GemmArgs a) {
         for (int c = 0; c < FC; ++c)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[r][c][e] = 0.0f;
-    const int steps = a.depth / BK, total = steps * (SPLIT ? 3 : 1);
-    int pass = 0, ks = 0;   // of the tile staged next
-    auto stage_next = [&](int buf) {
-        const half_t* P = a.P[SPLIT && pass == 2] + z * a.pbatch;
-        const half_t* Q = a.Q[SPLIT && pass == 1] + z * a.qbatch;
-        stage<ROWS>(P, a.ldp, i0, ks * BK, s_p[buf]);
-        stage<COLS>(Q, a.ldq, j0, ks * BK, s_q[buf]);
-        if (++ks == steps) {
-            ks = 0;
-            ++pass;
+    // Fragments of 16 along the depth, KK of them a tile and wave, are read one
+    // ahead of the products that use them, across tiles too: before the last of a
+    // tile's products the wave sees to it that the next tile has landed and that
+    // everyone has read this one, whose LDS the tile STAGES ahead then takes.
+    constexpr int KK = BK / 16 / S::WK;
+    static_assert(KK % 2 == 0, "fragments alternate between two sets of registers");
+    half8 p[2][FR], q[2][FC];
+    auto fragments = [&](int buf, int kk) {
+        const half_t *s_p = s_tiles + buf * (ROWS + COLS) * BK, *s_q = s_p + ROWS * BK;
+        const int chunk = (wk * KK + kk) * 2 + (lane >> 5);
+#pragma unroll
+        for (int r = 0; r < FR; ++r) {
+            const int row = wr + r * 32 + (lane & 31);
+            p[kk & 1][r] = *reinterpret_cast<const half8*>(&s_p[row * BK + slot_of(row, chunk) * 8]);
+        }
+#pragma unroll
+        for (int c = 0; c < FC; ++c) {
+            const int row = wc + c * 32 + (lane & 31);
+            q[kk & 1][c] = *reinterpret_cast<const half8*>(&s_q[row * BK + slot_of(row, chunk) * 8]);
         }
     };
-    stage_next(0);
+    auto products = [&](int kk) {
+#pragma unroll
+        for (int r = 0; r < FR; ++r)
+#pragma unroll
+            for (int c = 0; c < FC; ++c)
+                acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[kk & 1][r], q[kk & 1][c], acc[r][c], 0, 0, 0);
+    };
+    if (STAGES <= total)
+        wait_moves<(STAGES - 1) * S::MOVES>();
+    else
+        wait_moves<0>();
+    fragments(0, 0);
+    int cur = 0;
     for (int k = 0; k < total; ++k) {
-        // this wave's moves have landed; after the barrier everyone's have,
-        // and nobody reads the other buffer any more
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        const int cur = k & 1;
-        if (k + 1 < total) stage_next(cur ^ 1);
 #pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk) {
-            const int chunk = kk * 2 + (lane >> 5);
-            half8 p[FR], q[FC];
+        for (int kk = 0; kk + 1 < KK; ++kk) {
+            fragments(cur, kk + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            products(kk);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (k + 1 < total) {
+            if (k + STAGES <= total)
+                wait_moves<(STAGES - 2) * S::MOVES>();
+            else
+                wait_moves<0>();
+            const int next = cur + 1 == STAGES ? 0 : cur + 1;
+            fragments(next, 0);
+            if (k + STAGES < total) {
+                next_tile();
 #pragma unroll
-            for (int r = 0; r < FR; ++r) {
-                const int row = wr + r * 32 + (lane & 31);
-                p[r] = *reinterpret_cast<const half8*>(&s_p[cur][row * BK + slot_of(row, chunk) * 8]);
+                for (int m = 0; m < MOVES; ++m) move(m, cur);
             }
+            cur = next;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        products(KK - 1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();   // the tiles' LDS is free
+    float* all = reinterpret_cast<float*>(s_tiles);
+    if (S::WK > 1) {
+        // sums of the waves along the depth, in order, in wave 0 of them
+        constexpr int PER = FR * FC * 16 * 64;
 #pragma unroll
-            for (int c = 0; c < FC; ++c) {
-                const int row = wc + c * 32 + (lane & 31);
-                q[c] = *reinterpret_cast<const half8*>(&s_q[cur][row * BK + slot_of(row, chunk) * 8]);
-            }
+        for (int r = 0; r < FR; ++r)
+#pragma unroll
+            for (int c = 0; c < FC; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (wk) all[((wk - 1) * S::WR * S::WC + wq) * PER + ((r * FC + c) * 16 + e) * 64 + lane] = acc[r][c][e];
+        __syncthreads();
+        if (wk) return;
+#pragma unroll
+        for (int r = 0; r < FR; ++r)
+#pragma unroll
+            for (int c = 0; c < FC; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+#pragma unroll
+                    for (int k = 0; k < S::WK - 1; ++k)
+                        acc[r][c][e] += all[(k * S::WR * S::WC + wq) * PER + ((r * FC + c) * 16 + e) * 64 + lane];
+        all += (S::WK - 1) * S::WR * S::WC * PER;
+    }
+    // A lane holds column j = lane & 31 of C and, in groups of four, rows 8 g +
+    // 4 (lane >> 5) + 0..3 of each fragment.  Through LDS it gets eight values of
+    // one row of C transposed, then of C: four lanes move 64 bytes of a row.
+    float* buf = all + wq * FRAG_FLOATS;
+    const int64_t zc = z * a.cbatch;
+    const int seg = (lane & 3) * 8, line = lane >> 2;
+    constexpr bool BOTH = SPLIT || MODE == UPDATE || MODE == FINAL;   // words of S
+#pragma unroll
+    for (int c = 0; c < FC; ++c) {
+        const int fj = j0 + wc + c * 32;
+        half8 s0[FR][2], s1[FR][2];
+        if (MODE != GRAM)
 #pragma unroll
             for (int r = 0; r < FR; ++r)
 #pragma unroll
-                for (int c = 0; c < FC; ++c)
-                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[r], q[c], acc[r][c], 0, 0, 0);
-        }
-    }
-    // lane holds column lane & 31 and, in groups of four, rows
-    // 8 g + 4 (lane >> 5) + 0..3 of each fragment
-    const int64_t zc = z * a.cbatch;
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t at = zc + (int64_t)(fj + h * 16 + line) * a.ldt + i0 + wr + r * 32 + seg;
+                    s0[r][h] = *reinterpret_cast<const half8*>(a.S[0] + at);
+                    if (BOTH) s1[r][h] = *reinterpret_cast<const half8*>(a.S[1] + at);
+                }
 #pragma unroll
-    for (int r = 0; r < FR; ++r)
-#pragma unroll
-        for (int c = 0; c < FC; ++c)
+        for (int r = 0; r < FR; ++r) {
+            const int fi = i0 + wr + r * 32;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int64_t i = i0 + wr + r * 32 + g * 8 + (lane >> 5) * 4, j = j0 + wc + c * 32 + (lane & 31);
-                half4 h4, l4;
+                typedef float float4v __attribute__((ext_vector_type(4)));
+                float4v w;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t at = zc + (i + e) * a.ldc + j;
-                    float v = acc[r][c][g * 4 + e] * a.mul;
-                    if (MODE != GRAM) {
-                        float s = (float)a.S[0][at];
-                        if (SPLIT || MODE != POLY) s += (float)a.S[1][at];
-                        v = __builtin_fmaf(s, a.add, v);
+                for (int e = 0; e < 4; ++e) w[e] = acc[r][c][g * 4 + e] * a.mul;
+                *reinterpret_cast<float4v*>(&buf[(lane & 31) * FRAG_LD + g * 8 + (lane >> 5) * 4]) = w;
+            }
+            __builtin_amdgcn_wave_barrier();
+            float8 w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = fj + h * 16 + line, i = fi + seg;
+                w[h] = *reinterpret_cast<const float8*>(&buf[(h * 16 + line) * FRAG_LD + seg]);
+                if (MODE != GRAM)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float t = BOTH ? (float)s0[r][h][e] + (float)s1[r][h][e] : (float)s0[r][h][e];
+                        w[h][e] = __builtin_fmaf(t, a.add, w[h][e]);
+                        if (MODE == POLY && i + e == j) w[h][e] += a.diag;
                     }
-                    if (MODE == POLY && i + e == j) v += a.diag;
-                    if (MODE == FINAL) {
-                        if (i + e < a.rows && j < a.cols) {
-                            const int64_t o = z * a.obatch + (a.tall ? j * a.ldo + i + e : (i + e) * a.ldo + j);
-                            if (a.otype == AT_F32)
-                                static_cast<float*>(a.out)[o] = v;
-                            else
-                                static_cast<__bf16*>(a.out)[o] = (__bf16)v;
-                        }
-                    } else {
-                        h4[e] = (half_t)v;
-                        l4[e] = (half_t)(v - (float)h4[e]);
-                        a.C[0][at] = h4[e];
-                        if (SPLIT || MODE == UPDATE) a.C[1][at] = l4[e];
-                    }
-                }
-                if (MODE == UPDATE) {
-                    const int64_t at = zc + j * a.ldt + i;
-                    *reinterpret_cast<half4*>(a.T[0] + at) = h4;
-                    if (SPLIT) *reinterpret_cast<half4*>(a.T[1] + at) = l4;
-                }
-                if ((MODE == GRAM || MODE == POLY) && bi != bj) {
-                    const int64_t at = zc + j * a.ldc + i;
-                    *reinterpret_cast<half4*>(a.C[0] + at) = h4;
-                    if (SPLIT) *reinterpret_cast<half4*>(a.C[1] + at) = l4;
+                if (MODE == FINAL) {
+                    if (a.tall) put_out(a, z, j, i, a.cols, a.rows, w[h]);
+                } else {
+                    put_words<SPLIT || MODE == UPDATE>(a.T, zc + (int64_t)j * a.ldt + i, w[h]);
                 }
             }
+            __builtin_amdgcn_wave_barrier();
+            if (MODE == FINAL ? a.tall : MODE != UPDATE && bi == bj) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) buf[(seg + e) * FRAG_LD + h * 16 + line] = w[h][e];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = fi + h * 16 + line, j = fj + seg;
+                w[h] = *reinterpret_cast<const float8*>(&buf[(h * 16 + line) * FRAG_LD + seg]);
+                if (MODE == FINAL)
+                    put_out(a, z, i, j, a.rows, a.cols, w[h]);
+                else
+                    put_words<SPLIT>(a.C, zc + (int64_t)i * a.ldc + j, w[h]);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
 }
 
-int64_t up64(int64_t x) { return (x + TILE - 1) / TILE * TILE; }
-int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+// --------------------------------------------------------------------------
+// Small matrices: every step in one workgroup
+// --------------------------------------------------------------------------
+// Both sides padded to N; one wave a fragment of 32 x 32.  X stays in
+// registers, in fp32; LDS holds two operands at a time: X then B, and A then X
+// transposed.  Rows of N, 16-byte chunk c of row r in slot c ^ r (of 16) or c ^
+// r / 2 (of 8), so that 16 rows' chunks lie in different banks.
+template <int N>
+struct Small {
+    static constexpr int FRAGS = N / 32, THREADS = FRAGS * FRAGS * 64, CHUNKS = N / 8;
+    static constexpr int MATRIX = N * N;   // half words
+    static __device__ __forceinline__ int at(int r, int c) {
+        return r * N + (((c >> 3) ^ (CHUNKS == 16 ? r & 15 : (r >> 1) & 7)) << 3) + (c & 7);
+    }
+};
 
-// The split products cost three times as many matrix instructions; a matrix of
-// up to this many rows waits on launches more than on those, and has too few
-// singular values for fp16's rounding errors to average out.
-constexpr int64_t SPLIT_MAX = 256;
+template <int N, bool SPLIT>
+__device__ __forceinline__ void small_product(const half_t* P, const half_t* Q, int fi, int fj, float16v& acc) {
+    using S = Small<N>;
+    const int lane = threadIdx.x & 63, pi = fi + (lane & 31), qj = fj + (lane & 31);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; k += 16) {
+        const int c = k + (lane >> 5) * 8;
+        const half8 p = *reinterpret_cast<const half8*>(P + S::at(pi, c));
+        const half8 q = *reinterpret_cast<const half8*>(Q + S::at(qj, c));
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p, q, acc, 0, 0, 0);
+        if (SPLIT) {
+            const half8 pl = *reinterpret_cast<const half8*>(P + S::MATRIX + S::at(pi, c));
+            const half8 ql = *reinterpret_cast<const half8*>(Q + S::MATRIX + S::at(qj, c));
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p, ql, acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, q, acc, 0, 0, 0);
+        }
+    }
+}
+
+// v, this wave's fragment, transposed into LDS: element (i, j) to row j.
+template <int N, bool SPLIT>
+__device__ __forceinline__ void small_put_t(half_t* to, int fi, int fj, const float16v& v) {
+    using S = Small<N>;
+    const int lane = threadIdx.x & 63, j = fj + (lane & 31);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int i = fi + g * 8 + (lane >> 5) * 4;
+        half4 h, l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h[e] = (half_t)v[g * 4 + e];
+            l[e] = (half_t)(v[g * 4 + e] - (float)h[e]);
+        }
+        *reinterpret_cast<half4*>(to + S::at(j, i)) = h;
+        if (SPLIT) *reinterpret_cast<half4*>(to + S::MATRIX + S::at(j, i)) = l;
+    }
+}
+template <int N, bool SPLIT>
+__device__ __forceinline__ void small_put(half_t* to, int fi, int fj, const float16v& v) {
+    using S = Small<N>;
+    const int lane = threadIdx.x & 63, j = fj + (lane & 31);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int i = fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4;
+        const half_t h = (half_t)v[e];
+        to[S::at(i, j)] = h;
+        if (SPLIT) to[S::MATRIX + S::at(i, j)] = (half_t)(v[e] - (float)h);
+    }
+}
+
+template <int DT, int N, bool SPLIT>
+__global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, int tall, float xs) {
+    using S = Small<N>;
+    using T = typename Elem<DT>::T;
+    extern __shared__ half_t s_words[];   // two operands of MATRIX words, twice that when split
+    __shared__ double s_sum[S::THREADS / 64];
+    half_t *first = s_words, *second = s_words + S::MATRIX * (SPLIT ? 2 : 1);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int fi = wave / S::FRAGS * 32, fj = wave % S::FRAGS * 32, j = fj + (lane & 31);
+    const T* x = static_cast<const T*>(a.x) + blockIdx.x * a.xbatch;
+    const int s = (int)(tall ? a.cols : a.rows), l = (int)(tall ? a.rows : a.cols);
+    const int64_t di = tall ? 1 : a.ldx, dj = tall ? a.ldx : 1;
+    float16v X, A, acc;
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int i = fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4;
+        X[e] = i < s && j < l ? (float)x[i * di + j * dj] : 0.0f;
+        sum = __builtin_fma((double)X[e], (double)X[e], sum);
+    }
+    const double norm = sqrt(block_sum<S::THREADS>(sum, s_sum));
+    const float f = (float)((double)xs / (norm + (double)a.eps));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) X[e] *= f;
+    for (int step = 0; step < a.steps; ++step) {
+        const float shift = step + 2 >= a.steps ? 0.5f * (a.b + a.c) : 0.0f;
+        small_put<N, SPLIT>(first, fi, fj, X);
+        __syncthreads();
+        small_product<N, SPLIT>(first, first, fi, fj, A);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) A[e] *= A_SCALE / (xs * xs);
+        small_put_t<N, SPLIT>(second, fi, fj, A);   // A is its transpose
+        __syncthreads();
+        small_product<N, SPLIT>(second, second, fi, fj, acc);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int i = fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4;
+            // A as its operands hold it
+            float t = (float)(half_t)A[e];
+            if (SPLIT) t += (float)(half_t)(A[e] - t);
+            acc[e] = __builtin_fmaf(t, a.b, acc[e] * (a.c / A_SCALE)) - (i == j ? shift * A_SCALE : 0.0f);
+        }
+        small_put_t<N, SPLIT>(first, fi, fj, acc);
+        __syncthreads();   // everyone has read A
+        small_put_t<N, SPLIT>(second, fi, fj, X);
+        __syncthreads();
+        small_product<N, SPLIT>(first, second, fi, fj, acc);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) X[e] = __builtin_fmaf(X[e], a.a + shift, acc[e] * (1.0f / A_SCALE));
+        __syncthreads();   // everyone has read B and X
+    }
+    const float m = a.scale / xs;
+    const int64_t oi = tall ? 1 : a.ldo, oj = tall ? a.ldo : 1, o = blockIdx.x * a.obatch;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int i = fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4;
+        if (i >= s || j >= l) continue;
+        if (a.otype == AT_F32)
+            static_cast<float*>(a.out)[o + i * oi + j * oj] = X[e] * m;
+        else
+            static_cast<__bf16*>(a.out)[o + i * oi + j * oj] = (__bf16)(X[e] * m);
+    }
+}
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// fp16 operands are off by 2^-12 each; over many singular values that
+// averages out (s = 128: 1.2 times the error that bf16's rounding has alone; 64:
+// 1.4; 16: up to 2.2), so few rows take split products, at three times the
+// matrix instructions (which small matrices do not wait for).
+constexpr int64_t SPLIT_MAX = 64;
+constexpr int64_t SMALL_MAX = 128;
 
 struct OrthoPlan {
     int64_t s, l, sp, lp;
     int tall;
     bool split;
+    int small;            // side of the one-workgroup kernel, or 0
     float xs;
     int64_t off_x[2], off_t[2][2], off_a[2], off_b[2], off_part, bytes;
 };
@@ -292,24 +651,29 @@ OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, int otype) {
     p.tall = rows > cols;
     p.s = p.tall ? cols : rows;
     p.l = p.tall ? rows : cols;
-    p.sp = up64(p.s);
-    p.lp = up64(p.l);
+    // whole tiles of the shapes that run() picks
+    const int64_t unit = p.s >= 2048 ? 256 : p.s > 512 ? 128 : TILE;
+    p.sp = round_up(p.s, unit);
+    p.lp = round_up(p.l, unit);
     p.split = otype == AT_F32 || p.s <= SPLIT_MAX;
+    p.small = p.l <= SMALL_MAX ? (p.l <= 64 ? 64 : 128) : 0;
     // the power of two next to sqrt(s l)
     double f = 1.0;
     while (f < 4096.0 && f * f * 2.0 < (double)p.s * (double)p.l) f *= 2.0;
     p.xs = (float)f;
+    if (p.small) return p;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t off = at;
-        at = up256(at + bytes);
+        at = round_up(at + bytes, 256);
         return off;
     };
     const int64_t x = batch * p.sp * p.lp * 2, sq = batch * p.sp * p.sp * 2;
     for (int h = 0; h < 2; ++h) {
         const bool used = h == 0 || p.split;
-        p.off_x[h] = take(x);
-        for (int t = 0; t < 2; ++t) p.off_t[t][h] = take(used ? x : 0);
+        p.off_x[h] = take(used ? x : 0);
+        p.off_t[0][h] = take(x);
+        p.off_t[1][h] = used ? take(x) : p.off_t[0][h];
         p.off_a[h] = take(used ? sq : 0);
         p.off_b[h] = take(used ? sq : 0);
     }
@@ -318,11 +682,48 @@ OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, int otype) {
     return p;
 }
 
-template <int MODE, bool SPLIT>
-void gemm(const GemmArgs& a, int64_t batch, hipStream_t stream) {
+// Tile shapes, by how many workgroups they make (us for 2 x 1024 x 4096: A 25,
+// B 42; X 39 and 31; for 4096 x 4096: X with 64 by 64 not measured, 128 by 128
+// 149 to 155, 256 by 256 131).
+using Tile64 = Shape<2, 2, 1, 1, 1, 3>;
+using Tile128 = Shape<2, 4, 1, 2, 1, 2>;
+using Tile256 = Shape<2, 4, 1, 4, 2, 2>;
+
+template <class S, int MODE, bool SPLIT>
+hipError_t gemm_as(GemmArgs a, int64_t batch, hipStream_t stream) {
+    static std::atomic<uint64_t> ready{0};
+    const hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_gemm<S, MODE, SPLIT>), 0, S::LDS, ready);
+    if (e != hipSuccess) return e;
+    a.ti /= S::ROWS / TILE;
+    a.tj /= S::COLS / TILE;
     const bool sym = MODE == GRAM || MODE == POLY;
-    const int tiles = sym ? a.ti * (a.ti + 1) / 2 : a.ti * a.tj;
-    hipLaunchKernelGGL((k_gemm<TILE, TILE, MODE, SPLIT>), dim3(tiles, (unsigned)batch), dim3(GEMM_THREADS), 0, stream, a);
+    const int64_t tiles = sym ? (int64_t)a.ti * (a.ti + 1) / 2 : (int64_t)a.ti * a.tj;
+    hipLaunchKernelGGL((k_gemm<S, MODE, SPLIT>), dim3((unsigned)(tiles * batch)), dim3(S::THREADS), S::LDS, stream, a);
+    return hipGetLastError();
+}
+template <int MODE, bool SPLIT>
+hipError_t gemm(const GemmArgs& a, int64_t batch, hipStream_t stream) {
+    auto fills = [&](int64_t side) {   // whole tiles of this side, and one for every CU
+        const int64_t r = side / TILE;
+        if (a.ti % r || a.tj % r) return false;
+        const int64_t i = a.ti / r, j = a.tj / r;
+        return batch * (MODE == GRAM || MODE == POLY ? i * (i + 1) / 2 : i * j) >= 256;
+    };
+    if ((MODE == UPDATE || MODE == FINAL) && fills(256)) return gemm_as<Tile256, MODE, SPLIT>(a, batch, stream);
+    if (fills(128)) return gemm_as<Tile128, MODE, SPLIT>(a, batch, stream);
+    return gemm_as<Tile64, MODE, SPLIT>(a, batch, stream);
+}
+
+template <int DT, int N, bool SPLIT>
+hipError_t launch_small(const OrthoArgs& o, const OrthoPlan& p, hipStream_t stream) {
+    using S = Small<N>;
+    constexpr size_t lds = (size_t)S::MATRIX * 2 * (SPLIT ? 4 : 2);
+    static std::atomic<uint64_t> ready{0};
+    const hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_ortho_small<DT, N, SPLIT>), -1, lds, ready);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_ortho_small<DT, N, SPLIT>), dim3((unsigned)o.batch), dim3(S::THREADS), lds, stream, o, p.tall,
+                       p.xs);
+    return hipGetLastError();
 }
 
 template <bool SPLIT>
@@ -331,35 +732,38 @@ hipError_t run_steps(const OrthoArgs& o, const OrthoPlan& p, const OrthoBufs& b,
     const int64_t xb = p.sp * p.lp, sb = p.sp * p.sp;
     for (int step = 0; step < o.steps; ++step) {
         const float shift = step + 2 >= o.steps ? 0.5f * (o.b + o.c) : 0.0f;
+        hipError_t e = hipSuccess;
         GemmArgs g{};
         for (int h = 0; h < 2; ++h) {
             g.P[h] = g.Q[h] = b.X[h];
-            g.C[h] = b.A[h];
+            g.T[h] = g.C[h] = b.A[h];
         }
         g.pbatch = g.qbatch = xb;
         g.depth = g.ldp = g.ldq = lp;
         g.ti = g.tj = sp / TILE;
         g.cbatch = sb;
-        g.ldc = sp;
+        g.ldt = g.ldc = sp;
         g.mul = A_SCALE / (p.xs * p.xs);
-        gemm<GRAM, SPLIT>(g, o.batch, stream);
+        e = gemm<GRAM, SPLIT>(g, o.batch, stream);
         for (int h = 0; h < 2; ++h) {
             g.P[h] = g.Q[h] = b.A[h];
             g.S[h] = b.A[h];
-            g.C[h] = b.B[h];
+            g.T[h] = g.C[h] = b.B[h];
         }
         g.pbatch = g.qbatch = sb;
         g.depth = g.ldp = g.ldq = sp;
         g.mul = o.c / A_SCALE;
         g.add = o.b;
         g.diag = -shift * A_SCALE;
-        gemm<POLY, SPLIT>(g, o.batch, stream);
+        if (e == hipSuccess) e = gemm<POLY, SPLIT>(g, o.batch, stream);
+        if (e != hipSuccess) return e;
         GemmArgs u{};
         for (int h = 0; h < 2; ++h) {
             u.P[h] = b.B[h];
             u.Q[h] = b.XT[step & 1][h];
-            u.S[h] = u.C[h] = b.X[h];
+            u.S[h] = b.XT[step & 1][h];
             u.T[h] = b.XT[(step & 1) ^ 1][h];
+            u.C[h] = b.X[h];
         }
         u.pbatch = sb;
         u.qbatch = xb;
@@ -381,11 +785,10 @@ hipError_t run_steps(const OrthoArgs& o, const OrthoPlan& p, const OrthoBufs& b,
             u.rows = (int)p.s;
             u.cols = (int)p.l;
             u.tall = p.tall;
-            gemm<FINAL, SPLIT>(u, o.batch, stream);
+            e = gemm<FINAL, SPLIT>(u, o.batch, stream);
         } else {
-            gemm<UPDATE, SPLIT>(u, o.batch, stream);
+            e = gemm<UPDATE, SPLIT>(u, o.batch, stream);
         }
-        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -399,6 +802,13 @@ int64_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, int otype) {
 
 hipError_t launch_ortho(const OrthoArgs& o, void* workspace, hipStream_t stream) {
     const OrthoPlan p = plan_ortho(o.batch, o.rows, o.cols, o.otype);
+    if (p.small)
+        return with_type(o.xtype, [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            if (p.small == 64)
+                return p.split ? launch_small<DT, 64, true>(o, p, stream) : launch_small<DT, 64, false>(o, p, stream);
+            return p.split ? launch_small<DT, 128, true>(o, p, stream) : launch_small<DT, 128, false>(o, p, stream);
+        });
     char* ws = static_cast<char*>(workspace);
     OrthoBufs b{};
     auto buf = [&](int64_t off) { return reinterpret_cast<half_t*>(ws + off); };
@@ -413,7 +823,7 @@ hipError_t launch_ortho(const OrthoArgs& o, void* workspace, hipStream_t stream)
     const int sp = (int)p.sp, lp = (int)p.lp;
     const hipError_t e = with_type(o.xtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        const dim3 grid(lp / TILE, sp / TILE, (unsigned)o.batch);
+        const dim3 grid((p.tall ? sp : lp) / TILE, (p.tall ? lp : sp) / TILE, (unsigned)o.batch);
         hipLaunchKernelGGL((k_norm<DT>), dim3(NORM_BLOCKS, (unsigned)o.batch), dim3(NORM_THREADS), 0, stream, o, b.part);
         if (p.split)
             hipLaunchKernelGGL((k_layout<DT, true>), grid, dim3(256), 0, stream, o, b, sp, lp, p.tall, p.xs);
