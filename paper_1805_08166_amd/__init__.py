@@ -12,6 +12,7 @@ The library must have been built (``python -m paper_1805_08166_amd.build`` or
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -513,15 +514,35 @@ def entries(t) -> np.ndarray:
 AT_F32, AT_BF16, AT_F16 = 0, 1, 2
 AT_I32, AT_I64 = 0, 1
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
-_TYPES = None
+
+
+class _Torch:
+    """What these bindings need of torch, looked up once: a call costs a few
+    microseconds, which is what the smallest of these operators take."""
+
+    def __init__(self):
+        import torch
+        self.torch = torch
+        self.types = {torch.float32: AT_F32, torch.bfloat16: AT_BF16, torch.float16: AT_F16}
+        self.itypes = {torch.int32: AT_I32, torch.int64: AT_I64}
+        self.f32, self.i32 = torch.float32, torch.int32
+        # the current stream's handle, without the object around it where torch has that
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+_torch_parts = None
+
+
+def _T() -> _Torch:
+    global _torch_parts
+    if _torch_parts is None:
+        _torch_parts = _Torch()
+    return _torch_parts
 
 
 def _type(t, name):
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: AT_F32, torch.bfloat16: AT_BF16, torch.float16: AT_F16}
-    c = _TYPES.get(t.dtype)
+    c = _T().types.get(t.dtype)
     if c is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
     return c
@@ -531,71 +552,76 @@ def _rows(t, name, rows=None, cols=None):
     """(pointer, element type, row stride) of a device tensor [rows, cols]."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    sh, st = t.shape, t.stride()
+    sh = t.shape
     if len(sh) != 2 or (rows is not None and sh[0] != rows) or (cols is not None and sh[1] != cols):
         raise ValueError(f"{name} must be [{'n' if rows is None else rows}, {'n' if cols is None else cols}], "
                          f"got {list(sh)}")
+    st = t.stride()
     if sh[1] > 1 and st[1] != 1:
         raise ValueError(f"{name} must have contiguous rows")
     return t.data_ptr(), _type(t, name), (st[0] if sh[0] > 1 else max(st[0], sh[1]))
 
 
 def _vec(t, n, dtype, name):
+    """Pointer of a contiguous device tensor of n values, or None."""
     if t is None:
         return None
     if t.dtype != dtype or t.numel() != n:
         raise ValueError(f"{name} must hold {n} values of {dtype}")
-    return _dev(t, None, name)
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    return t.data_ptr()
 
 
 def _tokens(t, n=None):
     """(pointer, token type, count) of an int32 or int64 device tensor."""
-    import torch
-    if t.dtype not in (torch.int32, torch.int64):
+    ti = _T().itypes.get(t.dtype)
+    if ti is None:
         raise ValueError(f"tokens must be int32 or int64, got {t.dtype}")
-    if n is not None and t.numel() != n:
+    m = t.numel()
+    if n is not None and m != n:
         raise ValueError(f"tokens must hold {n} values")
-    return _dev(t, None, "tokens"), (AT_I64 if t.dtype == torch.int64 else AT_I32), t.numel()
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("tokens must be a contiguous device tensor")
+    return t.data_ptr(), ti, m
 
 
-class _on:
-    """The call's device made current, and its stream: `stream`, or the current
-    one of that device.  Every tensor must be on the first one's device."""
-
-    def __init__(self, stream, *tensors):
-        import torch
-        self.dev = tensors[0].device
-        for t in tensors:
-            if t is not None and t.device != self.dev:
-                raise ValueError("tensors are on different devices")
-        self.stream = torch.cuda.current_stream(self.dev) if stream is None else stream
-        self.guard = None
-
-    def __enter__(self):
-        import torch
-        if torch.cuda.current_device() != self.dev.index:
-            self.guard = torch.cuda.device(self.dev)
-            self.guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-        return False
-
-    def workspace(self, given, nbytes):
-        """(tensor kept alive, pointer, bytes)."""
-        import torch
-        if given is None:
-            if not nbytes:
-                return None, None, 0
-            with torch.cuda.stream(self.stream):
-                given = torch.empty(nbytes, dtype=torch.uint8, device=self.dev)
-        elif given.device != self.dev:
-            raise ValueError("workspace is on another device")
-        return given, _dev(given, torch.uint8, "workspace"), given.numel()
+def _one_device(*tensors) -> int:
+    d = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors are on different devices")
+    return d
 
 
+def _call(func, device: int, stream, args, workspace=None, need: int = 0):
+    """Calls the library on `device`, with `stream` or the device's current one
+    as the last argument; where the call takes a workspace (need >= 0, the bytes),
+    its pointer and size come before the stream."""
+    T = _T()
+    torch = T.torch
+    if torch.cuda.current_device() != device:
+        with torch.cuda.device(device):
+            return _call(func, device, stream, args, workspace, need)
+    if need >= 0:
+        if workspace is None:
+            if not need:
+                args += (None, 0)
+            elif stream is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            else:   # torch's allocator ties memory to the stream it is taken on
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if workspace is not None:
+            if workspace.get_device() != device:
+                raise ValueError("workspace is on another device")
+            args += (_vec(workspace, workspace.numel(), torch.uint8, "workspace"), workspace.numel())
+    st = getattr(_lib, func)(*args, T.stream(device) if stream is None else stream.cuda_stream)
+    if st:
+        _check(func, st)
+
+
+@functools.lru_cache(maxsize=256)
 def _bytes(func, *sizes) -> int:
     v = ctypes.c_int64()
     _check(func, getattr(_lib, func)(*sizes, ctypes.byref(v)))
@@ -608,10 +634,10 @@ def at_embed(weight, tokens, out, scale: float = 1.0, stream=None):
     weight and out each float32, bfloat16 or float16."""
     tp, ti, n = _tokens(tokens)
     wp, wt, lw = _rows(weight, "weight")
-    op, ot, lo = _rows(out, "out", n, weight.shape[1])
-    with _on(stream, weight, tokens, out) as on:
-        _check("at_embed", _lib.at_embed(wp, wt, lw, weight.shape[0], weight.shape[1], tp, ti, n, scale, op, ot, lo,
-                                         on.stream.cuda_stream))
+    vocab, dim = weight.shape
+    op, ot, lo = _rows(out, "out", n, dim)
+    _call("at_embed", _one_device(weight, tokens, out), stream,
+          (wp, wt, lw, vocab, dim, tp, ti, n, scale, op, ot, lo), need=-1)
 
 
 def at_embed_grad_workspace(n: int, vocab: int, dim: int) -> int:
@@ -623,14 +649,12 @@ def at_embed_grad(dout, tokens, dweight, scale: float = 1.0, accumulate: bool = 
     added to dweight with accumulate.  dout: [n, dim]; tokens: int32 or int64
     [n]; dweight: [vocab, dim]."""
     tp, ti, n = _tokens(tokens)
+    gp, gt, lg = _rows(dweight, "dweight")
     vocab, dim = dweight.shape
     dp, dt, ld = _rows(dout, "dout", n, dim)
-    gp, gt, lg = _rows(dweight, "dweight")
-    with _on(stream, dout, tokens, dweight) as on:
-        need = _bytes("at_embed_grad_workspace", n, vocab, dim) if workspace is None else 0
-        keep, wp, wb = on.workspace(workspace, need)
-        _check("at_embed_grad", _lib.at_embed_grad(dp, dt, ld, tp, ti, n, scale, 1 if accumulate else 0, gp, gt, lg,
-                                                   vocab, dim, wp, wb, on.stream.cuda_stream))
+    _call("at_embed_grad", _one_device(dout, tokens, dweight), stream,
+          (dp, dt, ld, tp, ti, n, scale, 1 if accumulate else 0, gp, gt, lg, vocab, dim), workspace,
+          _bytes("at_embed_grad_workspace", n, vocab, dim))
 
 
 def at_logprobs_workspace(n: int, vocab: int, k: int) -> int:
@@ -645,9 +669,9 @@ def at_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_logp
     int32 [n], the columns that each row has, or None; logp, entropy, lse:
     float32 [n]; top_logp: float32 [n, k]; top_idx: int32 [n, k]; an output
     that is None is not computed."""
-    import torch
-    n, vocab = logits.shape
+    T = _T()
     xp, xt, ld = _rows(logits, "logits")
+    n, vocab = logits.shape
     tp, ti, _ = _tokens(tokens, n) if tokens is not None else (None, AT_I32, n)
     k = 0
     for t in (top_logp, top_idx):
@@ -655,14 +679,10 @@ def at_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_logp
             if t.dim() != 2 or t.shape[0] != n or (k and t.shape[1] != k):
                 raise ValueError("top_logp and top_idx must be [n, k]")
             k = t.shape[1]
-    f32 = torch.float32
-    with _on(stream, logits, tokens, logp, entropy, lse, top_logp, top_idx, valid) as on:
-        need = _bytes("at_logprobs_workspace", n, vocab, k) if workspace is None else 0
-        keep, wp, wb = on.workspace(workspace, need)
-        _check("at_logprobs", _lib.at_logprobs(
-            xp, xt, ld, n, vocab, _vec(valid, n, torch.int32, "valid"), tp, ti, scale, k, _vec(logp, n, f32, "logp"),
-            _vec(entropy, n, f32, "entropy"), _vec(lse, n, f32, "lse"), _vec(top_logp, n * k, f32, "top_logp"),
-            _vec(top_idx, n * k, torch.int32, "top_idx"), wp, wb, on.stream.cuda_stream))
+    _call("at_logprobs", _one_device(logits, tokens, logp, entropy, lse, top_logp, top_idx, valid), stream,
+          (xp, xt, ld, n, vocab, _vec(valid, n, T.i32, "valid"), tp, ti, scale, k, _vec(logp, n, T.f32, "logp"),
+           _vec(entropy, n, T.f32, "entropy"), _vec(lse, n, T.f32, "lse"), _vec(top_logp, n * k, T.f32, "top_logp"),
+           _vec(top_idx, n * k, T.i32, "top_idx")), workspace, _bytes("at_logprobs_workspace", n, vocab, k))
 
 
 def at_logprobs_grad(logits, tokens, lse, entropy, dlogp, dlogits, dentropy=None, valid=None, scale: float = 1.0,
@@ -670,19 +690,17 @@ def at_logprobs_grad(logits, tokens, lse, entropy, dlogp, dlogits, dentropy=None
     """Gradient of at_logprobs with respect to its logits, from those of logp and
     entropy (float32 [n], or None for zero) and the forward call's lse and
     entropy.  dlogits: [n, vocab] of the logits' type."""
-    import torch
-    n, vocab = logits.shape
+    T = _T()
     xp, xt, ld = _rows(logits, "logits")
+    n, vocab = logits.shape
     dp, dt, ldd = _rows(dlogits, "dlogits", n, vocab)
     if dt != xt:
         raise ValueError("dlogits must have the logits' type")
     tp, ti, _ = _tokens(tokens, n) if tokens is not None else (None, AT_I32, n)
-    f32 = torch.float32
-    with _on(stream, logits, tokens, lse, entropy, dlogp, dlogits, dentropy, valid) as on:
-        _check("at_logprobs_grad", _lib.at_logprobs_grad(
-            xp, xt, ld, n, vocab, _vec(valid, n, torch.int32, "valid"), tp, ti, scale, _vec(lse, n, f32, "lse"),
-            _vec(entropy, n, f32, "entropy"), _vec(dlogp, n, f32, "dlogp"), _vec(dentropy, n, f32, "dentropy"), dp, ldd,
-            on.stream.cuda_stream))
+    _call("at_logprobs_grad", _one_device(logits, tokens, lse, entropy, dlogp, dlogits, dentropy, valid), stream,
+          (xp, xt, ld, n, vocab, _vec(valid, n, T.i32, "valid"), tp, ti, scale, _vec(lse, n, T.f32, "lse"),
+           _vec(entropy, n, T.f32, "entropy"), _vec(dlogp, n, T.f32, "dlogp"), _vec(dentropy, n, T.f32, "dentropy"), dp,
+           ldd), need=-1)
 
 
 def _matrices(t, name):
@@ -715,9 +733,6 @@ def at_orthogonalize(x, out, steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e
     rows, cols = x.shape[-2:]
     a, b, c = coef
     ot = _type(out, "out")
-    with _on(stream, x, out) as on:
-        need = _bytes("at_orthogonalize_workspace", batch, rows, cols, ot) if workspace is None else 0
-        keep, wp, wb = on.workspace(workspace, need)
-        _check("at_orthogonalize", _lib.at_orthogonalize(xp, _type(x, "x"), xb, ldx, batch, rows, cols, steps, a, b, c,
-                                                         eps, scale, op, ot, ob, ldo, wp, wb,
-                                                         on.stream.cuda_stream))
+    _call("at_orthogonalize", _one_device(x, out), stream,
+          (xp, _type(x, "x"), xb, ldx, batch, rows, cols, steps, a, b, c, eps, scale, op, ot, ob, ldo), workspace,
+          _bytes("at_orthogonalize_workspace", batch, rows, cols, ot))

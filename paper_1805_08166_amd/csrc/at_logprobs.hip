@@ -25,13 +25,44 @@ constexpr int LP_WAVES = LP_THREADS / 64;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// The word of lane (lane ^ O): moves between lanes of the vector unit, a few
+// cycles each, where a shuffle goes through LDS.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+template <int O>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+    if constexpr (O == 1) return dpp<0xb1>(x);                // quad_perm 1 0 3 2
+    if constexpr (O == 2) return dpp<0x4e>(x);                // quad_perm 2 3 0 1
+    if constexpr (O == 4) return dpp<0x1b>(dpp<0x141>(x));    // ^ 7, then ^ 3
+    if constexpr (O == 8) return dpp<0x128>(x);               // row_ror 8
+    if constexpr (O == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    }
+    if constexpr (O == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+    if constexpr (O == 63) return lane_xor<32>(lane_xor<16>(dpp<0x140>(x)));   // ^ 15, 16, 32
+}
+template <int O>
+__device__ __forceinline__ float lane_xor(float x) {
+    return __uint_as_float(lane_xor<O>(__float_as_uint(x)));
+}
+// The word of the lane before; lane 0 keeps its own.
+__device__ __forceinline__ uint32_t lane_before(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x138, 0xf, 0xf, false);   // wave_shr 1
+}
+
 // Running softmax sums.  y below -1000 weighs nothing; the bound keeps
-// 0 * -inf out of u.
+// 0 * -inf out of u.  A NaN y is lost here, but s has it.
 struct Stat {
     float m, s, u;
 };
 __device__ __forceinline__ Stat stat_empty() { return Stat{LOWEST, 0.0f, 0.0f}; }
-__device__ __forceinline__ float bounded(float y) { return y < -1000.0f ? -1000.0f : y; }   // keeps NaN
+__device__ __forceinline__ float bounded(float y) { return fmaxf(y, -1000.0f); }
 
 __device__ __forceinline__ void stat_rescale(Stat& a, float m, float c) {
     const float d = bounded((a.m - m) * c), f = exp2_fast(d);
@@ -45,128 +76,252 @@ __device__ __forceinline__ Stat stat_join(Stat a, Stat b, float c) {
     stat_rescale(b, m, c);
     return Stat{m, a.s + b.s, a.u + b.u};
 }
+template <int O>
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, lane_xor<O>(x));
+    if constexpr (O > 1) return wave_max<O / 2>(x);
+    return x;
+}
+template <int O>
+__device__ __forceinline__ float wave_sum(float x) {
+    x += lane_xor<O>(x);
+    if constexpr (O > 1) return wave_sum<O / 2>(x);
+    return x;
+}
+// The wave's, in every lane.
 __device__ __forceinline__ Stat stat_wave(Stat a, float c) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const Stat b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.u, o)};
-        a = stat_join(a, b, c);
-    }
-    return a;
+    stat_rescale(a, wave_max<32>(a.m), c);
+    return Stat{a.m, wave_sum<32>(a.s), wave_sum<32>(a.u)};
 }
 
-// A wave's best values: lane l holds the l-th, higher values first and among
-// equal ones the lower index; empty places hold -inf and the index -1.
+// A value and its column as one number that is larger for the larger value and,
+// among equal ones, for the lower column.  No value: 0x007fffff00000000, that
+// of -inf in column 2^32 - 1.
 struct Best {
-    float v;
-    uint32_t i;
+    uint64_t key;
+    __device__ __forceinline__ float value() const {
+        const uint32_t u = (uint32_t)(key >> 32);
+        return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+    }
+    __device__ __forceinline__ uint32_t column() const { return ~(uint32_t)key; }
 };
-__device__ __forceinline__ Best best_empty() { return Best{-__builtin_inff(), 0xffffffffu}; }
-__device__ __forceinline__ bool better(const Best& a, const Best& b) { return a.v > b.v || (a.v == b.v && a.i < b.i); }
-
-__device__ __forceinline__ float lane_value(float v, int lane) {
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+__device__ __forceinline__ Best best_empty() { return Best{(uint64_t)0x007fffffu << 32}; }
+__device__ __forceinline__ Best best_of(float v, uint32_t column) {
+    const uint32_t u = __float_as_uint(v + 0.0f);   // -0 is 0
+    const uint32_t ordered = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return Best{(uint64_t)ordered << 32 | (uint32_t)~column};
+}
+__device__ __forceinline__ bool better(Best a, Best b) { return a.key > b.key; }
+template <int O>
+__device__ __forceinline__ Best best_from(Best a) {
+    return Best{(uint64_t)lane_xor<O>((uint32_t)(a.key >> 32)) << 32 | lane_xor<O>((uint32_t)a.key)};
+}
+__device__ __forceinline__ Best best_lane(Best a, int lane) {
+    return Best{(uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(a.key >> 32), lane) << 32 |
+                (uint32_t)__builtin_amdgcn_readlane((int)a.key, lane)};
 }
 
-// v beats the k-th value and no value equal to it comes later in the list's
-// index order.
-__device__ __forceinline__ void best_insert(Best& b, float v, uint32_t i) {
+// A wave's best values are one a lane, sorted.  n takes its place in them; the
+// last falls out.
+__device__ __forceinline__ void best_insert(Best& b, Best n) {
     const int lane = threadIdx.x & 63;
-    const int at = __popcll(__ballot(b.v >= v));
-    const float pv = __shfl_up(b.v, 1);
-    const uint32_t pi = __shfl_up(b.i, 1);
-    if (lane == at) b = Best{v, i};
-    if (lane > at) b = Best{pv, pi};
+    const int at = __popcll(__ballot(better(b, n)));
+    const Best prev{(uint64_t)lane_before((uint32_t)(b.key >> 32)) << 32 | lane_before((uint32_t)b.key)};
+    if (lane == at) b = n;
+    if (lane > at) b = prev;
+}
+
+// One exchange of a bitonic network: lanes whose bit O is as their bit RUN (64:
+// clear) take the better of the pair, the others the worse.
+template <int O, int RUN>
+__device__ __forceinline__ void best_exchange(Best& a) {
+    const int lane = threadIdx.x & 63;
+    const Best q = best_from<O>(a);
+    if (better(q, a) == (((lane & O) == 0) == ((lane & RUN) == 0))) a = q;
+}
+template <int O, int RUN>
+__device__ __forceinline__ void best_exchanges(Best& a) {
+    best_exchange<O, RUN>(a);
+    if constexpr (O > 1) best_exchanges<O / 2, RUN>(a);
+}
+// Sorts over the lanes, best first.
+__device__ __forceinline__ Best best_sort(Best a) {
+    best_exchanges<1, 2>(a);
+    best_exchanges<2, 4>(a);
+    best_exchanges<4, 8>(a);
+    best_exchanges<8, 16>(a);
+    best_exchanges<16, 32>(a);
+    best_exchanges<32, 64>(a);
+    return a;
 }
 
 // The 64 best of two sorted lists, sorted: the pairwise best of one and the
 // other reversed, then a bitonic merge.
 __device__ __forceinline__ Best best_merge(Best a, Best b) {
-    const int lane = threadIdx.x & 63;
-    b = Best{__shfl_xor(b.v, 63), (uint32_t)__shfl_xor(b.i, 63)};
+    b = best_from<63>(b);
     if (better(b, a)) a = b;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const Best q{__shfl_xor(a.v, o), (uint32_t)__shfl_xor(a.i, o)};
-        const bool low = (lane & o) == 0;
-        if (better(q, a) == low) a = q;
-    }
+    best_exchanges<32, 64>(a);
     return a;
+}
+
+// A batch with more values for the list than this has them sorted, 64 at a time,
+// and merged into it (about 200 instructions); otherwise they are inserted one
+// by one (about 20 each).
+constexpr int INSERTIONS = 8;
+
+// The larger of three, one instruction.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
 // One row segment [c0, c1) walked by `waves` waves of a workgroup, this one
 // the w-th: statistics a lane, best values a wave.
 template <class T, bool TOP>
-__device__ __forceinline__ void walk(const T* x, int64_t c0, int64_t c1, int w, int waves, float c, int k, Stat& st,
-                                     Best& best) {
-    constexpr int VEC = 16 / sizeof(T);
-    constexpr int SPAN = 64 * VEC;
-    const int lane = threadIdx.x & 63;
-    float kth = -__builtin_inff();
-    for (int64_t b = c0 + (int64_t)w * SPAN; b < c1; b += (int64_t)waves * SPAN) {
-        const int64_t j = b + lane * VEC;
-        float v[VEC];
-        if (b + SPAN <= c1) {
-            const Pack<T, VEC> r = load_pack<T, VEC>(x + j);
+struct Walk {
+    static constexpr int VEC = 16 / sizeof(T), SPAN = 64 * VEC;
+    Stat& st;
+    Best& best;
+    const float c;
+    const int k;
+    volatile float* shared;    // the k-th values of the workgroup's waves, or null
+    volatile uint64_t* room;   // 128 keys of this wave's in LDS
+    float bar = -__builtin_inff();   // the list's k-th value
+    bool listed = false;
+
+    __device__ __forceinline__ Best kth() const { return best_lane(best, k - 1); }
+    // v's places in the batch at column b that `in` names, into the list.
+    __device__ __forceinline__ void add(const float (&v)[VEC], const uint64_t (&in)[VEC], int64_t b) {
+        const int lane = threadIdx.x & 63;
+        int total = 0;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = (float)r.v[e];
-        } else {
+        for (int e = 0; e < VEC; ++e) total += __popcll(in[e]);
+        if (total <= INSERTIONS) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = j + e < c1 ? (float)x[j + e] : -__builtin_inff();
+            for (int e = 0; e < VEC; ++e)
+                for (uint64_t m = in[e]; m; m &= m - 1) {
+                    const int l = __ffsll((unsigned long long)m) - 1;
+                    const float x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v[e]), l));
+                    best_insert(best, best_of(x, (uint32_t)(b + l * VEC + e)));
+                }
+            return;
         }
-        float top = v[0];
-#pragma unroll
-        for (int e = 1; e < VEC; ++e) top = fmaxf(top, v[e]);
-        if (top > st.m) stat_rescale(st, top, c);
+        int count = 0;
+        auto flush = [&](int n) {
+            __builtin_amdgcn_wave_barrier();
+            const Best have = lane < n ? Best{room[lane]} : best_empty();
+            best = best_merge(best, best_sort(have));
+        };
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const float y = (v[e] - st.m) * c, p = exp2_fast(y);
-            st.s += p;
-            st.u = __builtin_fmaf(p, bounded(y), st.u);
+            if (in[e] == 0) continue;
+            if (in[e] >> lane & 1)
+                room[count + __popcll(in[e] & (((uint64_t)1 << lane) - 1))] = best_of(v[e], (uint32_t)(b + lane * VEC + e)).key;
+            count += __popcll(in[e]);
+            if (count < 64) continue;
+            flush(64);
+            count -= 64;
+            const uint64_t rest = room[64 + lane];
+            __builtin_amdgcn_wave_barrier();
+            room[lane] = rest;
         }
-        if (TOP) {
-            uint64_t more = __ballot(top > kth);
-            while (more) {
-                const int l = __ffsll((unsigned long long)more) - 1;
+        if (count) flush(count);
+    }
+
+    // The batch of columns b .. b + SPAN - 1.
+    __device__ __forceinline__ void take(float (&v)[VEC], int64_t b) {
+        const int lane = threadIdx.x & 63;
+        float top = max3(v[0], v[1], v[2]);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float q = lane_value(v[e], l);
-                    if (q > kth) {
-                        best_insert(best, q, (uint32_t)(b + l * VEC + e));
-                        kth = lane_value(best.v, k - 1);
-                    }
-                }
-                more &= more - 1;
-                more &= __ballot(top > kth);
+        for (int e = 3; e + 1 < VEC; e += 2) top = max3(top, v[e], v[e + 1]);
+        if (VEC % 2 == 0) top = max3(top, top, v[VEC - 1]);
+        if (top > st.m) stat_rescale(st, top, c);
+        const float mc = st.m * c;
+        if (__ballot(!(fabsf(mc) < 1e30f)) == 0) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float y = __builtin_fmaf(v[e], c, -mc), p = exp2_fast(y);
+                st.s += p;
+                st.u = __builtin_fmaf(p, bounded(y), st.u);
+            }
+        } else {   // some lane has seen nothing but a mask's lowest value, whose product overflows
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float y = (v[e] - st.m) * c, p = exp2_fast(y);
+                st.s += p;
+                st.u = __builtin_fmaf(p, bounded(y), st.u);
             }
         }
+        if (!TOP) return;
+        // Batches come in ascending columns, so that a value no better than the
+        // k-th loses to it; one below another wave's k-th is not among the row's k.
+        uint64_t in[VEC];
+        if (!listed) {
+            // the lanes' best values first: they tell most of the others apart
+            const uint32_t j = (uint32_t)(b + lane * VEC);
+            float m = -__builtin_inff();
+            int at = -1;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (v[e] > m) {
+                    m = v[e];
+                    at = e;
+                }
+            if (__ballot(at >= 0) == 0) return;
+            best = best_sort(at >= 0 ? best_of(m, j + at) : best_empty());
+            listed = true;
+            const Best last = kth();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                in[e] = __ballot(e != at && v[e] > -__builtin_inff() && better(best_of(v[e], j + e), last));
+        } else {
+            if (__ballot(top > bar) == 0) return;
+            float others = -__builtin_inff();
+            if (shared) {
+#pragma unroll
+                for (int q = 0; q < LP_WAVES; ++q) others = fmaxf(others, shared[q]);
+                if (__ballot(top > bar && top >= others) == 0) return;
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) in[e] = __ballot(v[e] > bar && v[e] >= others);
+        }
+        add(v, in, b);
+        bar = kth().value();
+        if (shared) shared[threadIdx.x >> 6] = bar;
     }
-}
 
-// What a row's outputs are once its sums are known.  A row with nothing in it
-// has s == 0 (or a scaled maximum of -inf); a NaN or +inf among its values
-// makes s NaN.
-__device__ __forceinline__ void put_row(const LogprobsArgs& a, int64_t row, Stat st, float xt, bool given, bool inside) {
-    const bool empty = st.s == 0.0f || st.m * a.scale == -__builtin_inff();
-    const float ls = __builtin_logf(st.s);
-    const float lse = empty ? -__builtin_inff() : __builtin_fmaf(st.m, a.scale, ls);
-    if (a.lse) a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = empty ? 0.0f : ls - LN2 * (st.u / st.s);
-    if (a.logp) {
-        float lp = (xt - st.m) * a.scale - ls;
-        if (!inside || empty) lp = -__builtin_inff();
-        if (st.s != st.s) lp = st.s;
-        a.logp[row] = given ? lp : 0.0f;
+    // Whole batches, the next one on its way while one is worked on, then the
+    // rest.
+    __device__ __forceinline__ void run(const T* x, int64_t c0, int64_t c1, int w, int waves) {
+        const int lane = threadIdx.x & 63;
+        const int64_t step = (int64_t)waves * SPAN;
+        int64_t b = c0 + (int64_t)w * SPAN;
+        float v[VEC];
+        if (b + SPAN <= c1) {
+            typedef uint32_t raw __attribute__((ext_vector_type(4)));
+            raw next;
+            __builtin_memcpy(&next, x + b + lane * VEC, 16);
+            for (; b + SPAN <= c1; b += step) {
+                const raw now = next;
+                if (b + step + SPAN <= c1) __builtin_memcpy(&next, x + b + step + lane * VEC, 16);
+                Pack<T, VEC> r;
+                __builtin_memcpy(&r, &now, 16);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[e] = (float)r.v[e];
+                take(v, b);
+            }
+        }
+        if (b < c1) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const int64_t j = b + lane * VEC + e;
+                v[e] = j < c1 ? (float)x[j] : -__builtin_inff();
+            }
+            take(v, b);
+        }
     }
-}
-__device__ __forceinline__ void put_best(const LogprobsArgs& a, int64_t row, Stat st, Best b) {
-    const int lane = threadIdx.x & 63;
-    if (lane >= a.k) return;
-    const bool poisoned = st.s != st.s, none = b.v * a.scale == -__builtin_inff();
-    if (a.top_logp)
-        a.top_logp[row * a.k + lane] =
-            poisoned ? st.s : none ? -__builtin_inff() : (b.v - st.m) * a.scale - __builtin_logf(st.s);
-    if (a.top_idx) a.top_idx[row * a.k + lane] = poisoned || none ? -1 : (int32_t)b.i;
-}
+};
 
 __device__ __forceinline__ int64_t row_width(const int32_t* valid, int64_t row, int64_t vocab) {
     if (!valid) return vocab;
@@ -174,14 +329,44 @@ __device__ __forceinline__ int64_t row_width(const int32_t* valid, int64_t row, 
     return v < 0 ? 0 : v < vocab ? v : vocab;
 }
 
-// The row's token and its logit, by one lane.
+// The row's token and its logit, read while the walk waits for its first batch.
+struct Given {
+    bool given, inside;
+    float x;
+};
 template <class T>
-__device__ __forceinline__ void put_stats(const LogprobsArgs& a, int64_t row, int64_t width, Stat st) {
+__device__ __forceinline__ Given given_of(const LogprobsArgs& a, int64_t row, int64_t width) {
     const int64_t t = a.tokens ? token_at(a.tokens, a.wide, row, (int64_t)1 << 62) : -1;
     const bool inside = t >= 0 && t < width;
-    const float xt = inside ? (float)static_cast<const T*>(a.logits)[row * a.ld + t] : 0.0f;
-    put_row(a, row, st, xt, t >= 0, inside);
+    return Given{t >= 0, inside, inside ? (float)static_cast<const T*>(a.logits)[row * a.ld + t] : 0.0f};
 }
+
+// What a row's outputs are once its sums are known.  A row with nothing in it
+// has s == 0 (or a scaled maximum of -inf); a NaN or +inf among its values
+// makes s NaN.
+__device__ __forceinline__ void put_row(const LogprobsArgs& a, int64_t row, Stat st, Given g) {
+    const bool empty = st.s == 0.0f || st.m * a.scale == -__builtin_inff();
+    const float ls = __builtin_logf(st.s);
+    const float lse = empty ? -__builtin_inff() : __builtin_fmaf(st.m, a.scale, ls);
+    if (a.lse) a.lse[row] = lse;
+    if (a.entropy) a.entropy[row] = empty ? 0.0f : ls - LN2 * (st.u / st.s);
+    if (a.logp) {
+        float lp = (g.x - st.m) * a.scale - ls;
+        if (!g.inside || empty) lp = -__builtin_inff();
+        if (st.s != st.s) lp = st.s;
+        a.logp[row] = g.given ? lp : 0.0f;
+    }
+}
+__device__ __forceinline__ void put_best(const LogprobsArgs& a, int64_t row, Stat st, Best b) {
+    const int lane = threadIdx.x & 63;
+    if (lane >= a.k) return;
+    const bool poisoned = st.s != st.s, none = b.value() * a.scale == -__builtin_inff();
+    if (a.top_logp)
+        a.top_logp[row * a.k + lane] =
+            poisoned ? st.s : none ? -__builtin_inff() : (b.value() - st.m) * a.scale - __builtin_logf(st.s);
+    if (a.top_idx) a.top_idx[row * a.k + lane] = poisoned || none ? -1 : (int32_t)b.column();
+}
+
 
 // A wave a row.
 template <int DT, bool TOP>
@@ -191,11 +376,13 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs_wave(LogprobsArgs a) {
     if (row >= a.n) return;
     const float c = a.scale * LOG2E;
     const int64_t width = row_width(a.valid, row, a.vocab);
+    const Given g = given_of<T>(a, row, width);
     Stat st = stat_empty();
     Best best = best_empty();
-    walk<T, TOP>(static_cast<const T*>(a.logits) + row * a.ld, 0, width, 0, 1, c, a.k, st, best);
+    __shared__ uint64_t s_room[TOP ? LP_WAVES : 1][128];
+    Walk<T, TOP>{st, best, c, a.k, nullptr, s_room[TOP ? threadIdx.x >> 6 : 0]}.run(static_cast<const T*>(a.logits) + row * a.ld, 0, width, 0, 1);
     st = stat_wave(st, c);
-    if ((threadIdx.x & 63) == 0) put_stats<T>(a, row, width, st);
+    if ((threadIdx.x & 63) == 0) put_row(a, row, st, g);
     if (TOP) put_best(a, row, st, best);
 }
 
@@ -205,25 +392,24 @@ struct Part {
 };
 
 // The waves' sums and lists joined in wave 0.
-template <bool TOP>
+template <bool TOP, int WAVES>
 __device__ __forceinline__ void join_waves(Stat& st, Best& best, float c) {
-    __shared__ Stat s_stat[LP_WAVES];
-    __shared__ Best s_best[LP_WAVES][64];
+    __shared__ Stat s_stat[WAVES];
+    __shared__ Best s_best[WAVES][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     st = stat_wave(st, c);
     if (lane == 0) s_stat[w] = st;
-    if (TOP) s_best[w][lane] = best;
+    if (TOP && w > 0) s_best[w][lane] = best;
     __syncthreads();
 #pragma unroll
-    for (int half = LP_WAVES / 2; half > 0; half >>= 1) {
+    for (int half = WAVES / 2; half > 0; half >>= 1) {
         if (TOP && w < half) {
             best = best_merge(best, s_best[w + half][lane]);
-            s_best[w][lane] = best;
+            if (half > 1 && w > 0) s_best[w][lane] = best;
         }
-        if (TOP) __syncthreads();
+        if (TOP && half > 1) __syncthreads();
     }
-    if (w == 0)
-        for (int v = 1; v < LP_WAVES; ++v) st = stat_join(st, s_stat[v], c);
+    if (w == 0) st = stat_wave(lane < WAVES ? s_stat[lane] : stat_empty(), c);
 }
 
 // A workgroup a segment of a row; with one segment a row it writes the row's
@@ -238,13 +424,21 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs(LogprobsArgs a, int seg
     const int64_t width = row_width(a.valid, row, a.vocab);
     const int64_t c0 = seg * span, c1 = c0 + span < width ? c0 + span : width;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    Given g{};
+    if (segments == 1 && threadIdx.x == 0) g = given_of<T>(a, row, width);
     Stat st = stat_empty();
     Best best = best_empty();
-    walk<T, TOP>(static_cast<const T*>(a.logits) + row * a.ld, c0, c1, w, LP_WAVES, c, a.k, st, best);
-    join_waves<TOP>(st, best, c);
+    __shared__ float s_kth[LP_WAVES];
+    if (TOP) {
+        if (threadIdx.x < LP_WAVES) s_kth[threadIdx.x] = -__builtin_inff();
+        __syncthreads();
+    }
+    __shared__ uint64_t s_room[TOP ? LP_WAVES : 1][128];
+    Walk<T, TOP>{st, best, c, a.k, s_kth, s_room[TOP ? w : 0]}.run(static_cast<const T*>(a.logits) + row * a.ld, c0, c1, w, LP_WAVES);
+    join_waves<TOP, LP_WAVES>(st, best, c);
     if (w != 0) return;
     if (segments == 1) {
-        if (lane == 0) put_stats<T>(a, row, width, st);
+        if (lane == 0) put_row(a, row, st, g);
         if (TOP) put_best(a, row, st, best);
     } else {
         if (lane == 0) parts[blockIdx.x] = Part{st.m, st.s, st.u, 0.0f};
@@ -252,27 +446,39 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs(LogprobsArgs a, int seg
     }
 }
 
+// One row's segments, a list a wave at a time.
+constexpr int JOIN_THREADS = 1024;
 template <int DT, bool TOP>
-__global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobsArgs a, int segments, const Part* parts,
-                                                              const Best* lists) {
+__global__ __launch_bounds__(JOIN_THREADS) void k_logprobs_join(LogprobsArgs a, int segments, const Part* parts,
+                                                                const Best* lists) {
     using T = typename Elem<DT>::T;
+    constexpr int WAVES = JOIN_THREADS / 64;
     const int64_t row = blockIdx.x;
     const float c = a.scale * LOG2E;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    Given g{};
+    if (threadIdx.x == 0) g = given_of<T>(a, row, row_width(a.valid, row, a.vocab));
     Stat st = stat_empty();
     Best best = best_empty();
-    for (int s = threadIdx.x; s < segments; s += LP_THREADS) {
-        const Part p = parts[row * segments + s];
-        st = stat_join(st, Stat{p.m, p.s, p.u}, c);
+    if (threadIdx.x < segments) {   // at most SEGMENTS_MAX
+        const Part p = parts[row * segments + threadIdx.x];
+        st = Stat{p.m, p.s, p.u};
     }
     if (TOP)
-        for (int s = w; s < segments; s += LP_WAVES) {
-            const Best b = lane < a.k ? lists[(row * segments + s) * a.k + lane] : best_empty();
-            best = best_merge(best, b);
+        for (int s = w; s < segments; s += 4 * WAVES) {
+            Best b[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int t = s + q * WAVES;
+                b[q] = t < segments && lane < a.k ? lists[(row * segments + t) * a.k + lane] : best_empty();
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (s + q * WAVES < segments) best = best_merge(best, b[q]);
         }
-    join_waves<TOP>(st, best, c);
+    join_waves<TOP, WAVES>(st, best, c);
     if (w != 0) return;
-    if (lane == 0) put_stats<T>(a, row, row_width(a.valid, row, a.vocab), st);
+    if (lane == 0) put_row(a, row, st, g);
     if (TOP) put_best(a, row, st, best);
 }
 
@@ -280,6 +486,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobsArgs a, in
 constexpr int64_t WAVE_ROW_MAX = 2048;
 constexpr int64_t SEGMENT_MIN = 2048;
 constexpr int SEGMENTS_MAX = 256;
+static_assert(SEGMENTS_MAX <= JOIN_THREADS, "the join reads a segment a thread");
 
 int segments_of(int64_t n, int64_t vocab) {
     if (vocab <= WAVE_ROW_MAX) return 0;
@@ -316,7 +523,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs_grad(LogprobsGradArgs a
     // nothing in it, or nothing but a mask's lowest value
     const bool empty = lse < -1e30f;
     auto slope = [&](float v, int64_t j) {
-        const float lp = bounded(v * a.scale - lse), p = exp2_fast(lp * LOG2E);
+        const float z = v * a.scale - lse, p = exp2_fast(z * LOG2E), lp = bounded(z);
         float s = -p * __builtin_fmaf(h, lp + H, g);
         if (j == t) s += g;
         return j < width && !empty ? s * a.scale : 0.0f;
@@ -368,8 +575,8 @@ hipError_t launch_logprobs(const LogprobsArgs& a, void* workspace, hipStream_t s
             hipLaunchKernelGGL((k_logprobs<DT, TOP>), dim3((unsigned)(a.n * segments)), block, 0, stream, a, segments, span,
                                parts, lists);
             if (segments > 1)
-                hipLaunchKernelGGL((k_logprobs_join<DT, TOP>), dim3((unsigned)a.n), block, 0, stream, a, segments, parts,
-                                   lists);
+                hipLaunchKernelGGL((k_logprobs_join<DT, TOP>), dim3((unsigned)a.n), dim3(JOIN_THREADS), 0, stream, a, segments,
+                                   parts, lists);
             return hipGetLastError();
         };
         return a.k > 0 ? go(std::true_type{}) : go(std::false_type{});

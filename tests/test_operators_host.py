@@ -76,7 +76,9 @@ REFUSED = [
     (ortho, dict(steps=65), INVALID), (ortho, dict(a=NAN), INVALID), (ortho, dict(eps=-1.0), INVALID),
     (ortho, dict(scale=INF), INVALID), (ortho, dict(ldo=7), INVALID), (ortho, dict(obatch=63), INVALID),
     (ortho, dict(ldx=-1), INVALID), (ortho, dict(x=None), INVALID), (ortho, dict(out=ODD), INVALID),
-    (ortho, dict(ws=None), INVALID), (ortho, dict(wb=100), INVALID), (ortho, dict(batch=65536), UNSUPPORTED),
+    # both sides up to 128 take no workspace
+    (ortho, dict(rows=200, obatch=1600, ws=None), INVALID), (ortho, dict(rows=200, obatch=1600, wb=100), INVALID),
+    (ortho, dict(batch=65536), UNSUPPORTED),
     (ortho, dict(rows=65537), UNSUPPORTED), (ortho, dict(rows=-1), INVALID),
 ]
 
