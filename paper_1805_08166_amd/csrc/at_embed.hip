@@ -6,12 +6,15 @@
 // Sums are fp32.  Tokens outside [0, vocab) give a row of zeros and take no
 // part in the gradient.
 //
-// The gradient sorts (token, position) pairs, stably, and cuts the merged
-// sequence of sorted entries and row ends into equal pieces, one to a worker:
-// a row that no token names costs a worker as much as an entry, so few rows
-// with many entries and many rows with none keep every worker equally busy.
-// Rows cut by a boundary are joined in order, so the sums depend on the sizes
-// alone and never on the order in which workgroups run.
+// The gradient sorts (token, position) pairs, stably, and cuts the sorted
+// entries into equal pieces, one to a worker, so that a token that occurs ten
+// thousand times costs as much an entry as one that occurs once.  Rows cut by a
+// boundary are joined in order: the sums depend on the sizes alone and never on
+// the order in which workgroups run.  Sorting keeps few workgroups busy and the
+// zeros of the rows that no token names are most of what a large table's
+// gradient writes, so further workgroups of the sort's own launches write them.
+#include <utility>
+
 #include "at_ops.h"
 
 namespace at {
@@ -66,14 +69,49 @@ __global__ __launch_bounds__(EMB_THREADS) void k_embed(EmbedArgs a, int txs) {
 // --------------------------------------------------------------------------
 constexpr int SORT_THREADS = 256;
 constexpr int SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_ITEMS = 8;                             // a lane, one wave slice each
+constexpr int SORT_ITEMS = 4;                             // a lane, one wave slice each
 constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;      // entries a workgroup
 constexpr int SORT_BITS_MAX = 9;
 constexpr int SORT_BINS = 1 << SORT_BITS_MAX;
 constexpr int ONE_THREADS = 1024;                         // the single-workgroup sort
 constexpr int ONE_WAVES = ONE_THREADS / 64;
-constexpr int ONE_ITEMS = 8;
+constexpr int ONE_ITEMS = 8;                              // a lane at most
 constexpr int ONE_MAX = ONE_THREADS * ONE_ITEMS;
+constexpr int SCAN_TILES = 64;                            // up to here a tile scans the histograms itself
+
+// Zeros for `rows` rows of row_bytes, stride bytes apart, written by the
+// workgroups from `first` on; rows 0: none.
+struct Fill {
+    char* base;
+    int64_t rows, row_bytes, stride;
+    int first;
+};
+__device__ __forceinline__ void fill_zeros(const Fill& f) {
+    const int64_t me = blockIdx.x - f.first, groups = gridDim.x - f.first;
+    typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+    const word4 zero = {0, 0, 0, 0};
+    // bytes lo .. hi - 1 from p on, by `threads` threads of which this is `at`
+    auto run = [&](char* p, int64_t lo, int64_t hi, int at, int threads) {
+        int64_t o = lo + at * 16;
+        for (; o + (int64_t)threads * 48 + 16 <= hi; o += (int64_t)threads * 64)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) __builtin_memcpy(p + o + (int64_t)threads * 16 * u, &zero, 16);
+        for (; o < hi; o += (int64_t)threads * 16)
+            if (o + 16 <= hi)
+                __builtin_memcpy(p + o, &zero, 16);
+            else
+                for (int64_t e = o; e < hi; e += 2) *reinterpret_cast<uint16_t*>(p + e) = 0;
+    };
+    if (f.row_bytes == f.stride) {   // one run of bytes a workgroup
+        const int64_t all = f.rows * f.row_bytes, each = ((all + groups - 1) / groups + 4095) / 4096 * 4096;
+        const int64_t lo = me * each, hi = lo + each < all ? lo + each : all;
+        if (lo < hi) run(f.base, lo, hi, threadIdx.x, blockDim.x);
+    } else {   // a wave a row
+        const int64_t waves = blockDim.x / 64;
+        for (int64_t r = me * waves + threadIdx.x / 64; r < f.rows; r += groups * waves)
+            run(f.base + r * f.stride, 0, f.row_bytes, threadIdx.x & 63, 64);
+    }
+}
 
 struct SortIn {
     const void* tokens;   // first pass
@@ -139,7 +177,9 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* scratch) {
 }
 
 // hist[d * blocks + b]: entries of tile b with digit d.
-__global__ __launch_bounds__(SORT_THREADS) void k_sort_hist(SortIn in, int64_t n, int shift, int bits, uint32_t* hist) {
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_hist(SortIn in, int64_t n, int shift, int bits, uint32_t* hist,
+                                                            int blocks, Fill fill) {
+    if ((int)blockIdx.x >= blocks) return fill_zeros(fill);
     __shared__ uint32_t cnt[SORT_BINS];
     const int bins = 1 << bits;
     for (int d = threadIdx.x; d < bins; d += SORT_THREADS) cnt[d] = 0;
@@ -151,7 +191,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_hist(SortIn in, int64_t n
         if (i < n) atomicAdd(&cnt[(sort_key(in, i) >> shift) & (bins - 1)], 1u);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < bins; d += SORT_THREADS) hist[(int64_t)d * gridDim.x + blockIdx.x] = cnt[d];
+    for (int d = threadIdx.x; d < bins; d += SORT_THREADS) hist[(int64_t)d * blocks + blockIdx.x] = cnt[d];
 }
 
 // One workgroup a digit: exclusive scan over the tiles in place, total[d].
@@ -173,9 +213,11 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scan(uint32_t* hist, int 
     if (threadIdx.x == 0) total[blockIdx.x] = base;
 }
 
+// total: the digits' totals, hist scanned; or null, and hist as counted.
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(SortIn in, int64_t n, int shift, int bits,
                                                                const uint32_t* hist, const uint32_t* total,
-                                                               uint32_t* keys, uint32_t* pos) {
+                                                               uint32_t* keys, uint32_t* pos, int blocks, Fill fill) {
+    if ((int)blockIdx.x >= blocks) return fill_zeros(fill);
     __shared__ uint32_t cnt[SORT_WAVES][SORT_BINS];
     __shared__ uint32_t base[SORT_BINS];
     __shared__ uint32_t scratch[SORT_WAVES];
@@ -201,10 +243,24 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(SortIn in, int64_
     uint32_t run = 0;
     for (int d0 = 0; d0 < bins; d0 += SORT_THREADS) {
         const int d = d0 + threadIdx.x;
-        const uint32_t t = d < bins ? total[d] : 0;
+        uint32_t t = 0, before = 0;   // of this digit: entries, and those of earlier tiles
+        if (d < bins) {
+            const uint32_t* h = hist + (int64_t)d * blocks;
+            if (total) {
+                t = total[d];
+                before = h[blockIdx.x];
+            } else {
+#pragma unroll 8
+                for (int b = 0; b < blocks; ++b) {
+                    const uint32_t x = h[b];
+                    t += x;
+                    before += b < (int)blockIdx.x ? x : 0;
+                }
+            }
+        }
         const uint32_t e = block_scan<SORT_THREADS>(t, scratch);
         if (d < bins) {
-            uint32_t s = run + e + hist[(int64_t)d * gridDim.x + blockIdx.x];
+            uint32_t s = run + e + before;
             for (int w = 0; w < SORT_WAVES; ++w) {
                 const uint32_t c = cnt[w][d];
                 cnt[w][d] = s;
@@ -225,19 +281,21 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(SortIn in, int64_
         }
 }
 
-// The whole sort of at most ONE_MAX entries in one workgroup.
+// The whole sort of at most ONE_THREADS * ITEMS entries in one workgroup.
+template <int ITEMS>
 __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int bits_all, uint32_t* keys,
-                                                          uint32_t* pos) {
-    __shared__ uint32_t s_key[ONE_MAX];
-    __shared__ uint16_t s_pos[ONE_MAX];
+                                                          uint32_t* pos, Fill fill) {
+    if (blockIdx.x > 0) return fill_zeros(fill);
+    __shared__ uint32_t s_key[ONE_THREADS * ITEMS];
+    __shared__ uint16_t s_pos[ONE_THREADS * ITEMS];
     __shared__ uint32_t cnt[ONE_WAVES][SORT_BINS];
     __shared__ uint32_t scratch[ONE_WAVES];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int i0 = wave * 64 * ONE_ITEMS + lane;
-    uint32_t key[ONE_ITEMS], p[ONE_ITEMS], digit[ONE_ITEMS], rank[ONE_ITEMS];
-    bool ok[ONE_ITEMS];
+    const int i0 = wave * 64 * ITEMS + lane;
+    uint32_t key[ITEMS], p[ITEMS], digit[ITEMS], rank[ITEMS];
+    bool ok[ITEMS];
 #pragma unroll
-    for (int s = 0; s < ONE_ITEMS; ++s) {
+    for (int s = 0; s < ITEMS; ++s) {
         const int i = i0 + s * 64;
         ok[s] = i < n;
         key[s] = ok[s] ? sort_key(in, i) : 0;
@@ -249,8 +307,8 @@ __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int 
         for (int d = threadIdx.x; d < bins * ONE_WAVES; d += ONE_THREADS) cnt[d >> bits][d & (bins - 1)] = 0;
         __syncthreads();
 #pragma unroll
-        for (int s = 0; s < ONE_ITEMS; ++s) digit[s] = (key[s] >> shift) & (bins - 1);
-        wave_ranks<ONE_ITEMS>(digit, ok, bits, cnt[wave], rank);
+        for (int s = 0; s < ITEMS; ++s) digit[s] = (key[s] >> shift) & (bins - 1);
+        wave_ranks<ITEMS>(digit, ok, bits, cnt[wave], rank);
         __syncthreads();
         const int d = threadIdx.x;   // bins <= ONE_THREADS
         uint32_t t = 0;
@@ -265,7 +323,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int 
             }
         __syncthreads();
 #pragma unroll
-        for (int s = 0; s < ONE_ITEMS; ++s)
+        for (int s = 0; s < ITEMS; ++s)
             if (ok[s]) {
                 const uint32_t at = cnt[wave][digit[s]] + rank[s];
                 s_key[at] = key[s];
@@ -273,7 +331,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int 
             }
         __syncthreads();
 #pragma unroll
-        for (int s = 0; s < ONE_ITEMS; ++s)
+        for (int s = 0; s < ITEMS; ++s)
             if (ok[s]) {
                 key[s] = s_key[i0 + s * 64];
                 p[s] = s_pos[i0 + s * 64];
@@ -281,7 +339,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int 
         shift += bits;
     }
 #pragma unroll
-    for (int s = 0; s < ONE_ITEMS; ++s)
+    for (int s = 0; s < ITEMS; ++s)
         if (ok[s]) {
             keys[i0 + s * 64] = key[s];
             pos[i0 + s * 64] = p[s];
@@ -291,219 +349,205 @@ __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int 
 // --------------------------------------------------------------------------
 // Sums of rows by sorted token
 // --------------------------------------------------------------------------
-// The merged sequence has vocab + n units: entry j stands before the end of
-// row keys[j], so it is unit j + keys[j], and the entries before unit d are
-// those with j + keys[j] < d.
-constexpr int SUM_UNITS_MAX = 1024;   // units a workgroup
+constexpr int SUM_EACH = 16;                           // entries a worker, at least
+constexpr int SUM_ENTRIES_MAX = 1024;                  // a workgroup
+constexpr int SUM_LANES_MIN = 8;                       // a worker; at most a wave
+constexpr int SUM_WORKERS_MAX = EMB_THREADS / SUM_LANES_MIN;
 
 struct SumArgs {
     EmbedGradArgs g;
     const uint32_t *keys, *pos;
     float *head, *tail;   // [workgroups][dpad]
-    int32_t* meta;        // [workgroups][2]: some row ends here; the row continued from before that ends here, or -1
+    int32_t* meta;        // [workgroups][2]: whether the row of its tail begins here; the row that goes on from the
+                          // workgroup before and ends here, or -1
     int64_t dpad;
-    int units;            // a worker
-    int txs;
-    int groups;           // workgroups of one column tile
+    int each;             // entries a worker
+    int txs;              // 1 << txs lanes a worker
+    int ytiles;           // column tiles, neighbours among the workgroups: a row's bytes are read together
 };
 
-// First j in [0, n] with j + keys[j] >= d, by a whole wave.
-__device__ __forceinline__ int64_t split_at(const uint32_t* keys, int64_t n, int64_t d) {
-    const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = n < d ? n : d;
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64, p = lo + lane * step;
-        const bool before = p < hi && p + (int64_t)keys[p] < d;
-        const int cnt = __popcll(__ballot(before));
-        if (cnt == 0) break;
-        const int64_t q = lo + cnt * step;
-        lo = lo + (cnt - 1) * step + 1;
-        if (q < hi) hi = q;
-    }
-    return lo;
+// Elements a lane: 16 bytes of dout, or one where a row has fewer.
+template <int DT, bool NARROW>
+constexpr int sum_vec() {
+    return NARROW ? 1 : (int)(16 / sizeof(typename Elem<DT>::T));
 }
 
-template <class TO, int VEC>
-__device__ __forceinline__ void put_row(const SumArgs& a, int64_t row, int64_t c, const float (&acc)[VEC]) {
-    TO* p = static_cast<TO*>(a.g.dweight) + row * a.g.ldg + c;
-    const bool add = a.g.accumulate;
-    if (c + VEC <= a.g.dim) {
-        Pack<TO, VEC> o;
-        if (add) {
-            o = load_pack<TO, VEC>(p);
+// Columns of a lane: VEC from c on.  Where fewer are left it reads the row's last
+// VEC instead, so that every load is whole, and its first `skip` are its
+// neighbour's.
+template <int VEC>
+struct Columns {
+    int64_t c, at;
+    int skip;
+    bool live;
+    __device__ __forceinline__ Columns(int64_t first, int64_t dim) : c(first) {
+        at = c + VEC <= dim ? c : dim - VEC;
+        live = c < dim;
+        skip = (int)(c - at);
+    }
+};
+
+// scale * sum, with what the row held before, to dweight's row.
+template <class TO, int VEC, bool ADD>
+__device__ __forceinline__ void put_row(const SumArgs& a, int64_t row, const Columns<VEC>& k, const float (&acc)[VEC],
+                                        const Pack<TO, VEC>& before) {
+    TO* p = static_cast<TO*>(a.g.dweight) + row * a.g.ldg + k.at;
+    Pack<TO, VEC> o;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) o.v[e] = rounded<TO>((float)o.v[e] + acc[e] * a.g.scale);
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) o.v[e] = rounded<TO>(acc[e] * a.g.scale);
-        }
+    for (int e = 0; e < VEC; ++e)
+        o.v[e] = rounded<TO>(ADD ? (float)before.v[e] + acc[e] * a.g.scale : acc[e] * a.g.scale);
+    if (k.skip == 0) {
         store_pack<TO, VEC>(p, o);
     } else {
-        for (int e = 0; e < VEC && c + e < a.g.dim; ++e)
-            p[e] = rounded<TO>(add ? (float)p[e] + acc[e] * a.g.scale : acc[e] * a.g.scale);
+#pragma unroll
+        for (int e = 1; e < VEC; ++e)
+            if (e >= k.skip) p[e] = o.v[e];
     }
 }
 
-template <class TI, int VEC>
-__device__ __forceinline__ Pack<TI, VEC> get_row(const SumArgs& a, uint32_t row, int64_t c) {
-    const TI* p = static_cast<const TI*>(a.g.dout) + (int64_t)row * a.g.ldd + c;
-    if (c + VEC <= a.g.dim) return load_pack<TI, VEC>(p);
-    Pack<TI, VEC> r;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) r.v[e] = c + e < a.g.dim ? p[e] : (TI)0.0f;
-    return r;
-}
-
-template <int DT, int GT>
+template <int DT, int GT, bool ADD, bool NARROW>
 __global__ __launch_bounds__(EMB_THREADS) void k_embed_sum(SumArgs a) {
     using TI = typename Elem<DT>::T;
     using TO = typename Elem<GT>::T;
-    constexpr int VEC = 16 / sizeof(TI);
-    constexpr int U = 8;   // rows in flight
-    __shared__ uint32_t s_key[SUM_UNITS_MAX + 2], s_pos[SUM_UNITS_MAX];
-    __shared__ float s_head[EMB_THREADS * VEC], s_tail[EMB_THREADS * VEC];
-    __shared__ int s_has[EMB_THREADS / 8 + 1];
-    __shared__ int64_t s_j[2];
-    const int64_t n = a.g.n, V = a.g.vocab, total = V + n;
+    constexpr int VEC = sum_vec<DT, NARROW>();
+    __shared__ uint32_t s_key[SUM_ENTRIES_MAX + 2], s_pos[SUM_ENTRIES_MAX];
+    __shared__ float s_tail[EMB_THREADS * VEC];
+    __shared__ uint8_t s_begins[SUM_WORKERS_MAX];
+    const int64_t n = a.g.n, V = a.g.vocab;
     const int tx = 1 << a.txs, ty = EMB_THREADS >> a.txs;
     const int w = threadIdx.x >> a.txs, lane = threadIdx.x & (tx - 1);
-    const int64_t c = ((int64_t)blockIdx.y * tx + lane) * VEC;
-    const bool live = c < a.g.dim;
-    const int64_t d0 = (int64_t)blockIdx.x * a.units * ty;
-    const int64_t d1 = d0 + a.units * ty < total ? d0 + a.units * ty : total;
-    if (threadIdx.x < 128) {
-        const int64_t j = split_at(a.keys, n, threadIdx.x < 64 ? d0 : d1);
-        if ((threadIdx.x & 63) == 0) s_j[threadIdx.x >> 6] = j;
-    }
-    __syncthreads();
-    const int64_t J0 = s_j[0], J1 = s_j[1];
-    const int m = (int)(J1 - J0);   // at most d1 - d0
+    const int tile = blockIdx.x % a.ytiles;
+    const int64_t group = blockIdx.x / a.ytiles, j0 = group * a.each * ty;
+    const Columns<VEC> col(((int64_t)tile * tx + lane) * VEC, a.g.dim);
+    const int m = (int)(n - j0 < a.each * ty ? n - j0 : a.each * ty);
+    // local entry q is entry j0 + q, with its key in s_key[q + 1]
     for (int k = threadIdx.x; k < m + 2; k += EMB_THREADS) {
-        const int64_t j = J0 - 1 + k;
+        const int64_t j = j0 - 1 + k;
         s_key[k] = j >= 0 && j < n ? a.keys[j] : 0xffffffffu;
-        if (k < m) s_pos[k] = a.pos[J0 + k];
+        if (k < m) s_pos[k] = a.pos[j0 + k];
     }
     __syncthreads();
-    // this worker's units; local entry index q stands for entry J0 + q, its
-    // key is s_key[q + 1]
-    auto split = [&](int64_t d) {
-        int lo = 0, hi = m;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (J0 + mid + (int64_t)s_key[mid + 1] < d) lo = mid + 1; else hi = mid;
-        }
-        return lo;
-    };
-    const int64_t dw0 = d0 + (int64_t)w * a.units < d1 ? d0 + (int64_t)w * a.units : d1;
-    const int64_t dw1 = dw0 + a.units < d1 ? dw0 + a.units : d1;
-    const int q0 = split(dw0), q1 = split(dw1);
-    const int64_t i0 = dw0 - (J0 + q0), i1 = dw1 - (J0 + q1);
-    float acc[VEC];
+    const int q0 = w * a.each < m ? w * a.each : m, q1 = q0 + a.each < m ? q0 + a.each : m;
+    // the row of the first entry began before it
+    const bool goes_on = q1 > q0 && s_key[q0] == s_key[q0 + 1];
+    float acc[VEC], head[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
-    bool has = false, some = false;
-    int64_t i = i0;
-    auto end_row = [&]() {
-        if (!has) {
+    for (int e = 0; e < VEC; ++e) acc[e] = head[e] = 0.0f;
+    bool ended = false;
+    // rows asked for at once, together with those that they are added to
+    constexpr int AHEAD = ADD ? 8 : SUM_EACH;
+    const TI* dout = static_cast<const TI*>(a.g.dout);
+    const TO* dw = static_cast<const TO*>(a.g.dweight);
+    for (int q = q0; q < q1; q += AHEAD) {
+        typedef uint8_t raw __attribute__((ext_vector_type(VEC * sizeof(TI))));
+        raw r[AHEAD];
+        Pack<TO, VEC> before[ADD ? AHEAD : 1];
+        uint32_t key[AHEAD + 1];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s_head[threadIdx.x * VEC + e] = acc[e];
-            has = true;
-        } else if (live && (some || !a.g.accumulate)) {
-            put_row<TO, VEC>(a, i, c, acc);
-        }
+        for (int u = 0; u <= AHEAD; ++u) key[u] = s_key[(q + u < q1 ? q + u : q1) + 1];
+        // past the end the last entry again, which costs nothing and keeps the
+        // loads free of branches
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
-        some = false;
-        ++i;
-    };
-    for (int q = q0; q < q1; q += U) {
-        Pack<TI, VEC> r[U];
+        for (int u = 0; u < AHEAD; ++u)
+            __builtin_memcpy(&r[u], dout + (int64_t)s_pos[q + u < q1 ? q + u : q1 - 1] * a.g.ldd + col.at, sizeof(raw));
+        if (ADD)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (q + u < q1 && live && s_key[q + u + 1] < V) r[u] = get_row<TI, VEC>(a, s_pos[q + u], c);
+            for (int u = 0; u < AHEAD; ++u)
+                before[u] = load_pack<TO, VEC>(dw + (int64_t)(key[u] < V ? key[u] : 0) * a.g.ldg + col.at);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (q + u >= q1) break;
-            const int64_t t = s_key[q + u + 1];
-            if (t >= V) break;
-            while (i < t) end_row();
-            if (live) {
+        for (int u = 0; u < AHEAD; ++u) {
+            if (q + u < q1 && key[u] < V) {   // dropped tokens come last
+                Pack<TI, VEC> w;
+                __builtin_memcpy(&w, &r[u], sizeof(raw));
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] += (float)r[u].v[e];
+                for (int e = 0; e < VEC; ++e) acc[e] += (float)w.v[e];
+                if (key[u + 1] != key[u]) {   // the row ends here
+                    if (!ended && goes_on) {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) head[e] = acc[e];
+                    } else if (col.live) {
+                        put_row<TO, VEC, ADD>(a, key[u], col, acc, before[ADD ? u : 0]);
+                    }
+                    ended = true;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
+                }
             }
-            some = true;
         }
     }
-    while (i < i1) end_row();
+    // what is left belongs to a row that goes on
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s_tail[threadIdx.x * VEC + e] = acc[e];
-    if (lane == 0) s_has[w] = has;
+    if (lane == 0) s_begins[w] = ended || !goes_on;
     __syncthreads();
-    // Worker w's first row may have begun in earlier workers: their tails,
-    // ascending, then w's head.  Worker 0 also sums what the workgroup leaves
-    // for later ones, as if a worker stood behind the last.
+    // The tails of the workers before `upto` from the one on in which the row
+    // begins, ascending; false when it begins before the workgroup.
     auto joined = [&](int upto, float (&sum)[VEC]) {
         int b = upto;
-        while (b > 0 && !s_has[b - 1]) --b;
-        const bool from_start = b == 0;
-        if (!from_start) --b;
+        while (b > 0 && !s_begins[b - 1]) --b;
+        const bool here = b > 0;
+        if (here) --b;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
         for (; b < upto; ++b)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) sum[e] += s_tail[((b << a.txs) + lane) * VEC + e];
-        return from_start;
+        return here;
     };
-    const int64_t I0 = d0 - J0;
-    const bool continued = J0 > 0 && s_key[0] == (uint64_t)I0;
-    if (has) {
+    // meta: one worker at most ends a row that began before the workgroup
+    if (ended && goes_on) {
         float sum[VEC];
-        const bool from_start = joined(w, sum);
+        const bool here = joined(w, sum);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] += s_head[threadIdx.x * VEC + e];
-        if (from_start && continued) {
-            if (live) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) a.head[blockIdx.x * a.dpad + c + e] = sum[e];
-            }
-            if (lane == 0 && blockIdx.y == 0) a.meta[2 * blockIdx.x + 1] = (int32_t)i0;
+        for (int e = 0; e < VEC; ++e) sum[e] += head[e];
+        const uint32_t row = s_key[q0 + 1];
+        if (here) {
+            Pack<TO, VEC> before{};
+            if (ADD) before = load_pack<TO, VEC>(dw + (int64_t)row * a.g.ldg + col.at);
+            if (col.live) put_row<TO, VEC, ADD>(a, row, col, sum, before);
         } else {
-            // the row has entries when one before or after its worker's start is its own
-            const bool any = s_key[q0] == (uint64_t)i0 || s_key[q0 + 1] == (uint64_t)i0;
-            if (live && (any || !a.g.accumulate)) put_row<TO, VEC>(a, i0, c, sum);
-            if (from_start && lane == 0 && blockIdx.y == 0) a.meta[2 * blockIdx.x + 1] = -1;
+            if (col.live) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) a.head[group * a.dpad + col.c + e] = sum[e];
+            }
+            if (lane == 0 && tile == 0) a.meta[2 * group + 1] = (int32_t)row;
         }
     }
     if (w == 0) {
+        // for the workgroups behind
+        const bool on = s_key[m] == s_key[m + 1] && s_key[m] < V;
+        const int last = (m - 1) / a.each;   // worker of the last entry
         float sum[VEC];
-        const bool none = joined(ty, sum);
-        if (live) {
+        const bool here = joined(last + 1, sum);
+        if (on && col.live) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) a.tail[blockIdx.x * a.dpad + c + e] = sum[e];
+            for (int e = 0; e < VEC; ++e) a.tail[group * a.dpad + col.c + e] = sum[e];
         }
-        if (lane == 0 && blockIdx.y == 0) {
-            a.meta[2 * blockIdx.x] = !none;
-            if (none) a.meta[2 * blockIdx.x + 1] = -1;
+        if (lane == 0 && tile == 0) {
+            a.meta[2 * group] = here;
+            // no row that began before ends here: the first goes on to the end, or began here
+            const uint32_t first = s_key[1];
+            if (s_key[0] != first || first >= V || (s_key[m] == first && s_key[m + 1] == first)) a.meta[2 * group + 1] = -1;
         }
     }
 }
 
 // Rows that run over more than one workgroup: the tails of those before the
 // one that ends it, ascending, then its head.
-template <int DT, int GT>
+template <int DT, int GT, bool ADD, bool NARROW>
 __global__ __launch_bounds__(EMB_THREADS) void k_embed_join(SumArgs a) {
     using TO = typename Elem<GT>::T;
-    constexpr int VEC = 16 / sizeof(typename Elem<DT>::T);
+    constexpr int VEC = sum_vec<DT, NARROW>();
     __shared__ float s_part[EMB_THREADS * VEC];
     __shared__ int s_first;
-    const int last = blockIdx.x;
+    const int tile = blockIdx.x % a.ytiles, last = blockIdx.x / a.ytiles;
     const int32_t row = a.meta[2 * last + 1];
     if (row < 0) return;
     const int tx = 1 << a.txs, ty = EMB_THREADS >> a.txs;
     const int w = threadIdx.x >> a.txs, lane = threadIdx.x & (tx - 1);
-    const int64_t c = ((int64_t)blockIdx.y * tx + lane) * VEC;
+    const Columns<VEC> col(((int64_t)tile * tx + lane) * VEC, a.g.dim);
     if (threadIdx.x < 64) {
-        // the latest earlier workgroup in which a row ends: the row began there
+        // the latest earlier workgroup whose tail's row begins in it: this one
         int hi = last;
         for (;;) {
             const int b = hi - 1 - (int)threadIdx.x;
@@ -526,22 +570,24 @@ __global__ __launch_bounds__(EMB_THREADS) void k_embed_join(SumArgs a) {
     float sum[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-    if (c < a.g.dim) {
+    if (col.live) {
 #pragma unroll 4
         for (int b = b0; b < b1; ++b)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum[e] += a.tail[b * a.dpad + c + e];
+            for (int e = 0; e < VEC; ++e) sum[e] += a.tail[b * a.dpad + col.c + e];
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s_part[threadIdx.x * VEC + e] = sum[e];
     __syncthreads();
-    if (w == 0 && c < a.g.dim) {
+    if (w == 0 && col.live) {
         for (int v = 1; v < ty; ++v)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) sum[e] += s_part[((v << a.txs) + lane) * VEC + e];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] += a.head[last * a.dpad + c + e];
-        put_row<TO, VEC>(a, row, c, sum);
+        for (int e = 0; e < VEC; ++e) sum[e] += a.head[last * a.dpad + col.c + e];
+        Pack<TO, VEC> before{};
+        if (ADD) before = load_pack<TO, VEC>(static_cast<const TO*>(a.g.dweight) + (int64_t)row * a.g.ldg + col.at);
+        put_row<TO, VEC, ADD>(a, row, col, sum, before);
     }
 }
 
@@ -555,22 +601,24 @@ int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // Workers and workspace of one gradient.
 struct GradPlan {
-    int txs, units, groups, ytiles, sort_blocks;
+    int txs, each, groups, ytiles, sort_blocks;
+    bool narrow;
     int64_t dpad;
     int64_t off_keys[2], off_pos[2], off_hist, off_total, off_head, off_tail, off_meta, bytes;
 };
-GradPlan plan_grad(int64_t n, int64_t vocab, int64_t dim, int vec) {
+GradPlan plan_grad(int64_t n, int64_t dim, int size) {
     GradPlan p{};
+    int vec = 16 / size;   // as sum_vec()
+    p.narrow = dim < vec;
+    if (p.narrow) vec = 1;
     const int64_t chunks = (dim + vec - 1) / vec;
-    p.txs = log2_at_least(chunks, 3, 8);
+    p.txs = log2_at_least(chunks, 3, 6);
     const int ty = EMB_THREADS >> p.txs;
     p.ytiles = (int)((chunks + (1 << p.txs) - 1) >> p.txs);
-    // Units a worker: enough workgroups to fill the chip eight times over,
-    // but few enough that what is joined between them stays small.
-    const int64_t total = vocab + n;
-    p.units = 8;
-    while (p.units < 128 && p.units * 2 * ty <= SUM_UNITS_MAX && total > (int64_t)p.units * ty * 2048) p.units *= 2;
-    p.groups = (int)((total + (int64_t)p.units * ty - 1) / ((int64_t)p.units * ty));
+    // rows asked for at once, and again while that leaves eight workgroups for every CU
+    p.each = SUM_EACH;
+    while (p.each * 2 * ty <= SUM_ENTRIES_MAX && n * p.ytiles > (int64_t)p.each * 2 * ty * 2048) p.each *= 2;
+    p.groups = (int)((n + p.each * ty - 1) / (p.each * ty));
     p.dpad = align_up(dim, 8);
     p.sort_blocks = n <= ONE_MAX ? 0 : (int)((n + SORT_TILE - 1) / SORT_TILE);
     int64_t at = 0;
@@ -614,40 +662,68 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t stream) {
     });
 }
 
-int64_t embed_grad_workspace(int64_t n, int64_t vocab, int64_t dim) {
+int64_t embed_grad_workspace(int64_t n, int64_t dim) {
     // the larger of what the two element sizes need
-    const int64_t a = plan_grad(n, vocab, dim, 4).bytes, b = plan_grad(n, vocab, dim, 8).bytes;
+    const int64_t a = plan_grad(n, dim, 4).bytes, b = plan_grad(n, dim, 2).bytes;
     return a > b ? a : b;
 }
 
 hipError_t launch_embed_grad(const EmbedGradArgs& g, void* workspace, hipStream_t stream) {
-    const GradPlan p = plan_grad(g.n, g.vocab, g.dim, 16 / elem_size(g.dtype));
+    const GradPlan p = plan_grad(g.n, g.dim, elem_size(g.dtype));
     char* ws = static_cast<char*>(workspace);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + p.off_keys[0]), reinterpret_cast<uint32_t*>(ws + p.off_keys[1])};
     uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(ws + p.off_pos[0]), reinterpret_cast<uint32_t*>(ws + p.off_pos[1])};
     int bits_all = 1;   // keys reach vocab
     while (((int64_t)1 << bits_all) <= g.vocab) ++bits_all;
+    auto passes_of = [](int bits) { return (bits + SORT_BITS_MAX - 1) / SORT_BITS_MAX; };
+    // the rows to clear, shared out over the launches of the sort
+    const int64_t size = elem_size(g.gtype);
+    int launches = p.sort_blocks ? 2 * passes_of(bits_all) : 1;
+    int64_t cleared = g.accumulate ? g.vocab : 0;
+    auto fill_of = [&](int first, int threads) {
+        Fill f{static_cast<char*>(g.dweight) + cleared * g.ldg * size, (g.vocab - cleared) / launches, g.dim * size,
+               g.ldg * size, first};
+        --launches;
+        cleared += f.rows;
+        const int64_t groups = (f.rows * f.row_bytes + threads * 64 - 1) / (threads * 64);
+        return std::pair<Fill, int>(f, (int)(groups < 2048 ? groups : 2048));
+    };
     SortIn in{g.tokens, g.wide, (uint32_t)g.vocab, nullptr, nullptr};
     int cur = 0;
-    if (g.n > 0 && !p.sort_blocks) {
-        hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(ONE_THREADS), 0, stream, in, (int)g.n, bits_all, keys[0], pos[0]);
-    } else if (g.n > 0) {
+    if (!p.sort_blocks) {
+        const auto f = fill_of(1, ONE_THREADS);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(1 + f.second), dim3(ONE_THREADS), 0, stream, in, (int)g.n, bits_all, keys[0],
+                               pos[0], f.first);
+        };
+        if (g.n <= ONE_THREADS)
+            go(k_sort_one<1>);
+        else if (g.n <= 4 * ONE_THREADS)
+            go(k_sort_one<4>);
+        else
+            go(k_sort_one<ONE_ITEMS>);
+    } else {
         uint32_t* hist = reinterpret_cast<uint32_t*>(ws + p.off_hist);
         uint32_t* total = reinterpret_cast<uint32_t*>(ws + p.off_total);
         for (int shift = 0; shift < bits_all;) {
-            const int passes = (bits_all - shift + SORT_BITS_MAX - 1) / SORT_BITS_MAX;
-            const int bits = (bits_all - shift + passes - 1) / passes;
-            hipLaunchKernelGGL(k_sort_hist, dim3(p.sort_blocks), dim3(SORT_THREADS), 0, stream, in, g.n, shift, bits,
-                               hist);
-            hipLaunchKernelGGL(k_sort_scan, dim3(1 << bits), dim3(SORT_THREADS), 0, stream, hist, p.sort_blocks, total);
-            hipLaunchKernelGGL(k_sort_scatter, dim3(p.sort_blocks), dim3(SORT_THREADS), 0, stream, in, g.n, shift, bits,
-                               hist, total, keys[cur], pos[cur]);
+            const int passes = passes_of(bits_all - shift), bits = (bits_all - shift + passes - 1) / passes;
+            auto f = fill_of(p.sort_blocks, SORT_THREADS);
+            hipLaunchKernelGGL(k_sort_hist, dim3(p.sort_blocks + f.second), dim3(SORT_THREADS), 0, stream, in, g.n, shift,
+                               bits, hist, p.sort_blocks, f.first);
+            const bool scan = p.sort_blocks > SCAN_TILES;
+            if (scan)
+                hipLaunchKernelGGL(k_sort_scan, dim3(1 << bits), dim3(SORT_THREADS), 0, stream, hist, p.sort_blocks,
+                                   total);
+            f = fill_of(p.sort_blocks, SORT_THREADS);
+            hipLaunchKernelGGL(k_sort_scatter, dim3(p.sort_blocks + f.second), dim3(SORT_THREADS), 0, stream, in, g.n,
+                               shift, bits, hist, scan ? total : nullptr, keys[cur], pos[cur], p.sort_blocks, f.first);
             in.keys = keys[cur];
             in.pos = pos[cur];
             shift += bits;
             if (shift < bits_all) cur ^= 1;
         }
     }
+    if (g.n == 0) return hipGetLastError();
     SumArgs a{g,
               keys[cur],
               pos[cur],
@@ -655,15 +731,24 @@ hipError_t launch_embed_grad(const EmbedGradArgs& g, void* workspace, hipStream_
               reinterpret_cast<float*>(ws + p.off_tail),
               reinterpret_cast<int32_t*>(ws + p.off_meta),
               p.dpad,
-              p.units,
+              p.each,
               p.txs,
-              p.groups};
+              p.ytiles};
     return with_type(g.dtype, [&](auto dt) {
         return with_type(g.gtype, [&](auto gt) {
             constexpr int DT = decltype(dt)::value, GT = decltype(gt)::value;
-            hipLaunchKernelGGL((k_embed_sum<DT, GT>), dim3(p.groups, p.ytiles), dim3(EMB_THREADS), 0, stream, a);
-            if (p.groups > 1)
-                hipLaunchKernelGGL((k_embed_join<DT, GT>), dim3(p.groups, p.ytiles), dim3(EMB_THREADS), 0, stream, a);
+            const dim3 grid((unsigned)(p.groups * p.ytiles)), block(EMB_THREADS);
+            auto go = [&](auto add, auto narrow) {
+                constexpr bool ADD = decltype(add)::value, NARROW = decltype(narrow)::value;
+                hipLaunchKernelGGL((k_embed_sum<DT, GT, ADD, NARROW>), grid, block, 0, stream, a);
+                if (p.groups > 1) hipLaunchKernelGGL((k_embed_join<DT, GT, ADD, NARROW>), grid, block, 0, stream, a);
+            };
+            const std::true_type yes;
+            const std::false_type no;
+            if (p.narrow)
+                g.accumulate ? go(yes, yes) : go(no, yes);
+            else
+                g.accumulate ? go(yes, no) : go(no, no);
             return hipGetLastError();
         });
     });

@@ -100,7 +100,7 @@ at_status at_embed_grad_workspace(int64_t n, int64_t vocab, int64_t dim, int64_t
     if (!bytes) return refuse(AT_E_INVALID, fn, "NULL output");
     const at_status st = table_args(fn, AT_F32, dim, AT_F32, dim, AT_I32, n, vocab, dim, 1.0f);
     if (st != AT_OK) return st;
-    *bytes = dim == 0 ? 0 : embed_grad_workspace(n, vocab, dim);
+    *bytes = dim == 0 ? 0 : embed_grad_workspace(n, dim);
     return AT_OK;
 }
 
@@ -114,7 +114,7 @@ at_status at_embed_grad(const void* dout, int dtype, int64_t ldd, const void* to
     if (!dweight || (n > 0 && (!dout || !tokens))) return refuse(AT_E_INVALID, fn, "NULL buffer");
     if (!aligned_t(dout, dtype) || !aligned_t(dweight, gtype) || !aligned(tokens, itype == AT_I64 ? 8 : 4))
         return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
-    st = workspace_args(fn, workspace, workspace_bytes, embed_grad_workspace(n, vocab, dim));
+    st = workspace_args(fn, workspace, workspace_bytes, embed_grad_workspace(n, dim));
     if (st != AT_OK) return st;
     const EmbedGradArgs a{dout, dtype, ldd, tokens, itype, n, scale, accumulate != 0, dweight, gtype, ldg, vocab, dim};
     return done(launch_embed_grad(a, workspace, (hipStream_t)stream), fn);

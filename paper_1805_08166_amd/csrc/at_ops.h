@@ -97,7 +97,7 @@ struct EmbedGradArgs {
     int gtype;
     int64_t ldg, vocab, dim;
 };
-int64_t embed_grad_workspace(int64_t n, int64_t vocab, int64_t dim);
+int64_t embed_grad_workspace(int64_t n, int64_t dim);
 hipError_t launch_embed_grad(const EmbedGradArgs& a, void* workspace, hipStream_t stream);
 
 struct LogprobsArgs {

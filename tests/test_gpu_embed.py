@@ -124,6 +124,12 @@ def reference(dout, t, vocab, scale, before):
     (12000, 64, 200, "f32", "bf16", 0, "none", True, False),
     (12000, 64, 200, "f32", "bf16", 0, "none", True, True),
     (300, 20, 9001, "f32", "f32", 1, "flat", True, False),
+    # histograms scanned by a launch of their own; rows over many workgroups; narrow rows
+    (100000, 3000, 40, "bf16", "f32", 0, "outside", True, False),
+    (150000, 2, 24, "f16", "f32", 1, "flat", False, True),
+    (70000, 70001, 3, "f32", "f32", 0, "frequent", True, False),
+    (5000, 40, 7, "bf16", "bf16", 0, "outside", False, True),
+    (900, 5, 17, "f16", "bf16", 0, "one", True, True),
 ])
 def test_gradient(P, n, vocab, dim, dt, gt, pad, kind, wide, add):
     import torch

@@ -100,6 +100,34 @@ def test_steps(P, batch, rows, cols, dt, ot, steps, kind):
         assert err < tol, (k, err)
 
 
+@pytest.mark.parametrize("batch,rows,cols,ot", [
+    (1, 4096, 4096, "bf16"),      # the widest tiles
+    (2, 2300, 2500, "f32"),
+    (3, 4090, 700, "bf16"),
+    (5, 1030, 1040, "bf16"),
+])
+def test_large(P, batch, rows, cols, ot):
+    """As above, the recurrence in 64 bits on the GPU (float64 products)."""
+    import torch
+    say(f"large {batch} x {rows} x {cols} -> {ot}")
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    g = torch.randn(batch, rows, cols, generator=gen, device=DEV)
+    g += torch.matmul(torch.randn(batch, rows, 16, generator=gen, device=DEV),
+                      torch.randn(batch, 16, cols, generator=gen, device=DEV))
+    out = torch.empty(batch, rows, cols, dtype=types()[ot], device=DEV)
+    P.at_orthogonalize(g, out)
+    for k in range(batch):
+        x = g[k].double() if rows <= cols else g[k].double().T.contiguous()
+        x = x / (torch.linalg.norm(x) + 1e-7)
+        a, b, c = COEF
+        for _ in range(5):
+            m = torch.mm(x, x.T.contiguous())
+            x = a * x + torch.mm(b * m + c * torch.mm(m, m), x)
+        want = x if rows <= cols else x.T
+        err = float((out[k].double() - want).norm() / want.norm())
+        assert err < (1e-4 if ot == "f32" else 3e-3 + 2.0 ** -8), (k, err)
+
+
 def test_strides_scale_and_neighbours(P):
     """Views with gaps between rows and matrices, a scale; nothing outside the
     output's rows is touched, and what lies between the input's rows is not read."""
