@@ -534,34 +534,39 @@ __device__ __forceinline__ void small_product(const half_t* P, const half_t* Q, 
     }
 }
 
-// v, this wave's fragment, transposed into LDS: element (i, j) to row j.
+// A fragment's words: rounded, and what that left.
+template <bool SPLIT>
+struct Words {
+    half4 h[4], l[4];
+    __device__ __forceinline__ explicit Words(const float16v& v) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            h[e >> 2][e & 3] = (half_t)v[e];
+            if (SPLIT) l[e >> 2][e & 3] = (half_t)(v[e] - (float)h[e >> 2][e & 3]);
+        }
+    }
+};
+// Transposed into LDS: element (i, j) to row j.
 template <int N, bool SPLIT>
-__device__ __forceinline__ void small_put_t(half_t* to, int fi, int fj, const float16v& v) {
+__device__ __forceinline__ void small_put_t(half_t* to, int fi, int fj, const Words<SPLIT>& w) {
     using S = Small<N>;
     const int lane = threadIdx.x & 63, j = fj + (lane & 31);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        const int i = fi + g * 8 + (lane >> 5) * 4;
-        half4 h, l;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            h[e] = (half_t)v[g * 4 + e];
-            l[e] = (half_t)(v[g * 4 + e] - (float)h[e]);
-        }
-        *reinterpret_cast<half4*>(to + S::at(j, i)) = h;
-        if (SPLIT) *reinterpret_cast<half4*>(to + S::MATRIX + S::at(j, i)) = l;
+        const int at = S::at(j, fi + g * 8 + (lane >> 5) * 4);
+        *reinterpret_cast<half4*>(to + at) = w.h[g];
+        if (SPLIT) *reinterpret_cast<half4*>(to + S::MATRIX + at) = w.l[g];
     }
 }
 template <int N, bool SPLIT>
-__device__ __forceinline__ void small_put(half_t* to, int fi, int fj, const float16v& v) {
+__device__ __forceinline__ void small_put(half_t* to, int fi, int fj, const Words<SPLIT>& w) {
     using S = Small<N>;
     const int lane = threadIdx.x & 63, j = fj + (lane & 31);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        const int i = fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4;
-        const half_t h = (half_t)v[e];
-        to[S::at(i, j)] = h;
-        if (SPLIT) to[S::MATRIX + S::at(i, j)] = (half_t)(v[e] - (float)h);
+        const int at = S::at(fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4, j);
+        to[at] = w.h[e >> 2][e & 3];
+        if (SPLIT) to[S::MATRIX + at] = w.l[e >> 2][e & 3];
     }
 }
 
@@ -591,25 +596,31 @@ __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, 
     for (int e = 0; e < 16; ++e) X[e] *= f;
     for (int step = 0; step < a.steps; ++step) {
         const float shift = step + 2 >= a.steps ? 0.5f * (a.b + a.c) : 0.0f;
-        small_put<N, SPLIT>(first, fi, fj, X);
+        const Words<SPLIT> x_words(X);
+        small_put<N, SPLIT>(first, fi, fj, x_words);
         __syncthreads();
         small_product<N, SPLIT>(first, first, fi, fj, A);
 #pragma unroll
         for (int e = 0; e < 16; ++e) A[e] *= A_SCALE / (xs * xs);
-        small_put_t<N, SPLIT>(second, fi, fj, A);   // A is its transpose
+        const Words<SPLIT> a_words(A);
+        small_put_t<N, SPLIT>(second, fi, fj, a_words);   // A is its transpose
         __syncthreads();
         small_product<N, SPLIT>(second, second, fi, fj, acc);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int i = fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4;
             // A as its operands hold it
-            float t = (float)(half_t)A[e];
-            if (SPLIT) t += (float)(half_t)(A[e] - t);
-            acc[e] = __builtin_fmaf(t, a.b, acc[e] * (a.c / A_SCALE)) - (i == j ? shift * A_SCALE : 0.0f);
+            float t = (float)a_words.h[e >> 2][e & 3];
+            if (SPLIT) t += (float)a_words.l[e >> 2][e & 3];
+            acc[e] = __builtin_fmaf(t, a.b, acc[e] * (a.c / A_SCALE));
         }
-        small_put_t<N, SPLIT>(first, fi, fj, acc);
+        if (fi == fj && shift != 0.0f) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (e / 4 * 8 + (lane >> 5) * 4 + e % 4 == (lane & 31)) acc[e] -= shift * A_SCALE;
+        }
+        small_put_t<N, SPLIT>(first, fi, fj, Words<SPLIT>(acc));
         __syncthreads();   // everyone has read A
-        small_put_t<N, SPLIT>(second, fi, fj, X);
+        small_put_t<N, SPLIT>(second, fi, fj, x_words);
         __syncthreads();
         small_product<N, SPLIT>(first, second, fi, fj, acc);
 #pragma unroll
