@@ -166,7 +166,8 @@ __device__ __forceinline__ Best best_merge(Best a, Best b) {
 
 // A batch with more values for the list than this has them sorted, 64 at a time,
 // and merged into it (about 200 instructions); otherwise they are inserted one
-// by one (about 20 each).
+// by one (about 20 each).  Anything from 8 to 32 measures the same; sorting always
+// costs 4096 x 50048, k 20, 218 us for 142, inserting always 444 for 212 at k 64.
 constexpr int INSERTIONS = 8;
 
 // The larger of three, one instruction.
@@ -482,14 +483,23 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_logprobs_join(LogprobsArgs a, 
     if (TOP) put_best(a, row, st, best);
 }
 
-// Rows up to this many values go to one wave each.
+// How a call is cut.  Short rows, and rows enough for three on every SIMD, take
+// a wave each: its one list is merged with none.  Others take a workgroup each, and
+// few long rows a workgroup a segment (at least SEGMENT_MIN values) and a launch to
+// join them.  us, a wave against a workgroup or segments, bf16, k 0 and 5:
+//   64 x 2048 9.1 and 13.6 (k 0); 4096 x 4096 8.1 and 10.6, 17 and 25;
+//   4096 x 50048 77 and 78, 89 and 103 (k 64 149 and 212);
+//   2048 x 50048 61 and 42, 68 and 62; 512 x 50048 34 and 14, 47 and 27;
+//   256 x 4096 7.9 and 13.0, 11 and 14 (k 64 26 and 17).
+// Segments of 1024, 2048 and 8192 values, 1 x 131072, k 20: 15.7, 14.1, 17.1.
 constexpr int64_t WAVE_ROW_MAX = 2048;
+constexpr int64_t WAVE_ROWS = 3200;
 constexpr int64_t SEGMENT_MIN = 2048;
 constexpr int SEGMENTS_MAX = 256;
 static_assert(SEGMENTS_MAX <= JOIN_THREADS, "the join reads a segment a thread");
 
 int segments_of(int64_t n, int64_t vocab) {
-    if (vocab <= WAVE_ROW_MAX) return 0;
+    if (vocab <= WAVE_ROW_MAX || n >= WAVE_ROWS) return 0;
     int64_t s = (1024 + n - 1) / n, most = (vocab + SEGMENT_MIN - 1) / SEGMENT_MIN;
     if (s > most) s = most;
     if (s > SEGMENTS_MAX) s = SEGMENTS_MAX;

@@ -108,6 +108,8 @@ CASES = [
     (3, 70000, "f16", 0, 0, "far", True, 1.0),
     (1500, 2100, "bf16", 3, 0, "plain", True, 1.0),
     (1300, 33, "f32", 4, 0, "masked", True, 2.0),
+    (3300, 2501, "bf16", 33, 1, "plain", True, 1.0),
+    (3201, 4097, "f32", 2, 0, "lowest", False, 1.0),
 ]
 
 
