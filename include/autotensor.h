@@ -515,8 +515,8 @@ at_status at_logprobs(const void* logits, int type, int64_t ld, int64_t n, int64
 /* Gradient of at_logprobs: with g = dlogp[i] and h = dentropy[i],
  *   dlogits[i, j] = round(scale * (g * (1[j = t] - p_j) - h * p_j * (log p_j + entropy[i])))
  * and 0 in ruled-out columns, columns from valid[i] on and rows with nothing in
- * them or with an lse below -1e30 (nothing but a mask's lowest value).  g counts as 0 for a row without a token or whose token is ruled
- * out.  lse, entropy: the forward call's (device [n] float; entropy may be
+ * them or with an lse below -1e30 (nothing but a mask's lowest value).  g counts
+ * as 0 for a row without a token or whose token is ruled out.  lse, entropy: the forward call's (device [n] float; entropy may be
  * NULL without dentropy); dlogp, dentropy: device [n] float, or NULL for zero.
  * dlogits: device [n][vocab] of the logits' type, rows ldd apart. */
 at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, int64_t vocab, const int32_t* valid,
@@ -531,16 +531,17 @@ at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, 
  * matrices xbatch and rows ldx elements apart; out: device, bf16 or fp32
  * (otype), obatch and ldo apart; out may be x, of the same type.  The products
  * run on the matrix cores with fp16 operands and fp32 sums while X keeps 22
- * bits.  fp32 outputs, and matrices whose shorter side is at most 256, have
+ * bits.  fp32 outputs, and matrices whose shorter side is at most 64, have
  * fp32's accuracy before the result is rounded; other bf16 outputs are within
- * about 2e-3 of their norm (bf16's own rounding is 1.7e-3 of it).
+ * about 2.4e-3 of their norm (bf16's own rounding is 1.7e-3 of it).
  * A matrix of zeros gives zeros.  1 <= steps <= 64; batch <= 65535, rows and cols
  * <= 65536, AT_E_UNSUPPORTED beyond; coefficients that let singular values
  * grow past 8 overflow.  Workspace: at_orthogonalize_workspace bytes. */
 at_status at_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int otype, int64_t* bytes);
 at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx, int64_t batch, int64_t rows,
                            int64_t cols, int steps, float a, float b, float c, float eps, float scale, void* out,
-                           int otype, int64_t obatch, int64_t ldo, void* workspace, int64_t workspace_bytes, at_stream_t stream);
+                           int otype, int64_t obatch, int64_t ldo, void* workspace, int64_t workspace_bytes,
+                           at_stream_t stream);
 
 /* Thread-local description of the last non-OK status ("" if none). */
 const char* at_last_error(void);

@@ -99,7 +99,8 @@ __global__ __launch_bounds__(NORM_THREADS) void k_norm(OrthoArgs a, double* part
 }
 
 // xs * G / (|G| + eps) and its transpose, zero padded: one 64 x 64 tile of G a
-// workgroup, sixteen values of a row a thread.
+// workgroup, sixteen values of a row a thread.  2 x 1024 x 4096 bf16 16 us (the
+// norm before it 6), 4.2 TB/s.
 template <int DT, bool SPLIT>
 __global__ __launch_bounds__(256) void k_layout(OrthoArgs a, OrthoBufs b, int sp, int lp, int tall, float xs) {
     using T = typename Elem<DT>::T;
@@ -292,6 +293,9 @@ __device__ __forceinline__ void tile_of(const GemmArgs& a, int& z, int& bi, int&
 
 // SPLIT: the product of (P + p)(Q + q)^T without p q^T, three passes over the
 // depth into the same sums: fp32 results to about 2^-22.
+// Bound by what a CU takes into LDS, 50 to 75 KB/us here.  us a step of
+// 2 x 1024 x 4096: A 30 (half its products, 0.30 PF/s), B 11, X 33 (0.52 PF/s);
+// X of 4096 x 4096, in 256 x 256 tiles, 131 (1.05 PF/s).
 template <class S, int MODE, bool SPLIT>
 __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
     constexpr int ROWS = S::ROWS, COLS = S::COLS, FR = S::FR, FC = S::FC, STAGES = S::STAGES;
@@ -500,6 +504,9 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
 // --------------------------------------------------------------------------
 // Small matrices: every step in one workgroup
 // --------------------------------------------------------------------------
+// Bound by latency: three dependent products a step with barriers between.
+// 8 x 128 x 128, 5 steps, 21 us with sixteen waves; with eight of 64 x 32 25 and
+// four of 64 x 64 34.
 // Both sides padded to N; one wave a fragment of 32 x 32.  X stays in
 // registers, in fp32; LDS holds two operands at a time: X then B, and A then X
 // transposed.  Rows of N, 16-byte chunk c of row r in slot c ^ r (of 16) or c ^
@@ -645,8 +652,11 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // fp16 operands are off by 2^-12 each; over many singular values that
 // averages out (s = 128: 1.2 times the error that bf16's rounding has alone; 64:
 // 1.4; 16: up to 2.2), so few rows take split products, at three times the
-// matrix instructions (which small matrices do not wait for).
+// matrix instructions, which small matrices do not wait for.  Larger ones do: us,
+// split and not, 8 x 128 x 128 61 and 22, 2 x 1024 x 4096 938 and 355.
 constexpr int64_t SPLIT_MAX = 64;
+// Every step in one workgroup, against tiles: us, 1 x 128 x 128 22 and 68,
+// 1 x 64 x 64 17 and 64, 512 x 128 x 128 56 and 270.
 constexpr int64_t SMALL_MAX = 128;
 
 struct OrthoPlan {
@@ -693,9 +703,11 @@ OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, int otype) {
     return p;
 }
 
-// Tile shapes, by how many workgroups they make (us for 2 x 1024 x 4096: A 25,
-// B 42; X 39 and 31; for 4096 x 4096: X with 64 by 64 not measured, 128 by 128
-// 149 to 155, 256 by 256 131).
+// Tile shapes: the largest that divides both sides and makes a workgroup for
+// every CU.  A larger tile moves fewer bytes into LDS a product, which is what
+// these kernels wait for.  us a call, the rule against 64 x 64 always and, third,
+// 128 x 128 at most: 2 x 1024 x 4096 355, 414; 2048 x 8192 946, 1110, 977;
+// 4096 x 4096 1944, 2348, 2044.
 using Tile64 = Shape<2, 2, 1, 1, 1, 3>;
 using Tile128 = Shape<2, 4, 1, 2, 1, 2>;
 using Tile256 = Shape<2, 4, 1, 4, 2, 2>;
