@@ -69,21 +69,22 @@ __global__ __launch_bounds__(EMB_THREADS) void k_embed(EmbedArgs a, int txs) {
 // --------------------------------------------------------------------------
 // Stable radix sort of (token, position) pairs
 // --------------------------------------------------------------------------
-constexpr int SORT_THREADS = 256;
+constexpr int SORT_THREADS = 1024;
 constexpr int SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_ITEMS = 4;                             // a lane, one wave slice each
-constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;      // entries a workgroup
-constexpr int SORT_BITS_MAX = 9;
-constexpr int SORT_BINS = 1 << SORT_BITS_MAX;
-// The single-workgroup sort, one launch for two a pass: a gradient of 2000
-// tokens 24 us for 36, of 8000 35 for 40.
-constexpr int ONE_THREADS = 1024;
-constexpr int ONE_WAVES = ONE_THREADS / 64;
-constexpr int ONE_ITEMS = 8;                              // a lane at most
-constexpr int ONE_MAX = ONE_THREADS * ONE_ITEMS;
-// Up to so many tiles each scans the histograms itself, a launch less a pass: 59
-// tiles 41.0 us for 42.7 in all, 118 tiles 47.1 for 43.4.
-constexpr int SCAN_TILES = 64;
+constexpr int SORT_BITS_MAX = 10;
+constexpr int SORT_BINS = 1 << SORT_BITS_MAX;             // at most a thread each
+// The single-workgroup sort, one launch for two a pass: a gradient of 4000
+// tokens in a table of 32003, 26 us for 32; of 8000, 35 us for 32.
+constexpr int ONE_ITEMS = 4;                              // entries a thread at most
+constexpr int ONE_MAX = SORT_THREADS * ONE_ITEMS;
+// Up to so many entries a thread takes one of a tile, not TILE_ITEMS: 16000
+// tokens 30 us for 35, 131000 39 for 42; 720896 75 for 71.
+constexpr int64_t SPREAD_MAX = 131072;
+constexpr int TILE_ITEMS = 4;
+// Up to so many tiles each sums up the histograms itself, a launch less a pass:
+// 176 tiles 71 us for 73 in all, 366 tiles 136 for 104.
+constexpr int SCAN_TILES = 192;
+constexpr int SCAN_PARTS = 16;                            // threads a digit at most
 
 // Zeros for `rows` rows of row_bytes, stride bytes apart, written by the
 // workgroups from `first` on; rows 0: none.
@@ -123,11 +124,11 @@ struct SortIn {
     const void* tokens;   // first pass
     int wide;
     uint32_t vocab;
-    const uint32_t *keys, *pos;   // later passes
+    const uint2* pairs;   // later passes: key, position
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortIn& in, int64_t i) {
-    if (in.keys) return in.keys[i];
+    if (in.pairs) return in.pairs[i].x;
     const int64_t t = token_at(in.tokens, in.wide, i, in.vocab);
     return t >= 0 ? (uint32_t)t : in.vocab;   // dropped tokens sort behind every row
 }
@@ -146,9 +147,9 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, uint64_t ac
 // Rank of each of this wave's entries among the wave's earlier ones of the
 // same digit; counts[] ends as the wave's histogram.  Entries of a wave are
 // 64 * ITEMS consecutive ones, slice by slice.
-template <int ITEMS>
+template <class C, int ITEMS>
 __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[ITEMS], const bool (&in)[ITEMS], int bits,
-                                           volatile uint32_t* counts, uint32_t (&rank)[ITEMS]) {
+                                           volatile C* counts, uint32_t (&rank)[ITEMS]) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int s = 0; s < ITEMS; ++s) {
@@ -158,14 +159,13 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[ITEMS], const
         uint32_t c = 0;
         if (in[s]) c = counts[digit[s]];
         __builtin_amdgcn_wave_barrier();
-        if (in[s] && before == 0) counts[digit[s]] = c + (uint32_t)__popcll(m);
+        if (in[s] && before == 0) counts[digit[s]] = (C)(c + (uint32_t)__popcll(m));
         __builtin_amdgcn_wave_barrier();
         rank[s] = c + before;
     }
 }
 
-// Exclusive scan over THREADS values, one a thread; scratch: THREADS / 64.
-template <int THREADS>
+// Exclusive scan over SORT_THREADS values, one a thread.
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* scratch) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t x = v;
@@ -177,40 +177,42 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* scratch) {
     if (lane == 63) scratch[wave] = x;
     __syncthreads();
     uint32_t base = 0;
-    for (int w = 0; w < wave; ++w) base += scratch[w];
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; ++w) base += w < wave ? scratch[w] : 0;
     __syncthreads();
     return base + x - v;
 }
 
-// hist[d * blocks + b]: entries of tile b with digit d.
+// hist[d * by_digit + b * by_tile]: entries of tile b with digit d.
+template <int ITEMS>   // a lane, one wave slice each
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_hist(SortIn in, int64_t n, int shift, int bits, uint32_t* hist,
-                                                            int blocks, Fill fill) {
-    if ((int)blockIdx.x >= blocks) return fill_zeros(fill);
+                                                            int by_digit, int by_tile, int tiles, Fill fill) {
+    if ((int)blockIdx.x >= tiles) return fill_zeros(fill);
     __shared__ uint32_t cnt[SORT_BINS];
-    const int bins = 1 << bits;
-    for (int d = threadIdx.x; d < bins; d += SORT_THREADS) cnt[d] = 0;
+    const int bins = 1 << bits, d = threadIdx.x;
+    if (d < bins) cnt[d] = 0;
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * SORT_TILE;
+    const int64_t i0 = (int64_t)blockIdx.x * (SORT_THREADS * ITEMS);
 #pragma unroll
-    for (int s = 0; s < SORT_ITEMS; ++s) {
+    for (int s = 0; s < ITEMS; ++s) {
         const int64_t i = i0 + s * SORT_THREADS + threadIdx.x;
         if (i < n) atomicAdd(&cnt[(sort_key(in, i) >> shift) & (bins - 1)], 1u);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < bins; d += SORT_THREADS) hist[(int64_t)d * blocks + blockIdx.x] = cnt[d];
+    if (d < bins) hist[(int64_t)d * by_digit + (int64_t)blockIdx.x * by_tile] = cnt[d];
 }
 
-// One workgroup a digit: exclusive scan over the tiles in place, total[d].
-__global__ __launch_bounds__(SORT_THREADS) void k_sort_scan(uint32_t* hist, int blocks, uint32_t* total) {
+// One workgroup a digit, tiles next to each other: exclusive scan over them in place, total[d].
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_scan(uint32_t* hist, int tiles, uint32_t* total) {
     __shared__ uint32_t scratch[SORT_WAVES];
     __shared__ uint32_t last;
-    uint32_t* h = hist + (int64_t)blockIdx.x * blocks;
+    uint32_t* h = hist + (int64_t)blockIdx.x * tiles;
     uint32_t base = 0;
-    for (int b0 = 0; b0 < blocks; b0 += SORT_THREADS) {
+    for (int b0 = 0; b0 < tiles; b0 += SORT_THREADS) {
         const int b = b0 + threadIdx.x;
-        const uint32_t v = b < blocks ? h[b] : 0;
-        const uint32_t e = block_scan<SORT_THREADS>(v, scratch);
-        if (b < blocks) h[b] = base + e;
+        const uint32_t v = b < tiles ? h[b] : 0;
+        const uint32_t e = block_scan(v, scratch);
+        if (b < tiles) h[b] = base + e;
         if (threadIdx.x == SORT_THREADS - 1) last = e + v;
         __syncthreads();
         base += last;
@@ -219,83 +221,87 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scan(uint32_t* hist, int 
     if (threadIdx.x == 0) total[blockIdx.x] = base;
 }
 
-// total: the digits' totals, hist scanned; or null, and hist as counted.
+// total: the digits' totals, and hist scanned, a digit's tiles next to each
+// other; or null, and hist as counted, a tile's digits next to each other.
+template <int ITEMS>
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(SortIn in, int64_t n, int shift, int bits,
                                                                const uint32_t* hist, const uint32_t* total,
-                                                               uint32_t* keys, uint32_t* pos, int blocks, Fill fill) {
-    if ((int)blockIdx.x >= blocks) return fill_zeros(fill);
+                                                               uint2* pairs, int tiles, Fill fill) {
+    if ((int)blockIdx.x >= tiles) return fill_zeros(fill);
     __shared__ uint32_t cnt[SORT_WAVES][SORT_BINS];
-    __shared__ uint32_t base[SORT_BINS];
+    __shared__ uint32_t s_all[SORT_THREADS], s_before[SORT_THREADS];
     __shared__ uint32_t scratch[SORT_WAVES];
-    const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int d = threadIdx.x; d < bins; d += SORT_THREADS)
-        for (int w = 0; w < SORT_WAVES; ++w) cnt[w][d] = 0;
-    __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * SORT_TILE + wave * 64 * SORT_ITEMS + lane;
-    uint32_t key[SORT_ITEMS], p[SORT_ITEMS], digit[SORT_ITEMS], rank[SORT_ITEMS];
-    bool ok[SORT_ITEMS];
+    const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d = threadIdx.x & (bins - 1);
+    const int part = threadIdx.x >> bits;
+    const int64_t i0 = (int64_t)blockIdx.x * (SORT_THREADS * ITEMS) + wave * 64 * ITEMS + lane;
+    uint2 pair[ITEMS];
+    uint32_t digit[ITEMS], rank[ITEMS];
+    bool ok[ITEMS];
 #pragma unroll
-    for (int s = 0; s < SORT_ITEMS; ++s) {
+    for (int s = 0; s < ITEMS; ++s) {
         const int64_t i = i0 + s * 64;
         ok[s] = i < n;
-        key[s] = ok[s] ? sort_key(in, i) : 0;
-        p[s] = !ok[s] ? 0 : in.keys ? in.pos[i] : (uint32_t)i;
-        digit[s] = (key[s] >> shift) & (bins - 1);
+        pair[s] = make_uint2(0, (uint32_t)i);
+        if (!ok[s]) continue;
+        if (in.pairs)
+            pair[s] = in.pairs[i];
+        else
+            pair[s].x = sort_key(in, i);
     }
-    wave_ranks<SORT_ITEMS>(digit, ok, bits, cnt[wave], rank);
+    // of digit d: entries, and those of earlier tiles
+    uint32_t all = 0, before = 0;
+    if (total) {
+        if (part == 0) {
+            all = total[d];
+            before = hist[(int64_t)d * tiles + blockIdx.x];
+        }
+    } else if (part < SCAN_PARTS) {
+        const int parts = SORT_THREADS >> bits < SCAN_PARTS ? SORT_THREADS >> bits : SCAN_PARTS;
+#pragma unroll 8
+        for (int b = part; b < tiles; b += parts) {
+            const uint32_t x = hist[((int64_t)b << bits) + d];
+            all += x;
+            before += b < (int)blockIdx.x ? x : 0;
+        }
+        s_all[threadIdx.x] = all;
+        s_before[threadIdx.x] = before;
+    }
+    for (int k = threadIdx.x; k < bins * SORT_WAVES; k += SORT_THREADS) cnt[k >> bits][k & (bins - 1)] = 0;
     __syncthreads();
+    if (!total && part == 0)
+        for (int k = threadIdx.x + bins; k < bins * SCAN_PARTS && k < SORT_THREADS; k += bins) {
+            all += s_all[k];
+            before += s_before[k];
+        }
+#pragma unroll
+    for (int s = 0; s < ITEMS; ++s) digit[s] = (pair[s].x >> shift) & (bins - 1);
+    wave_ranks(digit, ok, bits, cnt[wave], rank);
     // where each digit starts: all entries of smaller digits, then those of
     // the same digit in earlier tiles and earlier waves
-    uint32_t run = 0;
-    for (int d0 = 0; d0 < bins; d0 += SORT_THREADS) {
-        const int d = d0 + threadIdx.x;
-        uint32_t t = 0, before = 0;   // of this digit: entries, and those of earlier tiles
-        if (d < bins) {
-            const uint32_t* h = hist + (int64_t)d * blocks;
-            if (total) {
-                t = total[d];
-                before = h[blockIdx.x];
-            } else {
-#pragma unroll 8
-                for (int b = 0; b < blocks; ++b) {
-                    const uint32_t x = h[b];
-                    t += x;
-                    before += b < (int)blockIdx.x ? x : 0;
-                }
-            }
-        }
-        const uint32_t e = block_scan<SORT_THREADS>(t, scratch);
-        if (d < bins) {
-            uint32_t s = run + e + before;
-            for (int w = 0; w < SORT_WAVES; ++w) {
-                const uint32_t c = cnt[w][d];
-                cnt[w][d] = s;
-                s += c;
-            }
-            if (threadIdx.x == SORT_THREADS - 1) base[0] = run + e + t;
-        }
-        __syncthreads();
-        if (d0 + SORT_THREADS < bins) run = base[0];
-        __syncthreads();
-    }
+    uint32_t at = block_scan(part == 0 ? all : 0, scratch) + before;
+    if (part == 0) {
 #pragma unroll
-    for (int s = 0; s < SORT_ITEMS; ++s)
-        if (ok[s]) {
-            const uint32_t at = cnt[wave][digit[s]] + rank[s];
-            keys[at] = key[s];
-            pos[at] = p[s];
+        for (int w = 0; w < SORT_WAVES; ++w) {
+            const uint32_t c = cnt[w][d];
+            cnt[w][d] = at;
+            at += c;
         }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < ITEMS; ++s)
+        if (ok[s]) pairs[cnt[wave][digit[s]] + rank[s]] = pair[s];
 }
 
-// The whole sort of at most ONE_THREADS * ITEMS entries in one workgroup.
+// The whole sort of at most SORT_THREADS * ITEMS entries in one workgroup.
 template <int ITEMS>
-__global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int bits_all, uint32_t* keys,
-                                                          uint32_t* pos, Fill fill) {
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_one(SortIn in, int n, int bits_all, uint2* pairs,
+                                                          Fill fill) {
     if (blockIdx.x > 0) return fill_zeros(fill);
-    __shared__ uint32_t s_key[ONE_THREADS * ITEMS];
-    __shared__ uint16_t s_pos[ONE_THREADS * ITEMS];
-    __shared__ uint32_t cnt[ONE_WAVES][SORT_BINS];
-    __shared__ uint32_t scratch[ONE_WAVES];
+    __shared__ uint32_t s_key[SORT_THREADS * ITEMS];
+    __shared__ uint16_t s_pos[SORT_THREADS * ITEMS];
+    __shared__ uint16_t cnt[SORT_WAVES][SORT_BINS];
+    __shared__ uint32_t scratch[SORT_WAVES];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int i0 = wave * 64 * ITEMS + lane;
     uint32_t key[ITEMS], p[ITEMS], digit[ITEMS], rank[ITEMS];
@@ -310,21 +316,21 @@ __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int 
     for (int shift = 0; shift < bits_all;) {
         const int passes = (bits_all - shift + SORT_BITS_MAX - 1) / SORT_BITS_MAX;
         const int bits = (bits_all - shift + passes - 1) / passes, bins = 1 << bits;
-        for (int d = threadIdx.x; d < bins * ONE_WAVES; d += ONE_THREADS) cnt[d >> bits][d & (bins - 1)] = 0;
+        for (int d = threadIdx.x; d < bins * SORT_WAVES; d += SORT_THREADS) cnt[d >> bits][d & (bins - 1)] = 0;
         __syncthreads();
 #pragma unroll
         for (int s = 0; s < ITEMS; ++s) digit[s] = (key[s] >> shift) & (bins - 1);
-        wave_ranks<ITEMS>(digit, ok, bits, cnt[wave], rank);
+        wave_ranks(digit, ok, bits, cnt[wave], rank);
         __syncthreads();
-        const int d = threadIdx.x;   // bins <= ONE_THREADS
+        const int d = threadIdx.x;   // bins <= SORT_THREADS
         uint32_t t = 0;
         if (d < bins)
-            for (int w = 0; w < ONE_WAVES; ++w) t += cnt[w][d];
-        uint32_t run = block_scan<ONE_THREADS>(t, scratch);
+            for (int w = 0; w < SORT_WAVES; ++w) t += cnt[w][d];
+        uint32_t run = block_scan(t, scratch);
         if (d < bins)
-            for (int w = 0; w < ONE_WAVES; ++w) {
+            for (int w = 0; w < SORT_WAVES; ++w) {
                 const uint32_t c = cnt[w][d];
-                cnt[w][d] = run;
+                cnt[w][d] = (uint16_t)run;
                 run += c;
             }
         __syncthreads();
@@ -346,10 +352,7 @@ __global__ __launch_bounds__(ONE_THREADS) void k_sort_one(SortIn in, int n, int 
     }
 #pragma unroll
     for (int s = 0; s < ITEMS; ++s)
-        if (ok[s]) {
-            keys[i0 + s * 64] = key[s];
-            pos[i0 + s * 64] = p[s];
-        }
+        if (ok[s]) pairs[i0 + s * 64] = make_uint2(key[s], p[s]);
 }
 
 // --------------------------------------------------------------------------
@@ -365,7 +368,7 @@ constexpr int SUM_WORKERS_MAX = EMB_THREADS / SUM_LANES_MIN;
 
 struct SumArgs {
     EmbedGradArgs g;
-    const uint32_t *keys, *pos;
+    const uint2* pairs;   // key, position
     float *head, *tail;   // [workgroups][dpad]
     int32_t* meta;        // [workgroups][2]: whether the row of its tail begins here; the row that goes on from the
                           // workgroup before and ends here, or -1
@@ -432,8 +435,9 @@ __global__ __launch_bounds__(EMB_THREADS) void k_embed_sum(SumArgs a) {
     // local entry q is entry j0 + q, with its key in s_key[q + 1]
     for (int k = threadIdx.x; k < m + 2; k += EMB_THREADS) {
         const int64_t j = j0 - 1 + k;
-        s_key[k] = j >= 0 && j < n ? a.keys[j] : 0xffffffffu;
-        if (k < m) s_pos[k] = a.pos[j0 + k];
+        const uint2 e = j >= 0 && j < n ? a.pairs[j] : make_uint2(0xffffffffu, 0);
+        s_key[k] = e.x;
+        if (k >= 1 && k <= m) s_pos[k - 1] = e.y;
     }
     __syncthreads();
     const int q0 = w * a.each < m ? w * a.each : m, q1 = q0 + a.each < m ? q0 + a.each : m;
@@ -610,10 +614,10 @@ int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // Workers and workspace of one gradient.
 struct GradPlan {
-    int txs, each, groups, ytiles, sort_blocks;
+    int txs, each, groups, ytiles, tiles;   // tiles 0: sorted by one workgroup
     bool narrow;
     int64_t dpad;
-    int64_t off_keys[2], off_pos[2], off_hist, off_total, off_head, off_tail, off_meta, bytes;
+    int64_t off_pairs[2], off_hist, off_total, off_head, off_tail, off_meta, bytes;
 };
 GradPlan plan_grad(int64_t n, int64_t dim, int size) {
     GradPlan p{};
@@ -629,19 +633,17 @@ GradPlan plan_grad(int64_t n, int64_t dim, int size) {
     while (p.each * 2 * ty <= SUM_ENTRIES_MAX && n * p.ytiles > (int64_t)p.each * 2 * ty * 2048) p.each *= 2;
     p.groups = (int)((n + p.each * ty - 1) / (p.each * ty));
     p.dpad = align_up(dim, 8);
-    p.sort_blocks = n <= ONE_MAX ? 0 : (int)((n + SORT_TILE - 1) / SORT_TILE);
+    const int tile = SORT_THREADS * (n <= SPREAD_MAX ? 1 : TILE_ITEMS);
+    p.tiles = n <= ONE_MAX ? 0 : (int)((n + tile - 1) / tile);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t off = at;
         at = align_up(at + bytes, 256);
         return off;
     };
-    for (int k = 0; k < (p.sort_blocks ? 2 : 1); ++k) {
-        p.off_keys[k] = take(4 * n);
-        p.off_pos[k] = take(4 * n);
-    }
-    p.off_hist = take((int64_t)4 * SORT_BINS * p.sort_blocks);
-    p.off_total = take(p.sort_blocks ? 4 * SORT_BINS : 0);
+    for (int k = 0; k < (p.tiles ? 2 : 1); ++k) p.off_pairs[k] = take(8 * n);
+    p.off_hist = take((int64_t)4 * SORT_BINS * p.tiles);
+    p.off_total = take(p.tiles ? 4 * SORT_BINS : 0);
     p.off_head = take(4 * p.dpad * p.groups);
     p.off_tail = take(4 * p.dpad * p.groups);
     p.off_meta = take((int64_t)8 * p.groups);
@@ -681,35 +683,32 @@ int64_t embed_grad_workspace(int64_t n, int64_t dim) {
 hipError_t launch_embed_grad(const EmbedGradArgs& g, void* workspace, hipStream_t stream) {
     const GradPlan p = plan_grad(g.n, g.dim, elem_size(g.dtype));
     char* ws = static_cast<char*>(workspace);
-    uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + p.off_keys[0]), reinterpret_cast<uint32_t*>(ws + p.off_keys[1])};
-    uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(ws + p.off_pos[0]), reinterpret_cast<uint32_t*>(ws + p.off_pos[1])};
+    uint2* pairs[2] = {reinterpret_cast<uint2*>(ws + p.off_pairs[0]), reinterpret_cast<uint2*>(ws + p.off_pairs[1])};
     int bits_all = 1;   // keys reach vocab
     while (((int64_t)1 << bits_all) <= g.vocab) ++bits_all;
     auto passes_of = [](int bits) { return (bits + SORT_BITS_MAX - 1) / SORT_BITS_MAX; };
     // the rows to clear, shared out over the launches of the sort
     const int64_t size = elem_size(g.gtype);
-    int launches = p.sort_blocks ? 2 * passes_of(bits_all) : 1;
+    int launches = p.tiles ? 2 * passes_of(bits_all) : 1;
     int64_t cleared = g.accumulate ? g.vocab : 0;
-    auto fill_of = [&](int first, int threads) {
+    auto fill_of = [&](int first) {
         Fill f{static_cast<char*>(g.dweight) + cleared * g.ldg * size, (g.vocab - cleared) / launches, g.dim * size,
                g.ldg * size, first};
         --launches;
         cleared += f.rows;
-        const int64_t groups = (f.rows * f.row_bytes + threads * 64 - 1) / (threads * 64);
+        const int64_t groups = (f.rows * f.row_bytes + SORT_THREADS * 64 - 1) / (SORT_THREADS * 64);
         return std::pair<Fill, int>(f, (int)(groups < 2048 ? groups : 2048));
     };
-    SortIn in{g.tokens, g.wide, (uint32_t)g.vocab, nullptr, nullptr};
+    SortIn in{g.tokens, g.wide, (uint32_t)g.vocab, nullptr};
     int cur = 0;
-    if (!p.sort_blocks) {
-        const auto f = fill_of(1, ONE_THREADS);
+    if (!p.tiles) {
+        const auto f = fill_of(1);
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(1 + f.second), dim3(ONE_THREADS), 0, stream, in, (int)g.n, bits_all, keys[0],
-                               pos[0], f.first);
+            hipLaunchKernelGGL(kernel, dim3(1 + f.second), dim3(SORT_THREADS), 0, stream, in, (int)g.n, bits_all, pairs[0],
+                               f.first);
         };
-        if (g.n <= ONE_THREADS)
+        if (g.n <= SORT_THREADS)
             go(k_sort_one<1>);
-        else if (g.n <= 4 * ONE_THREADS)
-            go(k_sort_one<4>);
         else
             go(k_sort_one<ONE_ITEMS>);
     } else {
@@ -717,26 +716,32 @@ hipError_t launch_embed_grad(const EmbedGradArgs& g, void* workspace, hipStream_
         uint32_t* total = reinterpret_cast<uint32_t*>(ws + p.off_total);
         for (int shift = 0; shift < bits_all;) {
             const int passes = passes_of(bits_all - shift), bits = (bits_all - shift + passes - 1) / passes;
-            auto f = fill_of(p.sort_blocks, SORT_THREADS);
-            hipLaunchKernelGGL(k_sort_hist, dim3(p.sort_blocks + f.second), dim3(SORT_THREADS), 0, stream, in, g.n, shift,
-                               bits, hist, p.sort_blocks, f.first);
-            const bool scan = p.sort_blocks > SCAN_TILES;
-            if (scan)
-                hipLaunchKernelGGL(k_sort_scan, dim3(1 << bits), dim3(SORT_THREADS), 0, stream, hist, p.sort_blocks,
-                                   total);
-            f = fill_of(p.sort_blocks, SORT_THREADS);
-            hipLaunchKernelGGL(k_sort_scatter, dim3(p.sort_blocks + f.second), dim3(SORT_THREADS), 0, stream, in, g.n,
-                               shift, bits, hist, scan ? total : nullptr, keys[cur], pos[cur], p.sort_blocks, f.first);
-            in.keys = keys[cur];
-            in.pos = pos[cur];
+            const bool scan = p.tiles > SCAN_TILES;
+            auto go = [&](auto items) {
+                constexpr int ITEMS = decltype(items)::value;
+                auto f = fill_of(p.tiles);
+                hipLaunchKernelGGL(k_sort_hist<ITEMS>, dim3(p.tiles + f.second), dim3(SORT_THREADS), 0, stream, in,
+                                   g.n, shift, bits, hist, scan ? p.tiles : 1, scan ? 1 : 1 << bits,
+                                   p.tiles, f.first);
+                if (scan)
+                    hipLaunchKernelGGL(k_sort_scan, dim3(1 << bits), dim3(SORT_THREADS), 0, stream, hist,
+                                       p.tiles, total);
+                f = fill_of(p.tiles);
+                hipLaunchKernelGGL(k_sort_scatter<ITEMS>, dim3(p.tiles + f.second), dim3(SORT_THREADS), 0, stream,
+                                   in, g.n, shift, bits, hist, scan ? total : nullptr, pairs[cur], p.tiles, f.first);
+            };
+            if (g.n <= SPREAD_MAX)
+                go(std::integral_constant<int, 1>());
+            else
+                go(std::integral_constant<int, TILE_ITEMS>());
+            in.pairs = pairs[cur];
             shift += bits;
             if (shift < bits_all) cur ^= 1;
         }
     }
     if (g.n == 0) return hipGetLastError();
     SumArgs a{g,
-              keys[cur],
-              pos[cur],
+              pairs[cur],
               reinterpret_cast<float*>(ws + p.off_head),
               reinterpret_cast<float*>(ws + p.off_tail),
               reinterpret_cast<int32_t*>(ws + p.off_meta),

@@ -124,7 +124,7 @@ def reference(dout, t, vocab, scale, before):
     (12000, 64, 200, "f32", "bf16", 0, "none", True, False),
     (12000, 64, 200, "f32", "bf16", 0, "none", True, True),
     (300, 20, 9001, "f32", "f32", 1, "flat", True, False),
-    # histograms scanned by a launch of their own; rows over many workgroups; narrow rows
+    # more entries than a tile each; rows over many workgroups; narrow rows
     (100000, 3000, 40, "bf16", "f32", 0, "outside", True, False),
     (150000, 2, 24, "f16", "f32", 1, "flat", False, True),
     (70000, 70001, 3, "f32", "f32", 0, "frequent", True, False),
@@ -154,6 +154,26 @@ def test_gradient(P, n, vocab, dim, dt, gt, pad, kind, wide, add):
         assert torch.equal(got[count == 0][:, :dim], before[count == 0])
     else:
         assert bool((got[count == 0][:, :dim] == 0).all())
+
+
+@pytest.mark.parametrize("n,vocab,dim,dt,gt,kind,wide,add", [
+    # one workgroup's sort, a few entries a thread, tiles
+    (1024, 1023, 16, "f32", "f32", "flat", True, False),
+    (1025, 1024, 16, "bf16", "f32", "outside", False, False),
+    (4096, 2000, 8, "f32", "f32", "frequent", True, False),
+    (4097, 2000, 8, "f32", "f32", "frequent", False, True),
+    (4097, 1, 8, "f32", "f32", "outside", True, False),
+    # one and four entries a thread
+    (131072, 1100000, 4, "f32", "f32", "flat", False, False),
+    (131073, 70000, 8, "bf16", "f32", "outside", True, False),
+    # the most tiles that scan for themselves, and a launch that scans
+    (192 * 4096, 1024, 8, "bf16", "f32", "flat", False, False),
+    (192 * 4096 + 1, 1023, 8, "bf16", "f32", "outside", True, True),
+    (1100000, 3, 8, "bf16", "f32", "outside", False, False),
+])
+def test_gradient_sort_sizes(P, n, vocab, dim, dt, gt, kind, wide, add):
+    """Where the sort changes its launches: numbers of entries, and of bits."""
+    test_gradient(P, n, vocab, dim, dt, gt, 0, kind, wide, add)
 
 
 def test_gradient_is_reproducible(P):
