@@ -206,6 +206,53 @@ def test_gradient_of_a_broadcast_row(P):
     assert torch.equal(out, want)
 
 
+def far_rows(shape, dtype, apart, gen):
+    """A [n, d] tensor whose rows lie apart elements from one another."""
+    import torch
+    n, d = shape
+    buf = torch.empty((n - 1) * apart + d, dtype=dtype, device=DEV)
+    x = torch.as_strided(buf, (n, d), (apart, 1))
+    x.copy_(torch.randn(n, d, generator=gen).to(dtype).to(DEV))
+    return x
+
+
+def test_rows_past_32_bits(P):
+    """Tables, gradients and outputs whose last rows start past 2^31 elements."""
+    import torch
+    gen = torch.Generator().manual_seed(9)
+    apart = (1 << 30) + 8
+    t = torch.tensor([2, 0, 2, 3, 1, 2], device=DEV)
+    w = far_rows((3, 100), torch.bfloat16, apart, gen)
+    out = far_rows((6, 100), torch.bfloat16, 1 << 29, gen)
+    P.at_embed(w, t, out, scale=1.5)
+    want = torch.empty(6, 100, dtype=torch.bfloat16, device=DEV)
+    P.at_embed(w.contiguous(), t, want, scale=1.5)
+    assert torch.equal(out, want)
+    for add in (False, True):
+        before = w.contiguous()
+        P.at_embed_grad(out, t, w, accumulate=add)
+        P.at_embed_grad(out.contiguous(), t, before, accumulate=add)
+        assert torch.equal(w, before)
+
+
+def test_tokens_past_32_bits(P):
+    """64-bit tokens whose low words are in range are not."""
+    import torch
+    gen = torch.Generator().manual_seed(10)
+    w = torch.randn(5, 40, generator=gen).to(DEV)
+    t = torch.tensor([1, (1 << 32) + 1, -(1 << 32) + 2, (1 << 63) - 1, 4, -(1 << 63)], device=DEV)
+    out = torch.full((6, 40), 3.0, device=DEV)
+    P.at_embed(w, t, out)
+    want = torch.zeros_like(out)
+    want[0], want[4] = w[1], w[4]
+    assert torch.equal(out, want)
+    dw = torch.full_like(w, 3.0)
+    P.at_embed_grad(torch.ones_like(out), t, dw)
+    want = torch.zeros_like(w)
+    want[1] = want[4] = 1.0
+    assert torch.equal(dw, want)
+
+
 def test_gradient_against_differences(P):
     """The lookup is linear in the table: <dout, embed(W + E) - embed(W)> is
     <gradient, E> for any E, exactly in exact arithmetic.  Whole numbers and

@@ -296,6 +296,26 @@ def test_long_row_past_32_bits(P):
     assert torch.equal(got, want)
 
 
+def test_gradient_past_32_bits(P):
+    """Logits and gradients whose last rows start past 2^31 elements, and 64-bit
+    tokens whose low words are in range."""
+    import torch
+    gen = torch.Generator().manual_seed(7)
+    n, vocab, ld = 4, 1000, (1 << 30) + 1
+    bufs = [torch.empty((n - 1) * ld + vocab, dtype=torch.float16, device=DEV) for _ in range(2)]
+    x, d = (torch.as_strided(b, (n, vocab), (ld, 1)) for b in bufs)
+    x.copy_(torch.randn(n, vocab, generator=gen).half().to(DEV))
+    t = torch.tensor([5, (1 << 32) + 6, 7, 8], device=DEV)
+    logp, lse, g = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.ones(n, device=DEV)
+    P.at_logprobs(x, t, logp, lse=lse)
+    assert bool(torch.isfinite(lse).all())
+    P.at_logprobs_grad(x, t, lse, None, g, d)
+    want = torch.empty(n, vocab, dtype=torch.float16, device=DEV)
+    P.at_logprobs_grad(x.contiguous(), t, lse, None, g, want)
+    assert torch.equal(d, want)
+    assert bool((d[1] == 0).all()) and not bool((d[0] == 0).all())
+
+
 def test_graph_and_streams(P):
     import torch
     gen = torch.Generator().manual_seed(8)

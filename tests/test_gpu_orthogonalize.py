@@ -147,6 +147,21 @@ def test_strides_scale_and_neighbours(P):
         assert bool((rest == 7.0).all())
 
 
+@pytest.mark.parametrize("rows,cols", [(3, 40), (3, 300)])
+def test_rows_past_32_bits(P, rows, cols):
+    """The last matrix, and its last row, start past 2^31 elements."""
+    import torch
+    gen = torch.Generator().manual_seed(8)
+    apart = (1 << 30) + 8
+    x, o = (torch.as_strided(torch.empty(2 * rows * apart, dtype=torch.bfloat16, device=DEV), (2, rows, cols),
+                             (rows * apart, apart, 1)) for _ in range(2))
+    x.copy_(torch.randn(2, rows, cols, generator=gen).bfloat16().to(DEV))
+    want = torch.empty(2, rows, cols, dtype=torch.bfloat16, device=DEV)
+    P.at_orthogonalize(x.contiguous(), want)
+    P.at_orthogonalize(x, o)
+    assert torch.equal(o, want)
+
+
 def test_batch_equals_single_and_repeats(P):
     import torch
     gen = torch.Generator().manual_seed(2)
