@@ -534,9 +534,11 @@ at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, 
  * bits.  fp32 outputs, and matrices whose shorter side is at most 64, have
  * fp32's accuracy before the result is rounded; other bf16 outputs are within
  * about 2.4e-3 of their norm (bf16's own rounding is 1.7e-3 of it).
- * A matrix of zeros gives zeros.  1 <= steps <= 64; batch <= 65535, rows and cols
- * <= 65536, AT_E_UNSUPPORTED beyond; coefficients that let singular values
- * grow past 8 overflow.  Workspace: at_orthogonalize_workspace bytes. */
+ * The same call gives the same bits; a batch may sum in another order than its
+ * matrices one by one.  A matrix of zeros gives zeros.  1 <= steps <= 64;
+ * batch <= 65535, rows and cols <= 65536, AT_E_UNSUPPORTED beyond;
+ * coefficients that let singular values grow past 8 overflow.  Workspace:
+ * at_orthogonalize_workspace bytes. */
 at_status at_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int otype, int64_t* bytes);
 at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx, int64_t batch, int64_t rows,
                            int64_t cols, int steps, float a, float b, float c, float eps, float scale, void* out,

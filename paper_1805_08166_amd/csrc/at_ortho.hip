@@ -48,6 +48,7 @@ struct OrthoBufs {
     half_t* XT[2][2];     // [step & 1]: X transposed, [batch][lp][sp]
     half_t *A[2], *B[2];  // [batch][sp][sp]
     double* part;         // [batch][NORM_BLOCKS]
+    float* sums;          // pieces of A
 };
 constexpr int NORM_BLOCKS = 256;
 constexpr int NORM_THREADS = 256;
@@ -156,6 +157,7 @@ __global__ __launch_bounds__(256) void k_layout(OrthoArgs a, OrthoBufs b, int sp
 // --------------------------------------------------------------------------
 // C[i, j] = sum_k P[i, k] Q[j, k], both operands along k
 // --------------------------------------------------------------------------
+typedef float float4v __attribute__((ext_vector_type(4)));
 enum { GRAM = 0, POLY = 1, UPDATE = 2, FINAL = 3 };
 
 struct GemmArgs {
@@ -175,7 +177,10 @@ struct GemmArgs {
     int otype;
     int64_t obatch, ldo;
     int rows, cols, tall;
+    int phase, pieces;           // of a product whose depth is cut (GRAM)
+    float* sums;                 // [tile][piece], each in the order of its lanes
 };
+enum { WHOLE = 0, PIECES = 1, JOIN = 2 };
 
 // A fragment in LDS: rows of 36 floats, 16-byte aligned.
 constexpr int FRAG_LD = 36, FRAG_FLOATS = 32 * FRAG_LD;
@@ -306,7 +311,23 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
     const int i0 = bi * ROWS, j0 = bj * COLS;
     const int wk = wave / (S::WR * S::WC), wq = wave % (S::WR * S::WC);
     const int wr = wq / S::WC * FR * 32, wc = wq % S::WC * FC * 32;
-    const int steps = a.depth / BK, total = steps * (SPLIT ? 3 : 1);
+    const int steps = a.depth / BK;
+    int pass = 0, ks = 0, total = steps * (SPLIT ? 3 : 1);   // of the tile staged next; tiles in all
+    constexpr bool CUT = MODE == GRAM && FR == 1 && FC == 1 && S::WK == 1;
+    float4v* sums = nullptr;   // of this lane, in the first piece or its own
+    if (CUT && a.phase != WHOLE) {
+        const int piece = a.phase == PIECES ? blockIdx.y : 0;
+        const int tile = z * (a.ti * (a.ti + 1) / 2) + bi * (bi + 1) / 2 + bj;
+        sums = reinterpret_cast<float4v*>(a.sums) + ((int64_t)(tile * a.pieces + piece) * S::WAVES + wave) * 256 + lane;
+        if (a.phase == PIECES) {
+            const int k0 = total * piece / a.pieces;
+            total = total * (piece + 1) / a.pieces - k0;
+            pass = k0 / steps;
+            ks = k0 - pass * steps;
+        } else {
+            total = 0;
+        }
+    }
     // A tile goes to LDS by direct moves of 16 bytes a lane, eight rows each:
     // first P's rows, then Q's; this lane's bytes lie at at_row from the tile's start.
     constexpr int MOVES = S::MOVES;
@@ -318,7 +339,6 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
         if (second) r -= ROWS;
         at_row[q] = (uint32_t)((r * (second ? a.ldq : a.ldp) + slot_of(r, lane & 7) * 8) * 2);
     }
-    int pass = 0, ks = 0;   // of the tile staged next
     const char *srcP = nullptr, *srcQ = nullptr;
     auto next_tile = [&]() {
         srcP = reinterpret_cast<const char*>(a.P[SPLIT && pass == 2] + z * a.pbatch + (int64_t)i0 * a.ldp + ks * BK);
@@ -345,6 +365,16 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
         for (int c = 0; c < FC; ++c)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[r][c][e] = 0.0f;
+    if (CUT && a.phase == JOIN) {   // the pieces in order
+#pragma unroll 4
+        for (int n = 0; n < a.pieces; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4v v = sums[(n * S::WAVES * 4 + g) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[0][0][g * 4 + e] += v[e];
+            }
+    }
     // Fragments of 16 along the depth, KK of them a tile and wave, are read one
     // ahead of the products that use them, across tiles too: before the last of a
     // tile's products the wave sees to it that the next tile has landed and that
@@ -377,7 +407,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
         wait_moves<(STAGES - 1) * S::MOVES>();
     else
         wait_moves<0>();
-    fragments(0, 0);
+    if (!CUT || total) fragments(0, 0);
     int cur = 0;
     for (int k = 0; k < total; ++k) {
 #pragma unroll
@@ -404,6 +434,16 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
         }
         products(KK - 1);
         __builtin_amdgcn_sched_barrier(0);
+    }
+    if (CUT && a.phase == PIECES) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float4v v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[0][0][g * 4 + e];
+            sums[g * 64] = v;
+        }
+        return;
     }
     __syncthreads();   // the tiles' LDS is free
     float* all = reinterpret_cast<float*>(s_tiles);
@@ -455,7 +495,6 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
             const int fi = i0 + wr + r * 32;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                typedef float float4v __attribute__((ext_vector_type(4)));
                 float4v w;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = acc[r][c][g * 4 + e] * a.mul;
@@ -665,8 +704,25 @@ struct OrthoPlan {
     bool split;
     int small;            // side of the one-workgroup kernel, or 0
     float xs;
-    int64_t off_x[2], off_t[2][2], off_a[2], off_b[2], off_part, bytes;
+    int pieces;           // of A's depth
+    int64_t off_x[2], off_t[2][2], off_a[2], off_b[2], off_part, off_sums, bytes;
 };
+int64_t triangle_of(int64_t n) { return n * (n + 1) / 2; }
+
+// Few tiles of A leave most CUs without one: their depth is then cut into pieces
+// of at least PIECE_TILES staged tiles, at most a workgroup for every CU, and joined by a
+// launch of its own (about 4 us) where that takes PIECE_GAIN tiles (0.36 us each) off
+// the longest.  us, cut and not: 1 x 16 x 4096 111 and 394; 5 x 64 x 2048 112 and 236;
+// 1 x 128 x 4096 100 and 155, fp32 133 and 419; 1 x 512 x 4096 148 and 201;
+// 1 x 32 x 512 87 and 98 (16 tiles off); 4 x 256 x 1024 103 and 99 (8 off).
+constexpr int64_t PIECE_TILES = 8, PIECES_MAX = 16, PIECE_GAIN = 12;
+int64_t pieces_of(int64_t batch, const OrthoPlan& p) {
+    const int64_t groups = batch * triangle_of(p.sp / TILE), tiles = p.lp / TILE * (p.split ? 3 : 1);
+    int64_t n = 256 / groups;
+    if (n > tiles / PIECE_TILES) n = tiles / PIECE_TILES;
+    if (n > PIECES_MAX) n = PIECES_MAX;
+    return n > 1 && tiles - tiles / n >= PIECE_GAIN ? n : 1;
+}
 OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, int otype) {
     OrthoPlan p{};
     p.tall = rows > cols;
@@ -699,6 +755,8 @@ OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, int otype) {
         p.off_b[h] = take(used ? sq : 0);
     }
     p.off_part = take(batch * NORM_BLOCKS * 8);
+    p.pieces = (int)pieces_of(batch, p);
+    p.off_sums = take(p.pieces > 1 ? batch * triangle_of(p.sp / TILE) * p.pieces * TILE * TILE * 4 : 0);
     p.bytes = at;
     return p;
 }
@@ -721,7 +779,8 @@ hipError_t gemm_as(GemmArgs a, int64_t batch, hipStream_t stream) {
     a.tj /= S::COLS / TILE;
     const bool sym = MODE == GRAM || MODE == POLY;
     const int64_t tiles = sym ? (int64_t)a.ti * (a.ti + 1) / 2 : (int64_t)a.ti * a.tj;
-    hipLaunchKernelGGL((k_gemm<S, MODE, SPLIT>), dim3((unsigned)(tiles * batch)), dim3(S::THREADS), S::LDS, stream, a);
+    hipLaunchKernelGGL((k_gemm<S, MODE, SPLIT>), dim3((unsigned)(tiles * batch), MODE == GRAM && a.phase == PIECES ? a.pieces : 1),
+                       dim3(S::THREADS), S::LDS, stream, a);
     return hipGetLastError();
 }
 template <int MODE, bool SPLIT>
@@ -767,6 +826,14 @@ hipError_t run_steps(const OrthoArgs& o, const OrthoPlan& p, const OrthoBufs& b,
         g.cbatch = sb;
         g.ldt = g.ldc = sp;
         g.mul = A_SCALE / (p.xs * p.xs);
+        if (p.pieces > 1) {
+            g.pieces = p.pieces;
+            g.sums = b.sums;
+            g.phase = PIECES;
+            e = gemm<GRAM, SPLIT>(g, o.batch, stream);
+            if (e != hipSuccess) return e;
+            g.phase = JOIN;
+        }
         e = gemm<GRAM, SPLIT>(g, o.batch, stream);
         for (int h = 0; h < 2; ++h) {
             g.P[h] = g.Q[h] = b.A[h];
@@ -843,6 +910,7 @@ hipError_t launch_ortho(const OrthoArgs& o, void* workspace, hipStream_t stream)
         b.B[h] = buf(p.off_b[h]);
     }
     b.part = reinterpret_cast<double*>(ws + p.off_part);
+    b.sums = reinterpret_cast<float*>(ws + p.off_sums);
     const int sp = (int)p.sp, lp = (int)p.lp;
     const hipError_t e = with_type(o.xtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;

@@ -128,6 +128,20 @@ def test_large(P, batch, rows, cols, ot):
         assert err < (1e-4 if ot == "f32" else 3e-3 + 2.0 ** -8), (k, err)
 
 
+@pytest.mark.parametrize("batch,rows,cols,dt,ot,steps,kind", [
+    (1, 1, 1500, "f32", "f32", 3, "plain"),
+    (1, 40, 3990, "f32", "f32", 5, "plain"),
+    (3, 2001, 64, "bf16", "bf16", 5, "plain"),
+    (2, 33, 1024, "f16", "f32", 5, "plain"),
+    (1, 65, 4000, "bf16", "bf16", 5, "plain"),
+    (1, 4001, 100, "f32", "f32", 5, "plain"),
+    (40, 20, 1100, "f32", "bf16", 4, "plain"),
+])
+def test_few_rows_and_long_ones(P, batch, rows, cols, dt, ot, steps, kind):
+    """X X^T in few tiles, whose depth is cut into pieces."""
+    test_steps(P, batch, rows, cols, dt, ot, steps, kind)
+
+
 def test_strides_scale_and_neighbours(P):
     """Views with gaps between rows and matrices, a scale; nothing outside the
     output's rows is touched, and what lies between the input's rows is not read."""
