@@ -53,6 +53,15 @@ struct OrthoBufs {
 constexpr int NORM_BLOCKS = 256;
 constexpr int NORM_THREADS = 256;
 
+// A value rounded to fp16, and what that left.  Both are of the same fp32 value: the
+// barrier keeps the compiler from rounding the first word from an unrounded product,
+// which near the middle of two fp16 values is not the word that the second belongs to.
+__device__ __forceinline__ void split_words(float v, half_t& h, half_t& l) {
+    asm("" : "+v"(v));
+    h = (half_t)v;
+    l = (half_t)(v - (float)h);
+}
+
 // --------------------------------------------------------------------------
 // Norm and layout
 // --------------------------------------------------------------------------
@@ -126,8 +135,8 @@ __global__ __launch_bounds__(256) void k_layout(OrthoArgs a, OrthoBufs b, int sp
     half8 w[2][2];   // word, half of the segment
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        const float y = v[e] * f;
-        const half_t h = (half_t)y, l = (half_t)(y - (float)h);
+        half_t h, l;
+        split_words(v[e] * f, h, l);
         w[0][e >> 3][e & 7] = h;
         w[1][e >> 3][e & 7] = l;
         s_w[0][seg + e][line] = h;
@@ -191,8 +200,10 @@ __device__ __forceinline__ void put_words(half_t* const (&to)[2], int64_t at, fl
     half8 h, l;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        h[e] = (half_t)v[e];
-        if (BOTH) l[e] = (half_t)(v[e] - (float)h[e]);
+        half_t first, rest;
+        split_words(v[e], first, rest);
+        h[e] = first;
+        if (BOTH) l[e] = rest;
     }
     *reinterpret_cast<half8*>(to[0] + at) = h;
     if (BOTH) *reinterpret_cast<half8*>(to[1] + at) = l;
@@ -587,8 +598,10 @@ struct Words {
     __device__ __forceinline__ explicit Words(const float16v& v) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            h[e >> 2][e & 3] = (half_t)v[e];
-            if (SPLIT) l[e >> 2][e & 3] = (half_t)(v[e] - (float)h[e >> 2][e & 3]);
+            half_t first, rest;
+            split_words(v[e], first, rest);
+            h[e >> 2][e & 3] = first;
+            if (SPLIT) l[e >> 2][e & 3] = rest;
         }
     }
 };

@@ -250,3 +250,24 @@ def test_graph_replays(P):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 700, 321), (1, 321, 700), (2, 1500, 1100), (1, 90, 3000), (30, 128, 120)])
+def test_both_words_of_x_belong_together(P, batch, rows, cols):
+    """With coefficients (a, 0, 0) a step multiplies X by a: element by element, what the
+    two words cannot hold (2^-22 of it, or half an fp16 subnormal in units of a power of two next to
+    sqrt(rows cols)) and a rounding of a product, each time X is written."""
+    import math
+    import torch
+    gen = torch.Generator().manual_seed(9)
+    g = torch.randn(batch, rows, cols, generator=gen)
+    out = torch.empty(batch, rows, cols, device=DEV)
+    unit = 2.0 ** math.floor(math.log2(math.sqrt(rows * cols)))
+    for steps, a in ((1, 1.0), (3, 1.7)):
+        P.at_orthogonalize(g.to(DEV), out, steps=steps, coef=(a, 0.0, 0.0))
+        a = float(torch.tensor(a, dtype=torch.float32))
+        for k in range(batch):
+            want = g[k].double() / (g[k].double().norm() + 1e-7) * a ** steps
+            err = (out[k].cpu().double() - want).abs()
+            tol = (steps + 1) * (2.0 ** -21 * want.abs() + a ** steps * 2.0 ** -24 / unit)
+            assert bool((err <= tol).all()), (steps, k, float((err / tol).max()))
