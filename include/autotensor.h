@@ -523,6 +523,8 @@ at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, 
                            const void* tokens, int itype, float scale, const float* lse, const float* entropy,
                            const float* dlogp, const float* dentropy, void* dlogits, int64_t ldd, at_stream_t stream);
 
+enum { AT_FP16_PRODUCTS = 16 };
+
 /* Orthogonalises a batch of equal matrices by Newton-Schulz steps, as an
  * update of hidden matrices wants it (singular values driven towards 1):
  *   X = x / (|x|_F + eps);  steps times:  A = X X^T, B = b A + c A A, X = a X + B X
@@ -530,10 +532,12 @@ at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, 
  * (on the transpose when rows > cols).  x: device [batch][rows][cols] xtype,
  * matrices xbatch and rows ldx elements apart; out: device, bf16 or fp32
  * (otype), obatch and ldo apart; out may be x, of the same type.  The products
- * run on the matrix cores with fp16 operands and fp32 sums while X keeps 22
- * bits.  fp32 outputs, and matrices whose shorter side is at most 64, have
- * fp32's accuracy before the result is rounded; other bf16 outputs are within
- * about 2.4e-3 of their norm (bf16's own rounding is 1.7e-3 of it).
+ * run on the matrix cores, each operand as two fp16 words (22 bits), with fp32
+ * sums: before they are rounded to otype, results are as far off as fp32 products
+ * would leave them (1e-6 to 3e-6 of their norm with the default steps).  otype | AT_FP16_PRODUCTS asks for products of the first words alone
+ * where the shorter side is above 128, in about a third of the time for large
+ * matrices: bf16 results are then within 2.4e-3 of their norm, of which bf16's
+ * own rounding is 1.7e-3.
  * The same call gives the same bits; a batch may sum in another order than its
  * matrices one by one.  A matrix of zeros gives zeros.  1 <= steps <= 64;
  * batch <= 65535, rows and cols <= 65536, AT_E_UNSUPPORTED beyond;

@@ -67,6 +67,7 @@ at_status row_args(const char* fn, int type, int64_t ld, int64_t n, int64_t voca
 }
 
 at_status ortho_args(const char* fn, int64_t batch, int64_t rows, int64_t cols, int otype) {
+    otype &= ~AT_FP16_PRODUCTS;
     if (otype != AT_BF16 && otype != AT_F32) return refuse(AT_E_UNSUPPORTED, fn, "the output is bf16 or fp32");
     if (batch < 0 || rows < 0 || cols < 0) return refuse(AT_E_INVALID, fn, "negative size");
     if (batch > 65535 || rows > 65536 || cols > 65536)
@@ -175,7 +176,7 @@ at_status at_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, 
     if (!bytes) return refuse(AT_E_INVALID, fn, "NULL output");
     const at_status st = ortho_args(fn, batch, rows, cols, otype);
     if (st != AT_OK) return st;
-    *bytes = batch && rows && cols ? ortho_workspace(batch, rows, cols, otype) : 0;
+    *bytes = batch && rows && cols ? ortho_workspace(batch, rows, cols, (otype & AT_FP16_PRODUCTS) != 0) : 0;
     return AT_OK;
 }
 
@@ -185,6 +186,8 @@ at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx
     const char* fn = "at_orthogonalize";
     at_status st = ortho_args(fn, batch, rows, cols, otype);
     if (st != AT_OK) return st;
+    const bool fp16_products = (otype & AT_FP16_PRODUCTS) != 0;
+    otype &= ~AT_FP16_PRODUCTS;
     if (!type_ok(xtype)) return refuse(AT_E_INVALID, fn, "unknown element type");
     if (ldx < 0 || xbatch < 0) return refuse(AT_E_INVALID, fn, "negative stride");
     if (ldo < cols) return refuse(AT_E_INVALID, fn, "output rows overlap (stride below cols)");
@@ -196,9 +199,10 @@ at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx
     if (batch > 1 && (obatch < (rows - 1) * ldo + cols)) return refuse(AT_E_INVALID, fn, "output matrices overlap");
     if (!x || !out) return refuse(AT_E_INVALID, fn, "NULL buffer");
     if (!aligned_t(x, xtype) || !aligned_t(out, otype)) return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
-    st = workspace_args(fn, workspace, workspace_bytes, ortho_workspace(batch, rows, cols, otype));
+    st = workspace_args(fn, workspace, workspace_bytes, ortho_workspace(batch, rows, cols, fp16_products));
     if (st != AT_OK) return st;
-    const OrthoArgs o{x, xtype, xbatch, ldx, batch, rows, cols, steps, a, b, c, eps, scale, out, otype, obatch, ldo};
+    const OrthoArgs o{x, xtype, xbatch, ldx,   batch, rows,  cols,   steps, a,
+                      b, c,     eps,    scale, out,   otype, obatch, ldo,   fp16_products};
     return done(launch_ortho(o, workspace, (hipStream_t)stream), fn);
 }
 

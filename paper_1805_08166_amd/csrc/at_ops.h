@@ -139,8 +139,9 @@ struct OrthoArgs {
     void* out;
     int otype;
     int64_t obatch, ldo;
+    bool fp16_products;
 };
-int64_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, int otype);
+int64_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, bool fp16_products);
 hipError_t launch_ortho(const OrthoArgs& a, void* workspace, hipStream_t stream);
 
 }  // namespace at

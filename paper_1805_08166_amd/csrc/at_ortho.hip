@@ -4,21 +4,24 @@
 //   each step:  A = X X^T,  B = b A + c A A,  X <- a X + B X
 //
 // The three products of a step run on the matrix cores in fp16 with fp32
-// sums.  What keeps fp16 operands good enough:
-//   - X is carried as two fp16 words, hi + lo (22 bits): only a product's operand
-//     is rounded to hi, so a rounding error never becomes part of X.
+// sums, their operands as two fp16 words each, hi + lo (22 bits): three products a
+// product, fp32's accuracy.  Everything is scaled by powers of two, so that
+// fp16 keeps its precision: X by about sqrt(rows * cols) (unit entries at first, and
+// below 2^15 for singular values up to 8), A and B by 256.
+//
+// A caller may ask for products of the hi words alone (fp16_products).  What keeps
+// those good enough:
+//   - X is still carried as both words: only a product's operand is rounded
+//     to hi, so a rounding error never becomes part of X.
 //     Newton-Schulz multiplies what lies in the small singular directions by
 //     up to a^steps, and rounding X itself would put noise there.
-//   - Everything is scaled by powers of two, so that fp16 keeps its precision:
-//     X by about sqrt(rows * cols) (unit entries at first, and below 2^15 for
-//     singular values up to 8), A and B by 256.
 //   - In the last two steps, where X is nearly orthogonal and A nearly the
 //     identity, B is stored less (b + c) / 2 times the identity, which is added
 //     to a instead: B's rounding error and that of the operand it multiplies
 //     halve.  Earlier this would put the difference between X and hi into
-//     directions that later steps still enlarge.
-//   - fp32 outputs, and small matrices, use products of both words of both
-//     operands.
+//     directions that later steps still enlarge.  (Products of both words do
+//     not need it, and do the same.)
+//   - Few rows use both words all the same.
 // A and B are symmetric: only tiles on and below the diagonal are computed,
 // and each is written twice.
 #include <atomic>
@@ -570,7 +573,7 @@ struct Small {
     }
 };
 
-template <int N, bool SPLIT>
+template <int N>
 __device__ __forceinline__ void small_product(const half_t* P, const half_t* Q, int fi, int fj, float16v& acc) {
     using S = Small<N>;
     const int lane = threadIdx.x & 63, pi = fi + (lane & 31), qj = fj + (lane & 31);
@@ -582,17 +585,14 @@ __device__ __forceinline__ void small_product(const half_t* P, const half_t* Q, 
         const half8 p = *reinterpret_cast<const half8*>(P + S::at(pi, c));
         const half8 q = *reinterpret_cast<const half8*>(Q + S::at(qj, c));
         acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p, q, acc, 0, 0, 0);
-        if (SPLIT) {
-            const half8 pl = *reinterpret_cast<const half8*>(P + S::MATRIX + S::at(pi, c));
-            const half8 ql = *reinterpret_cast<const half8*>(Q + S::MATRIX + S::at(qj, c));
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p, ql, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, q, acc, 0, 0, 0);
-        }
+        const half8 pl = *reinterpret_cast<const half8*>(P + S::MATRIX + S::at(pi, c));
+        const half8 ql = *reinterpret_cast<const half8*>(Q + S::MATRIX + S::at(qj, c));
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p, ql, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, q, acc, 0, 0, 0);
     }
 }
 
 // A fragment's words: rounded, and what that left.
-template <bool SPLIT>
 struct Words {
     half4 h[4], l[4];
     __device__ __forceinline__ explicit Words(const float16v& v) {
@@ -601,41 +601,41 @@ struct Words {
             half_t first, rest;
             split_words(v[e], first, rest);
             h[e >> 2][e & 3] = first;
-            if (SPLIT) l[e >> 2][e & 3] = rest;
+            l[e >> 2][e & 3] = rest;
         }
     }
 };
 // Transposed into LDS: element (i, j) to row j.
-template <int N, bool SPLIT>
-__device__ __forceinline__ void small_put_t(half_t* to, int fi, int fj, const Words<SPLIT>& w) {
+template <int N>
+__device__ __forceinline__ void small_put_t(half_t* to, int fi, int fj, const Words& w) {
     using S = Small<N>;
     const int lane = threadIdx.x & 63, j = fj + (lane & 31);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const int at = S::at(j, fi + g * 8 + (lane >> 5) * 4);
         *reinterpret_cast<half4*>(to + at) = w.h[g];
-        if (SPLIT) *reinterpret_cast<half4*>(to + S::MATRIX + at) = w.l[g];
+        *reinterpret_cast<half4*>(to + S::MATRIX + at) = w.l[g];
     }
 }
-template <int N, bool SPLIT>
-__device__ __forceinline__ void small_put(half_t* to, int fi, int fj, const Words<SPLIT>& w) {
+template <int N>
+__device__ __forceinline__ void small_put(half_t* to, int fi, int fj, const Words& w) {
     using S = Small<N>;
     const int lane = threadIdx.x & 63, j = fj + (lane & 31);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const int at = S::at(fi + e / 4 * 8 + (lane >> 5) * 4 + e % 4, j);
         to[at] = w.h[e >> 2][e & 3];
-        if (SPLIT) to[S::MATRIX + at] = w.l[e >> 2][e & 3];
+        to[S::MATRIX + at] = w.l[e >> 2][e & 3];
     }
 }
 
-template <int DT, int N, bool SPLIT>
+template <int DT, int N>
 __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, int tall, float xs) {
     using S = Small<N>;
     using T = typename Elem<DT>::T;
-    extern __shared__ half_t s_words[];   // two operands of MATRIX words, twice that when split
+    extern __shared__ half_t s_words[];   // both words of two operands
     __shared__ double s_sum[S::THREADS / 64];
-    half_t *first = s_words, *second = s_words + S::MATRIX * (SPLIT ? 2 : 1);
+    half_t *first = s_words, *second = s_words + S::MATRIX * 2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int fi = wave / S::FRAGS * 32, fj = wave % S::FRAGS * 32, j = fj + (lane & 31);
     const T* x = static_cast<const T*>(a.x) + blockIdx.x * a.xbatch;
@@ -655,21 +655,20 @@ __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, 
     for (int e = 0; e < 16; ++e) X[e] *= f;
     for (int step = 0; step < a.steps; ++step) {
         const float shift = step + 2 >= a.steps ? 0.5f * (a.b + a.c) : 0.0f;
-        const Words<SPLIT> x_words(X);
-        small_put<N, SPLIT>(first, fi, fj, x_words);
+        const Words x_words(X);
+        small_put<N>(first, fi, fj, x_words);
         __syncthreads();
-        small_product<N, SPLIT>(first, first, fi, fj, A);
+        small_product<N>(first, first, fi, fj, A);
 #pragma unroll
         for (int e = 0; e < 16; ++e) A[e] *= A_SCALE / (xs * xs);
-        const Words<SPLIT> a_words(A);
-        small_put_t<N, SPLIT>(second, fi, fj, a_words);   // A is its transpose
+        const Words a_words(A);
+        small_put_t<N>(second, fi, fj, a_words);   // A is its transpose
         __syncthreads();
-        small_product<N, SPLIT>(second, second, fi, fj, acc);
+        small_product<N>(second, second, fi, fj, acc);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             // A as its operands hold it
-            float t = (float)a_words.h[e >> 2][e & 3];
-            if (SPLIT) t += (float)a_words.l[e >> 2][e & 3];
+            const float t = (float)a_words.h[e >> 2][e & 3] + (float)a_words.l[e >> 2][e & 3];
             acc[e] = __builtin_fmaf(t, a.b, acc[e] * (a.c / A_SCALE));
         }
         if (fi == fj && shift != 0.0f) {
@@ -677,11 +676,11 @@ __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, 
             for (int e = 0; e < 16; ++e)
                 if (e / 4 * 8 + (lane >> 5) * 4 + e % 4 == (lane & 31)) acc[e] -= shift * A_SCALE;
         }
-        small_put_t<N, SPLIT>(first, fi, fj, Words<SPLIT>(acc));
+        small_put_t<N>(first, fi, fj, Words(acc));
         __syncthreads();   // everyone has read A
-        small_put_t<N, SPLIT>(second, fi, fj, x_words);
+        small_put_t<N>(second, fi, fj, x_words);
         __syncthreads();
-        small_product<N, SPLIT>(first, second, fi, fj, acc);
+        small_product<N>(first, second, fi, fj, acc);
 #pragma unroll
         for (int e = 0; e < 16; ++e) X[e] = __builtin_fmaf(X[e], a.a + shift, acc[e] * (1.0f / A_SCALE));
         __syncthreads();   // everyone has read B and X
@@ -702,11 +701,10 @@ __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // fp16 operands are off by 2^-12 each; over many singular values that
-// averages out (s = 128: 1.2 times the error that bf16's rounding has alone; 64:
-// 1.4; 16: up to 2.2), so few rows take split products, at three times the
-// matrix instructions, which small matrices do not wait for.  Larger ones do: us,
-// split and not, 8 x 128 x 128 61 and 22, 2 x 1024 x 4096 938 and 355.
-constexpr int64_t SPLIT_MAX = 64;
+// averages out (s = 128: 1.2 times the error that bf16's rounding has alone; 70:
+// 1.5; 16: up to 2.2), so few rows take split products even where fp16 ones are
+// asked for.  us, split and not, 2 x 1024 x 4096 938 and 355.
+constexpr int64_t SPLIT_MAX = 128;
 // Every step in one workgroup, against tiles: us, 1 x 128 x 128 22 and 68,
 // 1 x 64 x 64 17 and 64, 512 x 128 x 128 56 and 270.
 constexpr int64_t SMALL_MAX = 128;
@@ -736,7 +734,7 @@ int64_t pieces_of(int64_t batch, const OrthoPlan& p) {
     if (n > PIECES_MAX) n = PIECES_MAX;
     return n > 1 && tiles - tiles / n >= PIECE_GAIN ? n : 1;
 }
-OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, int otype) {
+OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, bool fp16_products) {
     OrthoPlan p{};
     p.tall = rows > cols;
     p.s = p.tall ? cols : rows;
@@ -745,7 +743,7 @@ OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, int otype) {
     const int64_t unit = p.s >= 2048 ? 256 : p.s > 512 ? 128 : TILE;
     p.sp = round_up(p.s, unit);
     p.lp = round_up(p.l, unit);
-    p.split = otype == AT_F32 || p.s <= SPLIT_MAX;
+    p.split = !fp16_products || p.s <= SPLIT_MAX;
     p.small = p.l <= SMALL_MAX ? (p.l <= 64 ? 64 : 128) : 0;
     // the power of two next to sqrt(s l)
     double f = 1.0;
@@ -809,14 +807,14 @@ hipError_t gemm(const GemmArgs& a, int64_t batch, hipStream_t stream) {
     return gemm_as<Tile64, MODE, SPLIT>(a, batch, stream);
 }
 
-template <int DT, int N, bool SPLIT>
+template <int DT, int N>
 hipError_t launch_small(const OrthoArgs& o, const OrthoPlan& p, hipStream_t stream) {
     using S = Small<N>;
-    constexpr size_t lds = (size_t)S::MATRIX * 2 * (SPLIT ? 4 : 2);
+    constexpr size_t lds = (size_t)S::MATRIX * 2 * 4;
     static std::atomic<uint64_t> ready{0};
-    const hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_ortho_small<DT, N, SPLIT>), -1, lds, ready);
+    const hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_ortho_small<DT, N>), -1, lds, ready);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_ortho_small<DT, N, SPLIT>), dim3((unsigned)o.batch), dim3(S::THREADS), lds, stream, o, p.tall,
+    hipLaunchKernelGGL((k_ortho_small<DT, N>), dim3((unsigned)o.batch), dim3(S::THREADS), lds, stream, o, p.tall,
                        p.xs);
     return hipGetLastError();
 }
@@ -899,18 +897,16 @@ hipError_t run_steps(const OrthoArgs& o, const OrthoPlan& p, const OrthoBufs& b,
 
 }  // namespace
 
-int64_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, int otype) {
-    return plan_ortho(batch, rows, cols, otype).bytes;
+int64_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, bool fp16_products) {
+    return plan_ortho(batch, rows, cols, fp16_products).bytes;
 }
 
 hipError_t launch_ortho(const OrthoArgs& o, void* workspace, hipStream_t stream) {
-    const OrthoPlan p = plan_ortho(o.batch, o.rows, o.cols, o.otype);
+    const OrthoPlan p = plan_ortho(o.batch, o.rows, o.cols, o.fp16_products);
     if (p.small)
         return with_type(o.xtype, [&](auto dt) {
             constexpr int DT = decltype(dt)::value;
-            if (p.small == 64)
-                return p.split ? launch_small<DT, 64, true>(o, p, stream) : launch_small<DT, 64, false>(o, p, stream);
-            return p.split ? launch_small<DT, 128, true>(o, p, stream) : launch_small<DT, 128, false>(o, p, stream);
+            return p.small == 64 ? launch_small<DT, 64>(o, p, stream) : launch_small<DT, 128>(o, p, stream);
         });
     char* ws = static_cast<char*>(workspace);
     OrthoBufs b{};

@@ -132,3 +132,16 @@ def test_binding_checks(P):
         P.at_orthogonalize(w, o)
     with pytest.raises(ValueError, match="device"):
         P.at_orthogonalize(w, w)
+
+
+def test_fp16_products_flag(P):
+    """The flag goes with an output type, of the same ones, and needs less workspace."""
+    for base in (F32, BF16):
+        assert ortho(P, rows=0, x=None, out=None, otype=base | P.AT_FP16_PRODUCTS) == 0
+        assert ortho(P, steps=0, otype=base | P.AT_FP16_PRODUCTS) == INVALID
+    assert ortho(P, otype=F16 | P.AT_FP16_PRODUCTS) == UNSUPPORTED
+    assert ortho(P, otype=32) == UNSUPPORTED
+    for base in (F32, BF16):
+        whole = P.at_orthogonalize_workspace(2, 700, 900, base)
+        assert whole == P.at_orthogonalize_workspace(2, 700, 900, F32) > 2 * 700 * 900 * 12
+        assert P.at_orthogonalize_workspace(2, 700, 900, base | P.AT_FP16_PRODUCTS) < whole
