@@ -7,8 +7,10 @@
 //
 // One pass over the logits: each lane keeps the running maximum m of its x,
 // s = sum 2^y and u = sum 2^y y with y = (x - m) scale log2(e), all in fp32;
-// a new maximum rescales s and u.  Subtracting before scaling keeps rows of
-// the type's lowest value finite.  Each wave keeps its best k values sorted
+// a new maximum rescales s and u.  Subtracting before scaling makes y at most 0
+// and 0 at the maximum, whatever the size of x: s is at least 1 and finite for rows
+// of the type's lowest value and of any mask's, and nothing of m's rounding is
+// in it.  Each wave keeps its best k values sorted
 // over its lanes and looks at a batch again only when one of its values beats
 // the k-th.
 #include "at_ops.h"
@@ -240,21 +242,11 @@ struct Walk {
         for (int e = 3; e + 1 < VEC; e += 2) top = max3(top, v[e], v[e + 1]);
         if (VEC % 2 == 0) top = max3(top, top, v[VEC - 1]);
         if (top > st.m) stat_rescale(st, top, c);
-        const float mc = st.m * c;
-        if (__ballot(!(fabsf(mc) < 1e30f)) == 0) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float y = __builtin_fmaf(v[e], c, -mc), p = exp2_fast(y);
-                st.s += p;
-                st.u = __builtin_fmaf(p, bounded(y), st.u);
-            }
-        } else {   // some lane has seen nothing but a mask's lowest value, whose product overflows
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float y = (v[e] - st.m) * c, p = exp2_fast(y);
-                st.s += p;
-                st.u = __builtin_fmaf(p, bounded(y), st.u);
-            }
+        for (int e = 0; e < VEC; ++e) {
+            const float y = (v[e] - st.m) * c, p = exp2_fast(y);
+            st.s += p;
+            st.u = __builtin_fmaf(p, bounded(y), st.u);
         }
         if (!TOP) return;
         // Batches come in ascending columns, so that a value no better than the
