@@ -58,6 +58,11 @@ __device__ __forceinline__ uint32_t lane_before(uint32_t x) {
     return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x138, 0xf, 0xf, false);   // wave_shr 1
 }
 
+// scale log2(e), which is finite: 0 times infinity would make the maximum's weight
+// NaN.  Where it would not be, only values within 2^-120 of the maximum have a weight that
+// the bound changes.
+__device__ __forceinline__ float exponent_scale(float scale) { return fminf(scale * LOG2E, -LOWEST); }
+
 // Running softmax sums.  y below -1000 weighs nothing; the bound keeps
 // 0 * -inf out of u.  A NaN y is lost here, but s has it.
 struct Stat {
@@ -369,7 +374,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs_wave(LogprobsArgs a) {
     using T = typename Elem<DT>::T;
     const int64_t row = (int64_t)blockIdx.x * LP_WAVES + (threadIdx.x >> 6);
     if (row >= a.n) return;
-    const float c = a.scale * LOG2E;
+    const float c = exponent_scale(a.scale);
     const int64_t width = row_width(a.valid, row, a.vocab);
     const Given g = given_of<T>(a, row, width);
     Stat st = stat_empty();
@@ -415,7 +420,7 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs(LogprobsArgs a, int seg
     using T = typename Elem<DT>::T;
     const int64_t row = blockIdx.x / segments;
     const int seg = (int)(blockIdx.x - row * segments);
-    const float c = a.scale * LOG2E;
+    const float c = exponent_scale(a.scale);
     const int64_t width = row_width(a.valid, row, a.vocab);
     const int64_t c0 = seg * span, c1 = c0 + span < width ? c0 + span : width;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -449,7 +454,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_logprobs_join(LogprobsArgs a, 
     using T = typename Elem<DT>::T;
     constexpr int WAVES = JOIN_THREADS / 64;
     const int64_t row = blockIdx.x;
-    const float c = a.scale * LOG2E;
+    const float c = exponent_scale(a.scale);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     Given g{};
     if (threadIdx.x == 0) g = given_of<T>(a, row, row_width(a.valid, row, a.vocab));

@@ -91,3 +91,27 @@ def test_forward(P, n, vocab, dt, mask, scale):
     assert torch.equal(idx.cpu().long(), w_idx)
     close(top, w_top, b + 4 * U * (w_top.abs() + 2 * ls.abs()[:, None]), "alternatives' log probabilities")
     assert bool((logp.cpu().double() <= b).all()) and bool((top.cpu().double() <= b).all())
+
+
+@pytest.mark.parametrize("vocab", [40, 5003])
+def test_largest_scale(P, vocab):
+    """A scale whose product with log2(e) is past fp32's range: the largest value, twice
+    in row 1, has all the probability."""
+    import torch
+    scale = 3e38
+    x = -torch.rand(3, vocab, generator=torch.Generator().manual_seed(2)) - 0.125
+    x[:, 7] = 0.0
+    x[1, vocab - 2] = 0.0
+    x[2] *= 0.5
+    t = torch.tensor([7, 7, 9], device=DEV)
+    new = lambda *s: torch.full(s, 9.0, device=DEV)  # noqa: E731
+    logp, H, lse, top = new(3), new(3), new(3), new(3, 2)
+    idx = torch.empty(3, 2, dtype=torch.int32, device=DEV)
+    P.at_logprobs(x.to(DEV), t, logp, H, lse, top, idx, scale=scale)
+    two, second = math.log(2.0), x[0].topk(2).indices[1]
+    want = torch.tensor([0.0, -two, float(x[2, 9]) * scale])
+    assert torch.allclose(logp.cpu(), want, rtol=1e-6, atol=1e-6)
+    assert torch.allclose(H.cpu(), torch.tensor([0.0, two, 0.0]), atol=1e-6)
+    assert torch.allclose(lse.cpu(), torch.tensor([0.0, two, 0.0]), atol=1e-6)
+    assert idx[0].tolist() == [7, int(second)] and idx[1].tolist() == [7, vocab - 2]
+    assert torch.allclose(top[:2].cpu(), torch.tensor([[0.0, float(x[0, second]) * scale], [-two, -two]]), rtol=1e-6, atol=1e-6)
