@@ -515,10 +515,12 @@ at_status at_logprobs(const void* logits, int type, int64_t ld, int64_t n, int64
 /* Gradient of at_logprobs: with g = dlogp[i] and h = dentropy[i],
  *   dlogits[i, j] = round(scale * (g * (1[j = t] - p_j) - h * p_j * (log p_j + entropy[i])))
  * and 0 in ruled-out columns, columns from valid[i] on and rows with nothing in
- * them or with an lse below -1e30 (nothing but a mask's lowest value).  g counts
- * as 0 for a row without a token or whose token is ruled out.  lse, entropy: the forward call's (device [n] float; entropy may be
- * NULL without dentropy); dlogp, dentropy: device [n] float, or NULL for zero.
- * dlogits: device [n][vocab] of the logits' type, rows ldd apart. */
+ * them.  g counts as 0 for a row without a token or whose token is ruled out.
+ * It is that of logp and entropy: lse and the alternatives pass nothing back.
+ * lse, entropy: the forward call's (device [n] float; entropy may be NULL without
+ * dentropy).  Rows with |lse| above 1024, whose fp32 value no longer holds the
+ * row's log sum, are read again for it, several times slower for long rows.
+ * dlogp, dentropy: device [n] float, or NULL for zero.  dlogits: device [n][vocab] of the logits' type, rows ldd apart. */
 at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, int64_t vocab, const int32_t* valid,
                            const void* tokens, int itype, float scale, const float* lse, const float* entropy,
                            const float* dlogp, const float* dentropy, void* dlogits, int64_t ldd, at_stream_t stream);
