@@ -505,6 +505,20 @@ int segments_of(int64_t n, int64_t vocab) {
     return (int)s;
 }
 
+// The call on at most `most` rows from `row` on.
+LogprobsArgs rows_from(LogprobsArgs a, int64_t row, int64_t most) {
+    a.logits = moved(a.logits, row * a.ld, elem_size(a.type));
+    a.valid = moved(a.valid, row);
+    a.tokens = moved(a.tokens, row, a.wide ? 8 : 4);
+    a.logp = moved(a.logp, row);
+    a.entropy = moved(a.entropy, row);
+    a.lse = moved(a.lse, row);
+    a.top_logp = moved(a.top_logp, row * a.k);
+    a.top_idx = moved(a.top_idx, row * a.k);
+    a.n = a.n - row < most ? a.n - row : most;
+    return a;
+}
+
 // --------------------------------------------------------------------------
 // Gradient
 // --------------------------------------------------------------------------
@@ -632,9 +646,14 @@ hipError_t launch_logprobs(const LogprobsArgs& a, void* workspace, hipStream_t s
             constexpr bool TOP = decltype(top)::value;
             const dim3 block(LP_THREADS);
             if (segments == 0) {
-                hipLaunchKernelGGL((k_logprobs_wave<DT, TOP>), dim3((unsigned)((a.n + LP_WAVES - 1) / LP_WAVES)), block, 0,
-                                   stream, a);
-                return hipGetLastError();
+                for (int64_t row = 0; row < a.n; row += GROUPS_MAX * LP_WAVES) {
+                    const LogprobsArgs p = rows_from(a, row, GROUPS_MAX * LP_WAVES);
+                    hipLaunchKernelGGL((k_logprobs_wave<DT, TOP>), dim3((unsigned)((p.n + LP_WAVES - 1) / LP_WAVES)), block, 0,
+                                       stream, p);
+                    const hipError_t e = hipGetLastError();
+                    if (e != hipSuccess) return e;
+                }
+                return hipSuccess;
             }
             constexpr int64_t VEC = 16 / sizeof(typename Elem<DT>::T);
             int64_t span = (a.vocab + segments - 1) / segments;

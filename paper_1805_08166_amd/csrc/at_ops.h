@@ -70,6 +70,20 @@ hipError_t with_type(int dt, F&& f) {
     }
 }
 
+// A launch holds fewer than 2^32 threads: longer calls are cut into launches of so
+// many workgroups of 256 at most.
+constexpr int64_t GROUPS_MAX = (int64_t)1 << 23;
+
+// A pointer to element `by` of an array of elements of `size` bytes; no array stays none.
+template <class T>
+T* moved(T* p, int64_t by, int64_t size) {
+    return p ? reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(p) + (uintptr_t)(by * size)) : p;
+}
+template <class T>
+T* moved(T* p, int64_t by) {
+    return moved(p, by, sizeof(T));
+}
+
 struct EmbedArgs {
     const void* weight;
     int wtype;

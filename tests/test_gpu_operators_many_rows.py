@@ -1,0 +1,63 @@
+"""Calls of more rows than one launch holds threads for (2^32, at 4 to 256 threads
+a row): every row is worked on, those on both sides of a cut among them."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def P():
+    import torch
+    torch.cuda.set_device(0)
+    import paper_1805_08166_amd
+    return paper_1805_08166_amd
+
+
+@pytest.fixture(autouse=True)
+def memory():
+    """The tensors here are large: none stays behind."""
+    import torch
+    yield
+    torch.cuda.empty_cache()
+
+
+def room(gib):
+    import torch
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip(f"needs {gib} GiB of device memory")
+
+
+def rows_to_look_at(n, cuts, count, gen):
+    """Rows around every cut, the ends, and some in between."""
+    import torch
+    near = [c + d for c in cuts for d in (-2, -1, 0, 1)] + [0, 1, n - 2, n - 1]
+    some = torch.randint(0, n, (count,), generator=gen)
+    return torch.unique(torch.cat([torch.tensor([r for r in near if 0 <= r < n]), some])).to(DEV)
+
+
+def test_log_probabilities(P):
+    """2^26 + 5 rows of three values, a wave each."""
+    import torch
+    room(8)
+    n, vocab, k = (1 << 26) + 5, 3, 2
+    print(f"[gpu-rows] log probabilities {n} x {vocab}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(n, vocab, generator=gen, device=DEV)
+    tokens = torch.randint(0, vocab, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    valid = torch.randint(1, vocab + 1, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    logp, H, lse = (torch.full((n,), 9.0, device=DEV) for _ in range(3))
+    top, idx = torch.full((n, k), 9.0, device=DEV), torch.full((n, k), 7, dtype=torch.int32, device=DEV)
+    P.at_logprobs(x, tokens, logp, H, lse, top, idx, valid=valid)
+    for lo in range(0, n, 1 << 24):     # every row, in 32 bits
+        s = slice(lo, lo + (1 << 24))
+        z = x[s].masked_fill(torch.arange(vocab, device=DEV) >= valid[s, None], -torch.inf)
+        lp = torch.log_softmax(z, 1)
+        want = torch.gather(lp, 1, tokens[s, None].long())[:, 0]
+        assert torch.allclose(logp[s], want, rtol=1e-5, atol=1e-5)
+        assert torch.allclose(lse[s], torch.logsumexp(z, 1), rtol=1e-5, atol=1e-5)
+        assert torch.allclose(H[s], -(lp.exp() * lp).nan_to_num().sum(1), rtol=1e-5, atol=1e-5)
+        best = z.argmax(1)
+        assert torch.equal(idx[s, 0].long(), best)
+        assert torch.allclose(top[s, 0], torch.gather(lp, 1, best[:, None])[:, 0], rtol=1e-5, atol=1e-5)
+        assert torch.equal(idx[s, 1] < 0, valid[s] < 2)
