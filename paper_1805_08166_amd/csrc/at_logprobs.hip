@@ -631,6 +631,20 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs_grad(LogprobsGradArgs a
     }
 }
 
+// The call on at most `most` rows from `row` on.
+LogprobsGradArgs rows_from(LogprobsGradArgs a, int64_t row, int64_t most) {
+    a.logits = moved(a.logits, row * a.ld, elem_size(a.type));
+    a.valid = moved(a.valid, row);
+    a.tokens = moved(a.tokens, row, a.wide ? 8 : 4);
+    a.lse = moved(a.lse, row);
+    a.entropy = moved(a.entropy, row);
+    a.dlogp = moved(a.dlogp, row);
+    a.dentropy = moved(a.dentropy, row);
+    a.dlogits = moved(a.dlogits, row * a.ldd, elem_size(a.type));
+    a.n = a.n - row < most ? a.n - row : most;
+    return a;
+}
+
 }  // namespace
 
 int64_t logprobs_workspace(int64_t n, int64_t vocab, int k) {
@@ -679,10 +693,15 @@ hipError_t launch_logprobs_grad(const LogprobsGradArgs& a, hipStream_t stream) {
         int txs = 3;
         while (txs < 8 && ((int64_t)1 << txs) < packs) ++txs;
         const int64_t per = (int64_t)1 << txs, segments = (packs + per - 1) / per;
-        const int64_t groups = (a.n + (LP_THREADS >> txs) - 1) / (LP_THREADS >> txs);
-        hipLaunchKernelGGL((k_logprobs_grad<DT>), dim3((unsigned)(groups * segments)), dim3(LP_THREADS), 0, stream, a, txs,
-                           (int)segments);
-        return hipGetLastError();
+        const int64_t rows = LP_THREADS >> txs, most = GROUPS_MAX / segments * rows;   // of a workgroup, of a launch
+        for (int64_t row = 0; row < a.n; row += most) {
+            const LogprobsGradArgs p = rows_from(a, row, most);
+            hipLaunchKernelGGL((k_logprobs_grad<DT>), dim3((unsigned)((p.n + rows - 1) / rows * segments)), dim3(LP_THREADS), 0,
+                               stream, p, txs, (int)segments);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     });
 }
 

@@ -164,7 +164,7 @@ at_status at_logprobs_grad(const void* logits, int type, int64_t ld, int64_t n, 
         !aligned(tokens, itype == AT_I64 ? 8 : 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(dlogp, 4) ||
         !aligned(dentropy, 4))
         return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
-    // 2048 values of a row a workgroup at least, and no more workgroups than a grid holds
+    // gradients past any memory, whose workgroups (2048 values of a row each at least) are past 2^31
     if ((vocab + 2047) / 2048 * n > SIZE_MAX_31) return refuse(AT_E_UNSUPPORTED, fn, "too many values for one call");
     const LogprobsGradArgs a{logits, type, ld,    n,       vocab,    valid,   tokens, itype, scale,
                              lse,    entropy, dlogp, dentropy, dlogits, ldd};

@@ -61,3 +61,45 @@ def test_log_probabilities(P):
         assert torch.equal(idx[s, 0].long(), best)
         assert torch.allclose(top[s, 0], torch.gather(lp, 1, best[:, None])[:, 0], rtol=1e-5, atol=1e-5)
         assert torch.equal(idx[s, 1] < 0, valid[s] < 2)
+
+
+def test_log_probabilities_gradient(P):
+    """2^29 + 37 rows of one value, 32 a workgroup.  They are given an lse of 0, so that p is
+    e^x and the gradient g (1 - e^x), or 0 without a token."""
+    import torch
+    room(24)
+    n = (1 << 29) + 37
+    print(f"[gpu-rows] gradient {n} x 1", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.empty(n, 1, dtype=torch.float16, device=DEV).uniform_(-2.0, 1.0, generator=gen)
+    g = torch.empty(n, device=DEV).uniform_(0.5, 2.0, generator=gen)
+    tokens = torch.randint(-1, 1, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    lse = torch.zeros(n, device=DEV)
+    d = torch.full((n, 1), 9.0, dtype=torch.float16, device=DEV)
+    P.at_logprobs_grad(x, tokens, lse, None, g, d)
+    for lo in range(0, n, 1 << 26):     # every row; the result's rounding is 2^-11
+        s = slice(lo, lo + (1 << 26))
+        want = torch.where(tokens[s] >= 0, g[s] * (1.0 - x[s, 0].float().exp()), torch.zeros_like(g[s]))
+        assert torch.allclose(d[s, 0].float(), want, rtol=1e-3, atol=1e-5)
+
+
+def test_log_probabilities_gradient_of_long_rows(P):
+    """Rows of several workgroups in more than one launch: 16500 rows of 2^22 + 9 columns, 513
+    workgroups each, 2^23 a launch."""
+    import torch
+    room(150)
+    n, vocab = 16500, (1 << 22) + 9
+    print(f"[gpu-rows] gradient {n} x {vocab}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    row = torch.randn(vocab, generator=gen, device=DEV).half()
+    x = row.expand(n, vocab)            # one row, n times
+    tokens = torch.randint(0, vocab, (n,), generator=gen, device=DEV)
+    lse = torch.logsumexp(row.float(), 0).expand(n).contiguous()
+    g = torch.arange(1, n + 1, device=DEV, dtype=torch.float32) * 2.0
+    d = torch.empty(n, vocab, dtype=torch.float16, device=DEV)
+    P.at_logprobs_grad(x, tokens, lse, None, g, d)
+    p = (row.float() - lse[0]).exp()
+    for r in rows_to_look_at(n, [(1 << 23) // 513], 20, torch.Generator().manual_seed(4)).tolist():
+        want = -float(g[r]) * p
+        want[tokens[r]] += float(g[r])
+        assert torch.allclose(d[r].float(), want, rtol=1e-3, atol=2.0 ** -23), r
