@@ -664,12 +664,20 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t stream) {
             // (65536 x 2048 bf16 92 us for 100; 16384 x 2048 22 for 21)
             const bool many = a.n > (int64_t)ty * 32768;
             const int64_t per = (int64_t)ty * (many ? 4 : 1);
-            const dim3 grid((unsigned)((a.n + per - 1) / per));
-            if (many)
-                hipLaunchKernelGGL((k_embed<WT, OT, 4>), grid, dim3(EMB_THREADS), 0, stream, a, txs);
-            else
-                hipLaunchKernelGGL((k_embed<WT, OT, 1>), grid, dim3(EMB_THREADS), 0, stream, a, txs);
-            return hipGetLastError();
+            for (int64_t row = 0; row < a.n; row += per * GROUPS_MAX) {
+                EmbedArgs p = a;
+                p.tokens = moved(a.tokens, row, a.wide ? 8 : 4);
+                p.out = moved(a.out, row * a.ldo, elem_size(OT));
+                p.n = a.n - row < per * GROUPS_MAX ? a.n - row : per * GROUPS_MAX;
+                const dim3 grid((unsigned)((p.n + per - 1) / per));
+                if (many)
+                    hipLaunchKernelGGL((k_embed<WT, OT, 4>), grid, dim3(EMB_THREADS), 0, stream, p, txs);
+                else
+                    hipLaunchKernelGGL((k_embed<WT, OT, 1>), grid, dim3(EMB_THREADS), 0, stream, p, txs);
+                const hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
+            return hipSuccess;
         });
     });
 }

@@ -103,3 +103,21 @@ def test_log_probabilities_gradient_of_long_rows(P):
         want = -float(g[r]) * p
         want[tokens[r]] += float(g[r])
         assert torch.allclose(d[r].float(), want, rtol=1e-3, atol=2.0 ** -23), r
+
+
+def test_embed(P):
+    """2^26 + 9 rows of 520, a workgroup each with four rows a lane: the calls' last rows are in
+    the third launch."""
+    import torch
+    room(80)
+    n, vocab, dim = (1 << 26) + 9, 1000, 520
+    print(f"[gpu-rows] lookup {n} x {dim}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    w = torch.randn(vocab, dim, generator=gen, device=DEV)
+    tokens = torch.randint(-1, vocab, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    out = torch.full((n, dim), 9.0, dtype=torch.bfloat16, device=DEV)
+    P.at_embed(w, tokens, out, scale=0.5)
+    rows = rows_to_look_at(n, [k << 25 for k in (1, 2)] + [1 << 24], 4000, torch.Generator().manual_seed(6))
+    t = tokens[rows].long()
+    want = torch.where((t >= 0)[:, None], w[t.clamp(min=0)] * 0.5, torch.zeros(1, device=DEV)).to(torch.bfloat16)
+    assert torch.equal(out[rows], want)
