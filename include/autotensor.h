@@ -483,7 +483,8 @@ at_status at_embed(const void* weight, int wtype, int64_t ldw, int64_t vocab, in
  * sum is added to what dweight holds, in fp32, and other rows are untouched.
  * dout: device [n][dim] dtype, rows ldd apart; dweight: device [vocab][dim]
  * gtype, rows ldg apart.  The tokens are sorted by value, stably, in the workspace
- * (at_embed_grad_workspace bytes). */
+ * (at_embed_grad_workspace bytes).  AT_E_UNSUPPORTED for sizes as above, and from
+ * about 2^41 gradients on (n rows that repeat one, ldd 0). */
 at_status at_embed_grad_workspace(int64_t n, int64_t vocab, int64_t dim, int64_t* bytes);
 at_status at_embed_grad(const void* dout, int dtype, int64_t ldd, const void* tokens, int itype, int64_t n, float scale,
                         int accumulate, void* dweight, int gtype, int64_t ldg, int64_t vocab, int64_t dim,

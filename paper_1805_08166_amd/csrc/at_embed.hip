@@ -688,6 +688,11 @@ int64_t embed_grad_workspace(int64_t n, int64_t dim) {
     return a > b ? a : b;
 }
 
+int64_t embed_grad_groups(int64_t n, int64_t dim, int dtype) {
+    const GradPlan p = plan_grad(n, dim, elem_size(dtype));
+    return (int64_t)p.groups * p.ytiles;
+}
+
 hipError_t launch_embed_grad(const EmbedGradArgs& g, void* workspace, hipStream_t stream) {
     const GradPlan p = plan_grad(g.n, g.dim, elem_size(g.dtype));
     char* ws = static_cast<char*>(workspace);

@@ -115,6 +115,9 @@ at_status at_embed_grad(const void* dout, int dtype, int64_t ldd, const void* to
     if (!dweight || (n > 0 && (!dout || !tokens))) return refuse(AT_E_INVALID, fn, "NULL buffer");
     if (!aligned_t(dout, dtype) || !aligned_t(dweight, gtype) || !aligned(tokens, itype == AT_I64 ? 8 : 4))
         return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
+    // a launch holds fewer than 2^32 threads; more takes 2^41 gradients, one row many times over
+    if (embed_grad_groups(n, dim, dtype) >= (int64_t)1 << 24)
+        return refuse(AT_E_UNSUPPORTED, fn, "more than 2^41 gradients in one call");
     st = workspace_args(fn, workspace, workspace_bytes, embed_grad_workspace(n, dim));
     if (st != AT_OK) return st;
     const EmbedGradArgs a{dout, dtype, ldd, tokens, itype, n, scale, accumulate != 0, dweight, gtype, ldg, vocab, dim};

@@ -112,6 +112,7 @@ struct EmbedGradArgs {
     int64_t ldg, vocab, dim;
 };
 int64_t embed_grad_workspace(int64_t n, int64_t dim);
+int64_t embed_grad_groups(int64_t n, int64_t dim, int dtype);   // workgroups of 256 of its largest launch
 hipError_t launch_embed_grad(const EmbedGradArgs& a, void* workspace, hipStream_t stream);
 
 struct LogprobsArgs {

@@ -145,3 +145,12 @@ def test_fp16_products_flag(P):
         whole = P.at_orthogonalize_workspace(2, 700, 900, base)
         assert whole == P.at_orthogonalize_workspace(2, 700, 900, F32) > 2 * 700 * 900 * 12
         assert P.at_orthogonalize_workspace(2, 700, 900, base | P.AT_FP16_PRODUCTS) < whole
+
+
+def test_embed_grad_past_a_launch(P):
+    """2^30 tokens of one row, repeated, of 8192 columns: 2^24 workgroups of 256 threads are
+    more than a launch holds.  One column tile fewer is not."""
+    many = dict(ldd=0, n=1 << 30, vocab=10, dtype=BF16, wb=1 << 42)
+    assert embed_grad(P, dim=8192, ldg=8192, **many) == UNSUPPORTED
+    assert "at_embed_grad" in P.lib().at_last_error().decode()
+    assert embed_grad(P, dim=8192 - 512, ldg=8192, ws=None, **many) == INVALID    # its workspace is looked at
