@@ -80,6 +80,13 @@ __device__ __forceinline__ double block_sum(double v, double* scratch) {
     return v;
 }
 
+// xs / (|G| + eps), 0 for a matrix of zeros whatever eps is.  64 bits, as is its
+// product with G: with eps 0 the quotient of the smallest or largest norms is not one
+// that fp32 holds.
+__device__ __forceinline__ double normaliser(double norm, float eps, float xs) {
+    return norm == 0.0 ? 0.0 : (double)xs / (norm + (double)eps);
+}
+
 // Partial sums of squares, in 64 bits: squares of what fp32 holds overflow it.
 template <int DT>
 __global__ __launch_bounds__(NORM_THREADS) void k_norm(OrthoArgs a, double* part) {
@@ -122,7 +129,7 @@ __global__ __launch_bounds__(256) void k_layout(OrthoArgs a, OrthoBufs b, int sp
     __shared__ double s_sum[4];
     static_assert(NORM_BLOCKS == 256, "one partial sum a thread");
     const double norm = sqrt(block_sum<256>(b.part[blockIdx.z * NORM_BLOCKS + threadIdx.x], s_sum));
-    const float f = (float)((double)xs / (norm + (double)a.eps));
+    const double f = normaliser(norm, a.eps, xs);
     const T* x = static_cast<const T*>(a.x) + blockIdx.z * a.xbatch;
     const int line = threadIdx.x >> 2, seg = (threadIdx.x & 3) * 16;
     const int64_t r0 = (int64_t)blockIdx.y * TILE, c0 = (int64_t)blockIdx.x * TILE, row = r0 + line, col = c0 + seg;
@@ -139,7 +146,7 @@ __global__ __launch_bounds__(256) void k_layout(OrthoArgs a, OrthoBufs b, int sp
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         half_t h, l;
-        split_words(v[e] * f, h, l);
+        split_words((float)((double)v[e] * f), h, l);
         w[0][e >> 3][e & 7] = h;
         w[1][e >> 3][e & 7] = l;
         s_w[0][seg + e][line] = h;
@@ -650,9 +657,9 @@ __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, 
         sum = __builtin_fma((double)X[e], (double)X[e], sum);
     }
     const double norm = sqrt(block_sum<S::THREADS>(sum, s_sum));
-    const float f = (float)((double)xs / (norm + (double)a.eps));
+    const double f = normaliser(norm, a.eps, xs);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) X[e] *= f;
+    for (int e = 0; e < 16; ++e) X[e] = (float)((double)X[e] * f);
     for (int step = 0; step < a.steps; ++step) {
         const float shift = step + 2 >= a.steps ? 0.5f * (a.b + a.c) : 0.0f;
         const Words x_words(X);

@@ -271,3 +271,24 @@ def test_both_words_of_x_belong_together(P, batch, rows, cols):
             err = (out[k].cpu().double() - want).abs()
             tol = (steps + 1) * (2.0 ** -21 * want.abs() + a ** steps * 2.0 ** -24 / unit)
             assert bool((err <= tol).all()), (steps, k, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("rows,cols", [(50, 60), (100, 90), (270, 260)])
+def test_no_eps(P, rows, cols):
+    """With eps 0 a matrix of zeros still gives zeros, and one of the smallest or the
+    largest values that fp32 holds is scaled without loss."""
+    import torch
+    gen = torch.Generator().manual_seed(7)
+    g = torch.randn(3, rows, cols, generator=gen)
+    g[0] = 0.0
+    g[1] *= 1e-42
+    g[2] = g[2] / g[2].abs().max() * 3e38
+    for ot in (torch.float32, torch.bfloat16):
+        out = torch.full((3, rows, cols), 9.0, dtype=ot, device=DEV)
+        P.at_orthogonalize(g.to(DEV), out, eps=0.0)
+        out = out.cpu()
+        assert bool((out[0] == 0).all())
+        for k in (1, 2):
+            want = reference(g[k], 5, eps=0.0)
+            err = float((out[k].double() - want).norm() / want.norm())
+            assert err < (1e-4 if ot == torch.float32 else 3e-3 + 2.0 ** -8), (k, err)
