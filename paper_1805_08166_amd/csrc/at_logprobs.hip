@@ -77,12 +77,6 @@ __device__ __forceinline__ void stat_rescale(Stat& a, float m, float c) {
     a.s = f * a.s;
     a.m = m;
 }
-__device__ __forceinline__ Stat stat_join(Stat a, Stat b, float c) {
-    const float m = fmaxf(a.m, b.m);
-    stat_rescale(a, m, c);
-    stat_rescale(b, m, c);
-    return Stat{m, a.s + b.s, a.u + b.u};
-}
 template <int O>
 __device__ __forceinline__ float wave_max(float x) {
     x = fmaxf(x, lane_xor<O>(x));

@@ -266,13 +266,12 @@ __device__ __forceinline__ void wait_moves() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// One tile shape: WR x WC waves, each FR x FC fragments of 32 x 32, times WK
-// that share out a staged tile's depth and add up at the end; STAGES staged
+// One tile shape: WR x WC waves, each FR x FC fragments of 32 x 32; STAGES staged
 // tiles in LDS.
-template <int WR_, int WC_, int WK_, int FR_, int FC_, int STAGES_>
+template <int WR_, int WC_, int FR_, int FC_, int STAGES_>
 struct Shape {
-    static constexpr int WR = WR_, WC = WC_, WK = WK_, FR = FR_, FC = FC_, STAGES = STAGES_;
-    static constexpr int WAVES = WR * WC * WK, THREADS = WAVES * 64;
+    static constexpr int WR = WR_, WC = WC_, FR = FR_, FC = FC_, STAGES = STAGES_;
+    static constexpr int WAVES = WR * WC, THREADS = WAVES * 64;
     static constexpr int ROWS = WR * FR * 32, COLS = WC * FC * 32;
     static constexpr int MOVES = (ROWS + COLS) / 8 / WAVES;   // of a wave and stage
     static constexpr int LDS = STAGES * (ROWS + COLS) * BK * 2;
@@ -330,11 +329,10 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
     int bi, bj, z;
     tile_of<MODE == GRAM || MODE == POLY>(a, z, bi, bj);
     const int i0 = bi * ROWS, j0 = bj * COLS;
-    const int wk = wave / (S::WR * S::WC), wq = wave % (S::WR * S::WC);
-    const int wr = wq / S::WC * FR * 32, wc = wq % S::WC * FC * 32;
+    const int wr = wave / S::WC * FR * 32, wc = wave % S::WC * FC * 32;
     const int steps = a.depth / BK;
     int pass = 0, ks = 0, total = steps * (SPLIT ? 3 : 1);   // of the tile staged next; tiles in all
-    constexpr bool CUT = MODE == GRAM && FR == 1 && FC == 1 && S::WK == 1;
+    constexpr bool CUT = MODE == GRAM && FR == 1 && FC == 1;
     float4v* sums = nullptr;   // of this lane, in the first piece or its own
     if (CUT && a.phase != WHOLE) {
         const int piece = a.phase == PIECES ? blockIdx.y : 0;
@@ -400,12 +398,12 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
     // ahead of the products that use them, across tiles too: before the last of a
     // tile's products the wave sees to it that the next tile has landed and that
     // everyone has read this one, whose LDS the tile STAGES ahead then takes.
-    constexpr int KK = BK / 16 / S::WK;
+    constexpr int KK = BK / 16;
     static_assert(KK % 2 == 0, "fragments alternate between two sets of registers");
     half8 p[2][FR], q[2][FC];
     auto fragments = [&](int buf, int kk) {
         const half_t *s_p = s_tiles + buf * (ROWS + COLS) * BK, *s_q = s_p + ROWS * BK;
-        const int chunk = (wk * KK + kk) * 2 + (lane >> 5);
+        const int chunk = kk * 2 + (lane >> 5);
 #pragma unroll
         for (int r = 0; r < FR; ++r) {
             const int row = wr + r * 32 + (lane & 31);
@@ -467,34 +465,10 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
         return;
     }
     __syncthreads();   // the tiles' LDS is free
-    float* all = reinterpret_cast<float*>(s_tiles);
-    if (S::WK > 1) {
-        // sums of the waves along the depth, in order, in wave 0 of them
-        constexpr int PER = FR * FC * 16 * 64;
-#pragma unroll
-        for (int r = 0; r < FR; ++r)
-#pragma unroll
-            for (int c = 0; c < FC; ++c)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (wk) all[((wk - 1) * S::WR * S::WC + wq) * PER + ((r * FC + c) * 16 + e) * 64 + lane] = acc[r][c][e];
-        __syncthreads();
-        if (wk) return;
-#pragma unroll
-        for (int r = 0; r < FR; ++r)
-#pragma unroll
-            for (int c = 0; c < FC; ++c)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-#pragma unroll
-                    for (int k = 0; k < S::WK - 1; ++k)
-                        acc[r][c][e] += all[(k * S::WR * S::WC + wq) * PER + ((r * FC + c) * 16 + e) * 64 + lane];
-        all += (S::WK - 1) * S::WR * S::WC * PER;
-    }
     // A lane holds column j = lane & 31 of C and, in groups of four, rows 8 g +
     // 4 (lane >> 5) + 0..3 of each fragment.  Through LDS it gets eight values of
     // one row of C transposed, then of C: four lanes move 64 bytes of a row.
-    float* buf = all + wq * FRAG_FLOATS;
+    float* buf = reinterpret_cast<float*>(s_tiles) + wave * FRAG_FLOATS;
     const int64_t zc = z * a.cbatch;
     const int seg = (lane & 3) * 8, line = lane >> 2;
     constexpr bool BOTH = SPLIT || MODE == UPDATE || MODE == FINAL;   // words of S
@@ -784,9 +758,9 @@ OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, bool fp16_produc
 // these kernels wait for.  us a call, the rule against 64 x 64 always and, third,
 // 128 x 128 at most: 2 x 1024 x 4096 355, 414; 2048 x 8192 946, 1110, 977;
 // 4096 x 4096 1944, 2348, 2044.
-using Tile64 = Shape<2, 2, 1, 1, 1, 3>;
-using Tile128 = Shape<2, 4, 1, 2, 1, 2>;
-using Tile256 = Shape<2, 4, 1, 4, 2, 2>;
+using Tile64 = Shape<2, 2, 1, 1, 3>;
+using Tile128 = Shape<2, 4, 2, 1, 2>;
+using Tile256 = Shape<2, 4, 4, 2, 2>;
 
 template <class S, int MODE, bool SPLIT>
 hipError_t gemm_as(GemmArgs a, int64_t batch, hipStream_t stream) {
