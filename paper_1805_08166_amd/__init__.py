@@ -509,7 +509,9 @@ def entries(t) -> np.ndarray:
 # any row stride (a last stride of 1); vectors are contiguous.  Outputs are
 # the caller's; a workspace may be given as a uint8 tensor (the *_workspace
 # functions say how many bytes), else one is taken from torch's allocator on the
-# call's stream.
+# call's stream.  Gradients are calls of their own: nothing is recorded for
+# autograd, which is told that the outputs changed, so that it refuses to use
+# what they overwrote.
 # --------------------------------------------------------------------------
 AT_F32, AT_BF16, AT_F16 = 0, 1, 2
 AT_I32, AT_I64 = 0, 1
@@ -530,6 +532,7 @@ class _Torch:
         # the current stream's handle, without the object around it where torch has that
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self.written = torch.autograd.graph.increment_version
 
 
 _torch_parts = None
@@ -595,15 +598,15 @@ def _one_device(*tensors) -> int:
     return d
 
 
-def _call(func, device: int, stream, args, workspace=None, need: int = 0):
+def _call(func, device: int, stream, args, outs, workspace=None, need: int = 0):
     """Calls the library on `device`, with `stream` or the device's current one
-    as the last argument; where the call takes a workspace (need >= 0, the bytes),
+    as the last argument; outs: the tensors that it writes; where the call takes a workspace (need >= 0, the bytes),
     its pointer and size come before the stream."""
     T = _T()
     torch = T.torch
     if torch.cuda.current_device() != device:
         with torch.cuda.device(device):
-            return _call(func, device, stream, args, workspace, need)
+            return _call(func, device, stream, args, outs, workspace, need)
     if need >= 0:
         if workspace is None:
             if not need:
@@ -620,6 +623,7 @@ def _call(func, device: int, stream, args, workspace=None, need: int = 0):
     st = getattr(_lib, func)(*args, T.stream(device) if stream is None else stream.cuda_stream)
     if st:
         _check(func, st)
+    T.written(outs)
 
 
 @functools.lru_cache(maxsize=256)
@@ -638,7 +642,7 @@ def at_embed(weight, tokens, out, scale: float = 1.0, stream=None):
     vocab, dim = weight.shape
     op, ot, lo = _rows(out, "out", n, dim)
     _call("at_embed", _one_device(weight, tokens, out), stream,
-          (wp, wt, lw, vocab, dim, tp, ti, n, scale, op, ot, lo), need=-1)
+          (wp, wt, lw, vocab, dim, tp, ti, n, scale, op, ot, lo), out, need=-1)
 
 
 def at_embed_grad_workspace(n: int, vocab: int, dim: int) -> int:
@@ -654,7 +658,7 @@ def at_embed_grad(dout, tokens, dweight, scale: float = 1.0, accumulate: bool = 
     vocab, dim = dweight.shape
     dp, dt, ld = _rows(dout, "dout", n, dim)
     _call("at_embed_grad", _one_device(dout, tokens, dweight), stream,
-          (dp, dt, ld, tp, ti, n, scale, 1 if accumulate else 0, gp, gt, lg, vocab, dim), workspace,
+          (dp, dt, ld, tp, ti, n, scale, 1 if accumulate else 0, gp, gt, lg, vocab, dim), dweight, workspace,
           _bytes("at_embed_grad_workspace", n, vocab, dim))
 
 
@@ -683,7 +687,9 @@ def at_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_logp
     _call("at_logprobs", _one_device(logits, tokens, logp, entropy, lse, top_logp, top_idx, valid), stream,
           (xp, xt, ld, n, vocab, _vec(valid, n, T.i32, "valid"), tp, ti, scale, k, _vec(logp, n, T.f32, "logp"),
            _vec(entropy, n, T.f32, "entropy"), _vec(lse, n, T.f32, "lse"), _vec(top_logp, n * k, T.f32, "top_logp"),
-           _vec(top_idx, n * k, T.i32, "top_idx")), workspace, _bytes("at_logprobs_workspace", n, vocab, k))
+           _vec(top_idx, n * k, T.i32, "top_idx")),
+          [t for t in (logp, entropy, lse, top_logp, top_idx) if t is not None], workspace,
+          _bytes("at_logprobs_workspace", n, vocab, k))
 
 
 def at_logprobs_grad(logits, tokens, lse, entropy, dlogp, dlogits, dentropy=None, valid=None, scale: float = 1.0,
@@ -701,7 +707,7 @@ def at_logprobs_grad(logits, tokens, lse, entropy, dlogp, dlogits, dentropy=None
     _call("at_logprobs_grad", _one_device(logits, tokens, lse, entropy, dlogp, dlogits, dentropy, valid), stream,
           (xp, xt, ld, n, vocab, _vec(valid, n, T.i32, "valid"), tp, ti, scale, _vec(lse, n, T.f32, "lse"),
            _vec(entropy, n, T.f32, "entropy"), _vec(dlogp, n, T.f32, "dlogp"), _vec(dentropy, n, T.f32, "dentropy"), dp,
-           ldd), need=-1)
+           ldd), dlogits, need=-1)
 
 
 def _matrices(t, name):
@@ -738,5 +744,5 @@ def at_orthogonalize(x, out, steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e
     a, b, c = coef
     ot = _type(out, "out") | (AT_FP16_PRODUCTS if fp16_products else 0)
     _call("at_orthogonalize", _one_device(x, out), stream,
-          (xp, _type(x, "x"), xb, ldx, batch, rows, cols, steps, a, b, c, eps, scale, op, ot, ob, ldo), workspace,
+          (xp, _type(x, "x"), xb, ldx, batch, rows, cols, steps, a, b, c, eps, scale, op, ot, ob, ldo), out, workspace,
           _bytes("at_orthogonalize_workspace", batch, rows, cols, ot))
