@@ -538,10 +538,10 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
 // --------------------------------------------------------------------------
 // Small matrices: every step in one workgroup
 // --------------------------------------------------------------------------
-// Bound by latency: three dependent products a step with barriers between.
-// 8 x 128 x 128, 5 steps, 21 us with sixteen waves; with eight of 64 x 32 25 and
-// four of 64 x 64 34.
-// Both sides padded to N; one wave a fragment of 32 x 32.  X stays in
+// Three dependent products a step with barriers between, 3 us each at N = 128: every
+// wave reads both words of 32 rows of both operands, 512 KB a product (1.7 us at a
+// CU's 128 bytes a clock), for 24 matrix instructions (1.3 us for four waves a SIMD).
+// 8 x 128 x 128, 5 steps, 47 us.  Both sides padded to N; one wave a fragment of 32 x 32.  X stays in
 // registers, in fp32; LDS holds two operands at a time: X then B, and A then X
 // transposed.  Rows of N, 16-byte chunk c of row r in slot c ^ r (of 16) or c ^
 // r / 2 (of 8), so that 16 rows' chunks lie in different banks.
@@ -560,7 +560,7 @@ __device__ __forceinline__ void small_product(const half_t* P, const half_t* Q, 
     const int lane = threadIdx.x & 63, pi = fi + (lane & 31), qj = fj + (lane & 31);
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-#pragma unroll
+#pragma unroll 4
     for (int k = 0; k < N; k += 16) {
         const int c = k + (lane >> 5) * 8;
         const half8 p = *reinterpret_cast<const half8*>(P + S::at(pi, c));
@@ -636,8 +636,7 @@ __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, 
     for (int e = 0; e < 16; ++e) X[e] = (float)((double)X[e] * f);
     for (int step = 0; step < a.steps; ++step) {
         const float shift = step + 2 >= a.steps ? 0.5f * (a.b + a.c) : 0.0f;
-        const Words x_words(X);
-        small_put<N>(first, fi, fj, x_words);
+        small_put<N>(first, fi, fj, Words(X));
         __syncthreads();
         small_product<N>(first, first, fi, fj, A);
 #pragma unroll
@@ -659,7 +658,11 @@ __global__ __launch_bounds__(Small<N>::THREADS) void k_ortho_small(OrthoArgs a, 
         }
         small_put_t<N>(first, fi, fj, Words(acc));
         __syncthreads();   // everyone has read A
-        small_put_t<N>(second, fi, fj, x_words);
+        // X's words again: kept from above, they and more loads in flight than four of
+        // a product's went to scratch (280 bytes a lane at N = 128; 61 us for 47)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(X[e]));
+        small_put_t<N>(second, fi, fj, Words(X));
         __syncthreads();
         small_product<N>(first, second, fi, fj, acc);
 #pragma unroll
@@ -686,8 +689,8 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // 1.5; 16: up to 2.2), so few rows take split products even where fp16 ones are
 // asked for.  us, split and not, 2 x 1024 x 4096 938 and 355.
 constexpr int64_t SPLIT_MAX = 128;
-// Every step in one workgroup, against tiles: us, 1 x 128 x 128 22 and 68,
-// 1 x 64 x 64 17 and 64, 512 x 128 x 128 56 and 270.
+// Every step in one workgroup, against tiles: us, 1 x 128 x 128 46 and 85,
+// 64 x 128 x 128 47 and 107, 512 x 128 x 128 111 and 406, 512 x 16 x 100 88 and 206.
 constexpr int64_t SMALL_MAX = 128;
 
 struct OrthoPlan {
