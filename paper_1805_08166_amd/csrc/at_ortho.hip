@@ -786,7 +786,9 @@ hipError_t gemm(const GemmArgs& a, int64_t batch, hipStream_t stream) {
         const int64_t i = a.ti / r, j = a.tj / r;
         return batch * (MODE == GRAM || MODE == POLY ? i * (i + 1) / 2 : i * j) >= 256;
     };
-    if ((MODE == UPDATE || MODE == FINAL) && fills(256)) return gemm_as<Tile256, MODE, SPLIT>(a, batch, stream);
+    if constexpr (MODE == UPDATE || MODE == FINAL) {
+        if (fills(256)) return gemm_as<Tile256, MODE, SPLIT>(a, batch, stream);
+    }
     if (fills(128)) return gemm_as<Tile128, MODE, SPLIT>(a, batch, stream);
     return gemm_as<Tile64, MODE, SPLIT>(a, batch, stream);
 }
