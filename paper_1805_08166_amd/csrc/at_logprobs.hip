@@ -330,7 +330,7 @@ struct Given {
 };
 template <class T>
 __device__ __forceinline__ Given given_of(const LogprobsArgs& a, int64_t row, int64_t width) {
-    const int64_t t = a.tokens ? token_at(a.tokens, a.wide, row, (int64_t)1 << 62) : -1;
+    const int64_t t = a.tokens ? token_of(a.tokens, a.wide, row) : -1;
     const bool inside = t >= 0 && t < width;
     return Given{t >= 0, inside, inside ? (float)static_cast<const T*>(a.logits)[row * a.ld + t] : 0.0f};
 }

@@ -54,9 +54,13 @@ __device__ __forceinline__ T rounded(float v) {
     return (T)v;
 }
 
-// Token i of an int32 or int64 list; anything outside [0, limit) is -1.
+// Token i of an int32 or int64 list, as it is.
+__device__ __forceinline__ int64_t token_of(const void* tokens, int wide, int64_t i) {
+    return wide ? static_cast<const int64_t*>(tokens)[i] : (int64_t) static_cast<const int32_t*>(tokens)[i];
+}
+// The same; anything outside [0, limit) is -1.
 __device__ __forceinline__ int64_t token_at(const void* tokens, int wide, int64_t i, int64_t limit) {
-    const int64_t t = wide ? static_cast<const int64_t*>(tokens)[i] : (int64_t) static_cast<const int32_t*>(tokens)[i];
+    const int64_t t = token_of(tokens, wide, i);
     return t >= 0 && t < limit ? t : -1;
 }
 

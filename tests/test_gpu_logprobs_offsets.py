@@ -115,3 +115,14 @@ def test_largest_scale(P, vocab):
     assert torch.allclose(lse.cpu(), torch.tensor([0.0, two, 0.0]), atol=1e-6)
     assert idx[0].tolist() == [7, int(second)] and idx[1].tolist() == [7, vocab - 2]
     assert torch.allclose(top[:2].cpu(), torch.tensor([[0.0, float(x[0, second]) * scale], [-two, -two]]), rtol=1e-6, atol=1e-6)
+
+
+@pytest.mark.parametrize("vocab", [40, 5003])
+def test_tokens_far_past_the_row(P, vocab):
+    """64-bit tokens past every column are ruled out, however large; negative ones are none."""
+    import torch
+    x = torch.randn(5, vocab, generator=torch.Generator().manual_seed(3)).to(DEV)
+    t = torch.tensor([vocab, 1 << 61, 1 << 62, (1 << 63) - 1, -(1 << 63)], device=DEV)
+    logp = torch.full((5,), 9.0, device=DEV)
+    P.at_logprobs(x, t, logp)
+    assert logp.tolist() == [-INF, -INF, -INF, -INF, 0.0]
