@@ -534,18 +534,21 @@ enum { AT_FP16_PRODUCTS = 16 };
  *   out = round(scale * X)
  * (on the transpose when rows > cols).  x: device [batch][rows][cols] xtype,
  * matrices xbatch and rows ldx elements apart; out: device, bf16 or fp32
- * (otype), obatch and ldo apart; out may be x, of the same type.  The products
- * run on the matrix cores, each operand as two fp16 words (22 bits), with fp32
- * sums: before they are rounded to otype, results are as far off as fp32 products
- * would leave them (1e-6 to 3e-6 of their norm with the default steps).  otype | AT_FP16_PRODUCTS asks for products of the first words alone
- * where the shorter side is above 128, in about a third of the time for large
- * matrices: bf16 results are then within 2.4e-3 of their norm, of which bf16's
- * own rounding is 1.7e-3.
+ * (otype), obatch and ldo apart; out may be x, of the same type.
+ * The products run on the matrix cores, each operand as two fp16 words (22
+ * bits), with fp32 sums: before they are rounded to otype, results are as far
+ * off as fp32 products would leave them (1e-6 to 3e-6 of their norm with the
+ * default steps; where the norm of x is below a hundredth of eps, so that X starts
+ * small, eps / norm times 2.5e-8).  otype | AT_FP16_PRODUCTS asks for products of the first
+ * words alone where the shorter side is above 128, in about 0.4 of the time for
+ * large matrices: bf16 results are then within 2.4e-3 of their norm, of which
+ * bf16's own rounding is 1.7e-3.
  * The same call gives the same bits; a batch may sum in another order than its
  * matrices one by one.  A matrix of zeros gives zeros.  1 <= steps <= 64;
- * batch <= 65535, rows and cols <= 65536, AT_E_UNSUPPORTED beyond;
- * coefficients that let singular values grow past 8 overflow.  Workspace:
- * at_orthogonalize_workspace bytes. */
+ * batch <= 65535, rows and cols <= 65536, AT_E_UNSUPPORTED beyond.  Results
+ * overflow for coefficients that let a singular value s grow past 8 or |b s^2 +
+ * c s^4| past 255 (with the default ones from s = 3.5 on; they keep s below 1.3).
+ * Workspace: at_orthogonalize_workspace bytes. */
 at_status at_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int otype, int64_t* bytes);
 at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx, int64_t batch, int64_t rows,
                            int64_t cols, int steps, float a, float b, float c, float eps, float scale, void* out,

@@ -733,7 +733,7 @@ def at_orthogonalize(x, out, steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e
     cols]; float32, bfloat16 or float16), normalised first, into out (bfloat16
     or float32, the same shape), times scale.  Products have fp32's accuracy;
     fp16_products rounds their operands to fp16 where the shorter side is above
-    128: about a third of the time for large matrices, bf16 results within 2.4e-3
+    128: about 0.4 of the time for large matrices, bf16 results within 2.4e-3
     of their norm for 1.7e-3 (its workspace: otype | AT_FP16_PRODUCTS)."""
     if out.shape != x.shape:
         raise ValueError("out must have x's shape")

@@ -27,8 +27,8 @@ constexpr int EMB_THREADS = 256;
 // Lookup
 // --------------------------------------------------------------------------
 // 1 << txs lanes share a row, VEC elements each; R rows a lane in flight.  Bound by
-// memory: 65536 rows of 2048 bf16, from a table of 131072, 97 to 103 us, 4.9 TB/s
-// (a copy of that size reaches 5.3); 3584 rows of 128 fp32 2.9 us.
+// memory: 65536 rows of 2048 bf16, from a table of 131072, 97 to 104 us for 252 MiB read and
+// 256 written, 5.3 TB/s (a copy of that size reaches 5.3); 3584 rows of 128 fp32 3.0 us.
 template <int WT, int OT, int R>
 __global__ __launch_bounds__(EMB_THREADS) void k_embed(EmbedArgs a, int txs) {
     using TW = typename Elem<WT>::T;
@@ -81,8 +81,8 @@ constexpr int ONE_MAX = SORT_THREADS * ONE_ITEMS;
 // tokens 30 us for 35, 131000 39 for 42; 720896 75 for 71.
 constexpr int64_t SPREAD_MAX = 131072;
 constexpr int TILE_ITEMS = 4;
-// Up to so many tiles each sums up the histograms itself, a launch less a pass:
-// 176 tiles 71 us for 73 in all, 366 tiles 136 for 104.
+// Up to so many tiles each sums up the histograms itself, a launch less a pass: of
+// 35 tiles 39 us in all for 43, 176 70 for 73, 220 81 for 83, 318 as many, 367 139 for 138.
 constexpr int SCAN_TILES = 192;
 constexpr int SCAN_PARTS = 16;                            // threads a digit at most
 
@@ -660,8 +660,9 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t stream) {
             const int size = elem_size(WT) > elem_size(OT) ? elem_size(WT) : elem_size(OT), vec = 16 / size;
             const int txs = log2_at_least((a.dim + vec - 1) / vec, 0, 8);
             const int ty = EMB_THREADS >> txs;
-            // Four rows a lane where one would make more than 32768 workgroups
-            // (65536 x 2048 bf16 92 us for 100; 16384 x 2048 22 for 21)
+            // Four rows a lane where one would make more than 32768 workgroups: us,
+            // four and one, 2000000 x 128 bf16 154 and 173, 6000000 x 128 461 and 522,
+            // 65536 x 2048 100 and 99; below, 16384 x 2048 25 and 23, 30000 x 2048 44 and 41
             const bool many = a.n > (int64_t)ty * 32768;
             const int64_t per = (int64_t)ty * (many ? 4 : 1);
             for (int64_t row = 0; row < a.n; row += per * GROUPS_MAX) {

@@ -180,8 +180,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // One row segment [c0, c1) walked by `waves` waves of a workgroup, this one
 // the w-th: statistics a lane, best values a wave.  Bound by memory without
-// alternatives (4096 x 50048 bf16 77 us, 5.3 TB/s), by the vector unit's work
-// on them with (k 5 89 us, k 64 149).
+// alternatives (4096 x 50048 bf16 78 us, 5.3 TB/s); they add to that what their
+// insertions and merges take, which loads do not hide (k 5 88 us, k 64 150).
 template <class T, bool TOP>
 struct Walk {
     static constexpr int VEC = 16 / sizeof(T), SPAN = 64 * VEC;
@@ -578,7 +578,7 @@ __device__ __forceinline__ void far_row(const T* x, int64_t width, float c, int 
 // One pass: lse and the entropy are the forward call's, so that a column's
 // gradient takes its own logit alone.  A workgroup holds LP_THREADS >> txs rows,
 // 1 << txs lanes each, and for longer rows one of `segments` pieces of a row.  Bound by memory:
-// 8192 x 131072 bf16 730 to 780 us, 5.5 to 5.9 TB/s; 3584 x 220 fp32 4.4 us.
+// 8192 x 131072 bf16 710 to 780 us, 5.5 to 6.0 TB/s; 3584 x 220 fp32 4.8 us.
 template <int DT>
 __global__ __launch_bounds__(LP_THREADS) void k_logprobs_grad(LogprobsGradArgs a, int txs, int segments) {
     using T = typename Elem<DT>::T;

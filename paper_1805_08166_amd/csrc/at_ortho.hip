@@ -119,8 +119,8 @@ __global__ __launch_bounds__(NORM_THREADS) void k_norm(OrthoArgs a, double* part
 }
 
 // xs * G / (|G| + eps) and its transpose, zero padded: one 64 x 64 tile of G a
-// workgroup, sixteen values of a row a thread.  2 x 1024 x 4096 bf16 16 us (the
-// norm before it 6), 4.2 TB/s.
+// workgroup, sixteen values of a row a thread.  2 x 1024 x 4096 bf16 17 us (the
+// norm before it 6), 4.9 TB/s.
 template <int DT, bool SPLIT>
 __global__ __launch_bounds__(256) void k_layout(OrthoArgs a, OrthoBufs b, int sp, int lp, int tall, float xs) {
     using T = typename Elem<DT>::T;
@@ -318,9 +318,11 @@ __device__ __forceinline__ void tile_of(const GemmArgs& a, int& z, int& bi, int&
 
 // SPLIT: the product of (P + p)(Q + q)^T without p q^T, three passes over the
 // depth into the same sums: fp32 results to about 2^-22.
-// Bound by what a CU takes into LDS, 50 to 75 KB/us here.  us a step of
-// 2 x 1024 x 4096: A 30 (half its products, 0.30 PF/s), B 11, X 33 (0.52 PF/s);
-// X of 4096 x 4096, in 256 x 256 tiles, 131 (1.05 PF/s).
+// us a step of 2 x 1024 x 4096, split and not: A 84 and 29 (half its products: of
+// matrix instructions 0.32 PF/s), B 26 and 11, X 71 and 32 (0.7 and 0.53 PF/s).
+// Bound by latency in A and B (272 workgroups, one to a CU: one wave a SIMD, whose
+// matrix unit is busy 16 per cent of the time) and by the way into LDS in X (40 per
+// cent busy, two workgroups a CU).
 template <class S, int MODE, bool SPLIT>
 __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs a) {
     constexpr int ROWS = S::ROWS, COLS = S::COLS, FR = S::FR, FC = S::FC, STAGES = S::STAGES;
@@ -687,7 +689,8 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // fp16 operands are off by 2^-12 each; over many singular values that
 // averages out (s = 128: 1.2 times the error that bf16's rounding has alone; 70:
 // 1.5; 16: up to 2.2), so few rows take split products even where fp16 ones are
-// asked for.  us, split and not, 2 x 1024 x 4096 938 and 355.
+// asked for.  us a call, split and not: 2 x 1024 x 4096 880 and 340, 2 x 512 x 2048 244
+// and 142, 4096 x 4096 5330 and 1880.
 constexpr int64_t SPLIT_MAX = 128;
 // Every step in one workgroup, against tiles: us, 1 x 128 x 128 46 and 85,
 // 64 x 128 x 128 47 and 107, 512 x 128 x 128 111 and 406, 512 x 16 x 100 88 and 206.
@@ -707,9 +710,10 @@ int64_t triangle_of(int64_t n) { return n * (n + 1) / 2; }
 // Few tiles of A leave most CUs without one: their depth is then cut into pieces
 // of at least PIECE_TILES staged tiles, at most a workgroup for every CU, and joined by a
 // launch of its own (about 4 us) where that takes PIECE_GAIN tiles (0.36 us each) off
-// the longest.  us, cut and not: 1 x 16 x 4096 111 and 394; 5 x 64 x 2048 112 and 236;
-// 1 x 128 x 4096 100 and 155, fp32 133 and 419; 1 x 512 x 4096 148 and 201;
-// 1 x 32 x 512 87 and 98 (16 tiles off); 4 x 256 x 1024 103 and 99 (8 off).
+// the longest.  us, cut and not: 1 x 16 x 4096 115 and 383; 5 x 64 x 2048 115 and 228;
+// 1 x 128 x 4096 136 and 404; 1 x 512 x 4096 243 and 492, fp16 products 149 and 203;
+// 4 x 256 x 1024 149 and 192; 1 x 300 x 700 147 and 166; 1 x 32 x 512 94 and 99
+// (16 tiles off); 4 x 256 x 1024 with fp16 products, forced, 103 and 99 (8 off).
 constexpr int64_t PIECE_TILES = 8, PIECES_MAX = 16, PIECE_GAIN = 12;
 int64_t pieces_of(int64_t batch, const OrthoPlan& p) {
     const int64_t groups = batch * triangle_of(p.sp / TILE), tiles = p.lp / TILE * (p.split ? 3 : 1);
@@ -758,9 +762,9 @@ OrthoPlan plan_ortho(int64_t batch, int64_t rows, int64_t cols, bool fp16_produc
 
 // Tile shapes: the largest that divides both sides and makes a workgroup for
 // every CU.  A larger tile moves fewer bytes into LDS a product, which is what
-// these kernels wait for.  us a call, the rule against 64 x 64 always and, third,
-// 128 x 128 at most: 2 x 1024 x 4096 355, 414; 2048 x 8192 946, 1110, 977;
-// 4096 x 4096 1944, 2348, 2044.
+// these kernels wait for.  us a call, the rule, 64 x 64 always and 128 x 128 at most:
+// 2 x 1024 x 4096 881, 985, 883; 2048 x 8192 2450, 3020, 2610; 4096 x 4096 5330, 6790,
+// 5660; with fp16 products 337, 360, 337; 916, 1056, 934; 1878, 2230, 1951.
 using Tile64 = Shape<2, 2, 1, 1, 3>;
 using Tile128 = Shape<2, 4, 2, 1, 2>;
 using Tile256 = Shape<2, 4, 4, 2, 2>;
