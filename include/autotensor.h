@@ -555,6 +555,106 @@ at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx
                            int otype, int64_t obatch, int64_t ldo, void* workspace, int64_t workspace_bytes,
                            at_stream_t stream);
 
+/* --------------------------------------------------------------------------
+ * Operators that let such a model propose one token after another: keys and
+ * values kept in pages, attention over them, and changes to logits before
+ * at_logprobs.  The conventions above hold; tensors with heads have a distance
+ * between tokens and one between heads, in elements.  They serve: there are no
+ * gradients.
+ *
+ * at_paged says where the keys and values of a batch of sequences lie and which
+ * of a call's n tokens belong to which.  Sequence b's new tokens are
+ * starts[b] .. starts[b+1] - 1 of the call's, the last of its lengths[b]
+ * positions: token i has position p = lengths[b] - (starts[b+1] - i).  Position p
+ * lies in place p % page_size of page table[b][p / page_size].  starts goes up;
+ * a sequence may have no new tokens; tokens from starts[batch] on (and before
+ * starts[0]) belong to none, and what a call writes for tokens is left as it was for them.
+ * Whatever these arrays hold, nothing outside the caches and the table is touched: pages
+ * outside [0, pages) and positions past width * page_size or below 0 are not there.
+ * All pointers are device; k and v may be NULL where there are no pages.
+ * batch below 2^24, pages and page_size below 2^31, heads <= 65535, 1 <= dim <= 256.
+ * -------------------------------------------------------------------------- */
+typedef struct {
+    void* k;                           /* [pages][page_size][heads][dim] of `type`, by the distances below */
+    void* v;
+    int64_t k_page, k_token, k_head;   /* between pages, places of a page, heads */
+    int64_t v_page, v_token, v_head;
+    int64_t type;                      /* at_dtype, of the tokens' keys, values, queries and outputs too */
+    int64_t pages, page_size, heads, dim;
+    const int32_t* table;              /* [batch][width], rows table_ld apart */
+    int64_t table_ld, width;
+    const int32_t* starts;             /* [batch + 1] */
+    const int32_t* lengths;            /* [batch], with the new tokens */
+    int64_t batch;
+} at_paged;
+
+/* Appends the keys and values of new tokens to their pages, the keys turned by their
+ * position, and turns the same tokens' queries.  For each head x of a key or query
+ *   x <- x / sqrt(mean(x^2) + eps) * weight      (with k_weight or q_weight: device [dim] of the type)
+ *   (x_a, x_b) <- rot_scale * (x_a cos t - x_b sin t, x_b cos t + x_a sin t),  t = p * freqs[j]
+ * for the pairs j < rot / 2: elements (j, j + rot/2), or (2j, 2j+1) with
+ * interleaved; elements from rot on stay.  Angles are 64-bit, the rest fp32,
+ * rounded once.  Values are copied.
+ * k, v: device [n][heads][dim]; q, q_out: device [n][q_heads][dim], or q NULL
+ * for none; q_out may be q.  freqs: device [rot / 2] double, in radians a
+ * position (base, stretching and the like are in them).  A token whose position is not there
+ * is not stored; its query is turned all the same.  Two tokens of a call must not share a place of a
+ * page: where they do, it holds values of either.
+ * rot: even, 0 to dim. */
+at_status at_paged_append(const at_paged* cache, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                          int64_t v_token, int64_t v_head, int64_t n, const void* q, int64_t q_token, int64_t q_head,
+                          int64_t q_heads, void* q_out, int64_t o_token, int64_t o_head, const void* k_weight,
+                          const void* q_weight, float eps, const double* freqs, int64_t rot, int interleaved,
+                          float rot_scale, at_stream_t stream);
+
+/* Attention of new tokens over all that the cache holds of their sequences (the
+ * new tokens' own keys and values are in it already).  A token at position p sees
+ * positions j <= p, with window > 0 only j > p - window:
+ *   s_j = scale * q . k_j,  out = sum_j exp(s_j - lse) v_j,  lse = log sum_j exp(s_j)
+ * Query head h goes with cache head h / (q_heads / heads).  A token that sees
+ * nothing gets zeros, and -inf for lse.  NaN and infinities reach the tokens that
+ * see them, whose outputs are then not finite, and no others.
+ * q, out: device [n][q_heads][dim] of the cache's type; lse: device float
+ * [n][q_heads], or NULL.  scale must be positive and finite.  q_heads is a multiple of the
+ * cache's heads.
+ * Products of 16-bit types run on the matrix cores in that type with fp32 sums,
+ * for which the weights exp(s_j - max) are rounded to it; fp32 in fp32.
+ * Long sequences may be cut into pieces, joined in order: the same call gives the same bits, a
+ * batch may sum in another order than its sequences one by one.
+ * Workspace: at_paged_attention_workspace bytes (positions: width * page_size of the table). */
+at_status at_paged_attention_workspace(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads,
+                                       int64_t dim, int type, int64_t* bytes);
+at_status at_paged_attention(const at_paged* cache, const void* q, int64_t q_token, int64_t q_head, int64_t n,
+                             int64_t q_heads, float scale, int64_t window, void* out, int64_t o_token, int64_t o_head,
+                             float* lse, void* workspace, int64_t workspace_bytes, at_stream_t stream);
+
+/* Changes rows of logits by what their sequences hold, in this order, in fp32,
+ * rounded once:
+ *   x <- x > 0 ? x / repetition[i] : x * repetition[i]   for tokens of the row's past
+ *   x <- x - frequency[i] * c, then x - presence[i] if c > 0
+ *                                c: how often the token is in the past, its prompt left out
+ *   x <- x + bias[i][e]          for t = bias_tokens[i][e]; of several e for t the last counts
+ *   x <- -inf                    where bit t of row mask_rows[i] of mask is 0
+ * A logit of -inf stays so.  Logits that nothing applies to are copied bit for bit.
+ * The past of row i is past[i][0 .. lengths[i] - 1] (all past_len where
+ * lengths is NULL), the first prompt_lengths[i] of them (none where it is NULL) the prompt; lengths are clamped to
+ * what there is.  Tokens outside [0, vocab) are ignored, in the past and in the biases.
+ * logits: device [n][vocab] type, rows ld apart; out the same, ldo apart, and
+ * may be logits.  past: device [n][past_len] itype, rows ldp apart; bias_tokens
+ * of the same itype and bias (float): device [n][n_bias], rows bias_ld apart;
+ * repetition, frequency, presence: device [n] float, each of them NULL for none;
+ * mask: device int32 [mask_count][words], rows mask_ld apart, words = ceil(vocab / 32), bit t % 32 of word
+ * t / 32; mask_rows: device [n] int32, or NULL for row i of mask for row i;
+ * rows outside [0, mask_count) have no mask.  valid: device [n] int32, the columns
+ * that a row has (clamped to [0, vocab]; every column when NULL): others are neither read nor written.
+ * n, vocab, past_len and n_bias are below 2^31. */
+at_status at_adjust_logits(const void* logits, int type, int64_t ld, int64_t n, int64_t vocab, void* out, int64_t ldo,
+                           int itype, const void* past, int64_t ldp, int64_t past_len, const int32_t* lengths,
+                           const int32_t* prompt_lengths, const float* repetition, const float* frequency,
+                           const float* presence, const void* bias_tokens, const float* bias, int64_t n_bias,
+                           int64_t bias_ld, const int32_t* mask, int64_t mask_ld, int64_t mask_count,
+                           const int32_t* mask_rows, const int32_t* valid, at_stream_t stream);
+
 /* Thread-local description of the last non-OK status ("" if none). */
 const char* at_last_error(void);
 

@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 import numpy as np
 
@@ -40,6 +41,7 @@ EXPORTED = [
     "at_sa_kernel_times", "at_chains_set_path", "at_chains_last_path", "at_chains_last_plan", "at_select_batch", "at_select_batch_noalloc", "at_last_error",
     "at_embed", "at_embed_grad_workspace", "at_embed_grad", "at_logprobs_workspace", "at_logprobs",
     "at_logprobs_grad", "at_orthogonalize_workspace", "at_orthogonalize",
+    "at_paged_append", "at_paged_attention_workspace", "at_paged_attention", "at_adjust_logits",
 ]
 
 # at_sa_path
@@ -105,6 +107,12 @@ def _load():
         "at_orthogonalize_workspace": [i64, i64, i64, i32, vp],
         "at_orthogonalize": [vp, i32, i64, i64, i64, i64, i64, i32, f32, f32, f32, f32, f32, vp, i32, i64, i64, vp,
                              i64, vp],
+        "at_paged_append": [vp, vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, i64, vp, i64, i64, vp, vp, f32, vp, i64, i32,
+                            f32, vp],
+        "at_paged_attention_workspace": [i64, i64, i64, i64, i64, i64, i32, vp],
+        "at_paged_attention": [vp, vp, i64, i64, i64, i64, f32, i64, vp, i64, i64, vp, vp, i64, vp],
+        "at_adjust_logits": [vp, i32, i64, i64, i64, vp, i64, i32, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, i64, i64, vp,
+                             i64, i64, vp, vp, vp],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -746,3 +754,161 @@ def at_orthogonalize(x, out, steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e
     _call("at_orthogonalize", _one_device(x, out), stream,
           (xp, _type(x, "x"), xb, ldx, batch, rows, cols, steps, a, b, c, eps, scale, op, ot, ob, ldo), out, workspace,
           _bytes("at_orthogonalize_workspace", batch, rows, cols, ot))
+
+
+# --------------------------------------------------------------------------
+# Serving: keys and values in pages, attention over them, changes to logits.
+# Caches are [pages, page_size, heads, dim] with any strides but the last; a layout
+# with the heads outside the places of a page is its transposed view.
+# --------------------------------------------------------------------------
+_PAGED = struct.Struct("=19q")
+
+
+def _heads(t, name, n=None, heads=None, dim=None, of=None):
+    """(pointer, token stride, head stride) of a device tensor [n, heads, dim]."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    sh = t.shape
+    if len(sh) != 3 or (n is not None and sh[0] != n) or (heads is not None and sh[1] != heads) or (
+            dim is not None and sh[2] != dim):
+        raise ValueError(f"{name} must be [{'n' if n is None else n}, {'heads' if heads is None else heads}, "
+                         f"{'dim' if dim is None else dim}], got {list(sh)}")
+    if of is not None and t.dtype != of:
+        raise ValueError(f"{name} must have the cache's type {of}, got {t.dtype}")
+    st = t.stride()
+    if sh[2] > 1 and st[2] != 1:
+        raise ValueError(f"{name} must have contiguous heads")
+    return t.data_ptr(), st[0], st[1]
+
+
+def _paged(k_cache, v_cache, table, starts, lengths):
+    """The C side's at_paged of a cache and a batch."""
+    T = _T()
+    if not (k_cache.is_cuda and v_cache.is_cuda and table.is_cuda):
+        raise ValueError("the caches and the table must be device tensors")
+    sh = k_cache.shape
+    if len(sh) != 4 or v_cache.shape != sh or v_cache.dtype != k_cache.dtype:
+        raise ValueError("the caches must be [pages, page_size, heads, dim] of one shape and type")
+    ks, vs = k_cache.stride(), v_cache.stride()
+    if sh[3] > 1 and (ks[3] != 1 or vs[3] != 1):
+        raise ValueError("the caches must have contiguous heads")
+    if table.dim() != 2 or table.dtype != T.i32:
+        raise ValueError("table must be int32 [batch, width]")
+    batch, width = table.shape
+    if width > 1 and table.stride(1) != 1:
+        raise ValueError("table must have contiguous rows")
+    return _PAGED.pack(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                       _type(k_cache, "k_cache"), sh[0], sh[1], sh[2], sh[3], table.data_ptr(), table.stride(0), width,
+                       _vec(starts, batch + 1, T.i32, "starts"), _vec(lengths, batch, T.i32, "lengths"), batch)
+
+
+def at_paged_append(k, v, k_cache, v_cache, table, starts, lengths, q=None, q_out=None, freqs=None,
+                    interleaved: bool = False, rot_scale: float = 1.0, k_weight=None, q_weight=None, eps: float = 1e-6,
+                    stream=None):
+    """Puts the keys and values of new tokens into their pages and turns keys and
+    queries by position.  k, v: [n, heads, dim]; q, q_out: [n, q_heads, dim] or
+    None; k_cache, v_cache: [pages, page_size, heads, dim]; table: int32 [batch,
+    width], a sequence's pages in order; starts: int32 [batch + 1], where each
+    sequence's new tokens start; lengths: int32 [batch], its positions with
+    them.  freqs: float64 [rot / 2], radians a position, or None for no
+    turning; pairs are (j, j + rot / 2), or (2j, 2j + 1) with interleaved; a
+    turned pair is multiplied by rot_scale.  k_weight, q_weight: [dim], norm each head
+    first.  All of one type: float32, bfloat16 or float16."""
+    T = _T()
+    paged = _paged(k_cache, v_cache, table, starts, lengths)
+    of, (_, _, heads, dim) = k_cache.dtype, k_cache.shape
+    n = k.shape[0]
+    kp, kt, kh = _heads(k, "k", n, heads, dim, of)
+    vp, vt, vh = _heads(v, "v", n, heads, dim, of)
+    qp, qt, qh, q_heads, op, ot, oh = None, 0, 0, 0, None, 0, 0
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q needs q_out")
+        q_heads = q.shape[1]
+        qp, qt, qh = _heads(q, "q", n, None, dim, of)
+        op, ot, oh = _heads(q_out, "q_out", n, q_heads, dim, of)
+    rot = 2 * freqs.numel() if freqs is not None else 0
+    _call("at_paged_append", _one_device(k, v, k_cache, v_cache, table, starts, lengths, q, q_out, freqs, k_weight, q_weight),
+          stream, (paged, kp, kt, kh, vp, vt, vh, n, qp, qt, qh, q_heads, op, ot, oh, _vec(k_weight, dim, of, "k_weight"),
+                   _vec(q_weight, dim, of, "q_weight"), eps, _vec(freqs, rot // 2, T.torch.float64, "freqs"), rot,
+                   1 if interleaved else 0, rot_scale),
+          (k_cache, v_cache) if q is None else (k_cache, v_cache, q_out), need=-1)
+
+
+def at_paged_attention_workspace(n: int, batch: int, positions: int, q_heads: int, heads: int, dim: int,
+                                 type: int = AT_BF16) -> int:
+    return _bytes("at_paged_attention_workspace", n, batch, positions, q_heads, heads, dim, type)
+
+
+def at_paged_attention(q, k_cache, v_cache, table, starts, lengths, out, scale=None, window: int = 0, lse=None,
+                       workspace=None, stream=None):
+    """Attention of new tokens over the pages of their sequences, which hold their
+    own keys and values already: position p sees positions up to p, with window
+    the last `window` of them.  q, out: [n, q_heads, dim] of the caches' type;
+    scale: 1 / sqrt(dim) where None; lse: float32 [n, q_heads] or None.  The
+    caches, table, starts and lengths are those of at_paged_append."""
+    paged = _paged(k_cache, v_cache, table, starts, lengths)
+    of, (_, size, heads, dim) = k_cache.dtype, k_cache.shape
+    qp, qt, qh = _heads(q, "q", None, None, dim, of)
+    n, q_heads = q.shape[:2]
+    op, ot, oh = _heads(out, "out", n, q_heads, dim, of)
+    batch, width = table.shape
+    _call("at_paged_attention", _one_device(q, k_cache, v_cache, table, starts, lengths, out, lse), stream,
+          (paged, qp, qt, qh, n, q_heads, dim ** -0.5 if scale is None else scale, window, op, ot, oh,
+           _vec(lse, n * q_heads, _T().f32, "lse")), out if lse is None else (out, lse), workspace,
+          _bytes("at_paged_attention_workspace", n, batch, width * size, q_heads, heads, dim, _type(k_cache, "k_cache")))
+
+
+def at_adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None, repetition=None, presence=None,
+                     frequency=None, bias_tokens=None, bias=None, mask=None, mask_rows=None, valid=None, stream=None):
+    """Penalties for the tokens of each row's past, biases and masks on logits
+    [n, vocab], into out (which may be logits).  tokens: int32 or int64 [n,
+    past], of which a row has lengths[i] (all of them where None), the first
+    prompt_lengths[i] its prompt; repetition, presence, frequency: float32 [n];
+    bias_tokens (the type of tokens) and bias (float32): [n, biases]; mask:
+    int32 [masks, ceil(vocab / 32)], bit t of a row allows token t; mask_rows:
+    int32 [n], each row's mask (-1 for none), or None for mask i for row i;
+    valid: int32 [n], the columns that each row has."""
+    T = _T()
+    xp, xt, ld = _rows(logits, "logits")
+    n, vocab = logits.shape
+    op, ot, ldo = _rows(out, "out", n, vocab)
+    if ot != xt:
+        raise ValueError("out must have the logits' type")
+    ti, pp, ldp, past = AT_I32, None, 0, 0
+    if tokens is not None:
+        pp, ti, ldp, past = _list(tokens, "tokens", n)
+    bt, b, ldb, n_bias = None, None, 0, 0
+    if bias_tokens is not None:
+        bt, bti, ldb, n_bias = _list(bias_tokens, "bias_tokens", n)
+        if tokens is not None and bti != ti:
+            raise ValueError("bias_tokens must have the type of tokens")
+        ti = bti
+        if bias is None or bias.shape != bias_tokens.shape or bias.dtype != T.f32 or bias.stride() != bias_tokens.stride():
+            raise ValueError("bias must be float32, with the shape and strides of bias_tokens")
+        b = bias.data_ptr()
+    elif bias is not None:
+        raise ValueError("bias needs bias_tokens")
+    mp, ldm, masks = None, 0, 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.dtype != T.i32 or mask.shape[1] != (vocab + 31) // 32 or not mask.is_cuda or (
+                mask.shape[1] > 1 and mask.stride(1) != 1):
+            raise ValueError(f"mask must be an int32 device tensor [masks, {(vocab + 31) // 32}] with contiguous rows")
+        mp, ldm, masks = mask.data_ptr(), mask.stride(0), mask.shape[0]
+    _call("at_adjust_logits",
+          _one_device(logits, out, tokens, lengths, prompt_lengths, repetition, presence, frequency, bias_tokens, bias, mask,
+                      mask_rows, valid), stream,
+          (xp, xt, ld, n, vocab, op, ldo, ti, pp, ldp, past, _vec(lengths, n, T.i32, "lengths"),
+           _vec(prompt_lengths, n, T.i32, "prompt_lengths"), _vec(repetition, n, T.f32, "repetition"),
+           _vec(frequency, n, T.f32, "frequency"), _vec(presence, n, T.f32, "presence"), bt, b, n_bias, ldb, mp, ldm, masks,
+           _vec(mask_rows, n, T.i32, "mask_rows"), _vec(valid, n, T.i32, "valid")), out, need=-1)
+
+
+def _list(t, name, n):
+    """(pointer, token type, row stride, columns) of an int32 or int64 device tensor [n, columns]."""
+    ti = _T().itypes.get(t.dtype)
+    if ti is None:
+        raise ValueError(f"{name} must be int32 or int64, got {t.dtype}")
+    if not t.is_cuda or t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a device tensor [{n}, ...] with contiguous rows")
+    return t.data_ptr(), ti, t.stride(0), t.shape[1]

@@ -1,0 +1,706 @@
+// Attention of new tokens over a paged cache.
+//
+//   s_j = scale q . k_j  (position j at most the token's own, within the window),  p_j = exp(s_j - max)
+//   out = sum p_j v_j / sum p_j,  lse = max + log sum p_j
+//
+// in one pass over the keys with a running maximum and sum.  The query heads that
+// share a cache head and the tokens of a sequence are the rows of one
+// problem: row r is token r / G, head r % G.  A workgroup takes a tile of rows
+// and passes over their keys in tiles that it stages in LDS, two of them in
+// turn, 16 bytes a lane straight from the pages.  Each wave has 32 rows:
+//
+//   S^T = K Q^T     32 keys x 32 rows a matrix instruction; Q stays in registers
+//   O^T += V^T P^T  the lane that holds a row's S holds its P as the instruction
+//                   wants it: key order within the sum is free, so the keys that a
+//                   lane has are taken as they lie
+//
+// so that P never leaves registers, and a row's maximum and sum are a lane's own (its
+// keys lie in two lanes).  V^T comes from V's rows by LDS's transposing reads.
+// Waves share the tile's keys (ROW_WAVES: prompts) or split them (KEY_WAVES: few rows).
+//
+// Few tiles of rows over long sequences are cut along the keys: all sequences' key tiles are laid
+// out in a row and cut into pieces of equal length, which leave their sums in the
+// workspace for a joining launch that adds them in order.
+#include <algorithm>
+#include <atomic>
+
+#include "at_paged.h"
+
+namespace at {
+
+namespace {
+
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LN2 = 0.69314718055994530942f;
+
+// Element types: fragments of 16 bytes and their products.
+template <int DT>
+struct Mat;
+template <>
+struct Mat<AT_BF16> {
+    typedef __bf16 Frag __attribute__((ext_vector_type(8)));
+    // P is rounded to bf16 (its largest value is 1): half a step is 2^-9 of it, like that of the values it multiplies.
+    static constexpr float SHIFT = 0.0f;
+    static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mat<AT_F16> {
+    typedef _Float16 Frag __attribute__((ext_vector_type(8)));
+    // P times 2^14, so that fp16's smallest normal value is 2^-28 of a row's largest.
+    static constexpr float SHIFT = 14.0f;
+    static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mat<AT_F32> {
+    typedef float Frag __attribute__((ext_vector_type(4)));
+    static constexpr float SHIFT = 0.0f;
+    static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// How a call is laid out; the same for both kernels.
+struct Plan {
+    Divider size;        // of a page
+    int group;           // G, query heads of a cache head
+    int rows;            // of a tile
+    int keys;            // of a tile
+    int target;          // pieces a head that the keys are cut into, about; 0: whole sequences
+    int slots;           // pieces a head, at most
+    int direct;          // rows of the cache can be moved to LDS 16 aligned bytes at a time
+    float* sums;         // [slot][head][row][dim padded]
+    float* stats;        // [slot][head][row][2]: maximum and sum
+};
+constexpr int LEAST_TILES = 4;   // of a piece
+
+// What a sequence has to do: tiles of rows, and the key tiles [lo, hi) that any of them sees.
+struct Task {
+    int first, count, length;   // new tokens; positions in the cache
+    int64_t position;           // of the first new token
+    int row_tiles, lo, hi;
+};
+__device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int b) {
+    Task t;
+    const Span s = span_of(a.c.starts, b, (int)a.n);
+    t.first = s.first;
+    t.count = s.count;
+    const int64_t room = a.c.width * a.c.page_size, l = a.c.lengths[b];
+    t.position = l - s.count;
+    t.length = (int)(l < 0 ? 0 : l < room ? l : room);
+    t.row_tiles = (int)(((int64_t)s.count * p.group + p.rows - 1) / p.rows);
+    int64_t lo = a.window > 0 ? t.position - a.window + 1 : 0;
+    lo = lo < 0 ? 0 : lo < t.length ? lo : t.length;
+    t.lo = (int)(lo / p.keys);
+    t.hi = (t.length + p.keys - 1) / p.keys;
+    return t;
+}
+
+// Sum over a workgroup, in every thread.  Ends with all threads past their reads of scratch.
+template <int THREADS>
+__device__ __forceinline__ int64_t block_total(int64_t v, int64_t* scratch) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if (THREADS == 64) return v;
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+    for (int w = 0; w < THREADS / 64; ++w) v += scratch[w];
+    __syncthreads();
+    return v;
+}
+
+// Key tiles of a piece.  A sequence counts once for every tile of its rows.
+template <int THREADS>
+__device__ __forceinline__ int piece_tiles(const AttendArgs& a, const Plan& p, int64_t* scratch) {
+    if (p.target == 0) return 1 << 30;
+    int64_t work = 0;
+    for (int b = threadIdx.x; b < a.c.batch; b += THREADS) {
+        const Task t = task_of(a, p, b);
+        work += (int64_t)t.row_tiles * (t.hi - t.lo);
+    }
+    work = block_total<THREADS>(work, scratch);
+    const int64_t each = (work + p.target - 1) / p.target;
+    return (int)(each < LEAST_TILES ? LEAST_TILES : each < (1 << 30) ? each : 1 << 30);
+}
+__device__ __forceinline__ int pieces_of(const Task& t, int tiles) {
+    const int n = (t.hi - t.lo + tiles - 1) / tiles;
+    return n < 1 ? 1 : n;
+}
+
+template <int DT_, int DP_, int ROW_WAVES_, int KEY_WAVES_>
+struct Shape {
+    static constexpr int DT = DT_, DP = DP_;
+    static constexpr int ROW_WAVES = ROW_WAVES_, KEY_WAVES = KEY_WAVES_, WAVES = ROW_WAVES * KEY_WAVES;
+    static constexpr int THREADS = WAVES * 64;
+    static constexpr int SIZE = sizeof(typename Elem<DT>::T), VEC = 16 / SIZE;
+    static constexpr int CHUNKS = DP / VEC;            // of 16 bytes in a row
+    static constexpr int ROW = DP * SIZE;              // bytes
+    static constexpr int SUBS = KEY_WAVES > 1 || ROW > 512 ? 1 : 2;   // 32 keys of a wave and tile each
+    static constexpr int KEYS = KEY_WAVES * SUBS * 32;
+    static constexpr int ROWS = ROW_WAVES * 32;
+    static constexpr int TILE = KEYS * ROW;            // bytes of a tile of keys or values
+    static constexpr int MOVES = TILE / 1024 / WAVES;  // of a wave, a KB each
+    static constexpr int OUT_LD = DP + 4;
+    static constexpr int JOIN = KEY_WAVES > 1 ? WAVES * 32 * OUT_LD * 4 : 0;
+    static constexpr int LDS = 4 * TILE > JOIN ? 4 * TILE : JOIN;
+    static_assert(MOVES >= 1 && CHUNKS <= 64, "whole moves");
+};
+
+// Chunk c of row r lies in slot c ^ swizzle(r).  Keys: 32 lanes read one chunk of 32 rows.
+template <int CHUNKS>
+__device__ __forceinline__ int key_swizzle(int r) {
+    return CHUNKS >= 16 ? r & 15 : CHUNKS == 8 ? (r >> 1) & 7 : (r >> 2) & 3;
+}
+// Values: 16-bit ones are read as 64 bytes of four rows at once, fp32 as 128 bytes of rows r and r + 4.
+template <int CHUNKS, int SIZE>
+__device__ __forceinline__ int value_swizzle(int r) {
+    if (SIZE == 4) return CHUNKS >= 16 ? (r >> 2 & 1) << 3 : 0;
+    return CHUNKS >= 16 ? (r & 3) << 2 : CHUNKS == 8 ? (r >> 1 & 1) << 2 : 0;
+}
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+// Four rows of one column: lane i of 16 gives the address of four elements of row i / 4.
+__device__ __forceinline__ short4v read_transposed(const char* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) short4v*)(__attribute__((address_space(3))) char*)p);
+}
+
+template <class T>
+__device__ __forceinline__ bool is_finite(T v) {
+    return __builtin_isfinite((float)v);
+}
+
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host needs its launch stub only, and does not know all of the device's instructions
+    constexpr int DT = S::DT, DP = S::DP, RW = S::ROW_WAVES, KW = S::KEY_WAVES;
+    using T = typename Elem<DT>::T;
+    using M = Mat<DT>;
+    using Frag = typename M::Frag;
+    constexpr int VEC = S::VEC, SUBS = S::SUBS, KEYS = S::KEYS, CHUNKS = S::CHUNKS, DTILES = DP / 32;
+    extern __shared__ char s_tiles[];          // [2][keys, values][KEYS][DP]
+    __shared__ uint32_t s_gone[2][KEYS];       // whether a tile's row is not there
+    __shared__ int64_t s_scratch[S::WAVES];
+    __shared__ int s_place[2];
+    __shared__ float s_stats[S::WAVES][32][2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, mine = lane & 31;
+    const int rw = wave % RW, kw = wave / RW;
+    const int heads = (int)a.c.heads, head = blockIdx.x % heads, slot = blockIdx.x / heads;
+
+    // Which sequence, tile of rows and piece of keys.
+    const int tiles = piece_tiles<S::THREADS>(a, p, s_scratch);
+    {
+        if (threadIdx.x == 0) s_place[0] = -1;
+        const int batch = (int)a.c.batch, each = (batch + S::THREADS - 1) / S::THREADS;
+        const int b0 = threadIdx.x * each, b1 = b0 + each < batch ? b0 + each : batch;
+        int64_t here = 0;
+        for (int b = b0; b < b1; ++b) {
+            const Task t = task_of(a, p, b);
+            here += (int64_t)t.row_tiles * pieces_of(t, tiles);
+        }
+        int64_t upto = here;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t v = __shfl_up(upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 63) s_scratch[wave] = upto;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) upto += s_scratch[w];
+        int64_t rest = slot - (upto - here);
+        if (rest >= 0 && rest < here) {
+            for (int b = b0; b < b1; ++b) {
+                const Task t = task_of(a, p, b);
+                const int64_t n = (int64_t)t.row_tiles * pieces_of(t, tiles);
+                if (rest < n) {
+                    s_place[0] = b;
+                    s_place[1] = (int)rest;
+                    break;
+                }
+                rest -= n;
+            }
+        }
+        __syncthreads();
+    }
+    const int b = s_place[0];
+    if (b < 0) return;
+    const Task task = task_of(a, p, b);
+    const int pieces = pieces_of(task, tiles), piece = s_place[1] % pieces;
+    const int row_tile = task.row_tiles - 1 - s_place[1] / pieces;   // a prompt's longest first
+
+    // Rows of this workgroup, and the keys that they see.
+    const int G = p.group;
+    const int64_t row0 = (int64_t)row_tile * S::ROWS, all_rows = (int64_t)task.count * G;
+    const int rows = (int)(all_rows - row0 < S::ROWS ? all_rows - row0 : S::ROWS);
+    const int64_t first_pos = task.position + row0 / G, last_pos = task.position + (row0 + rows - 1) / G;
+    const int64_t window = a.window > 0 ? a.window : (int64_t)1 << 40;
+    int64_t lo = first_pos - window + 1, hi = last_pos + 1;   // positions [lo, hi)
+    lo = lo < 0 ? 0 : lo;
+    hi = hi < task.length ? hi : task.length;
+    int tile = (int)((lo < hi ? lo : 0) / KEYS), tile_end = (int)(hi > lo ? (hi + KEYS - 1) / KEYS : 0);
+    {
+        const int64_t from = (int64_t)task.lo + (int64_t)piece * tiles, to = from + tiles;
+        if (tile < from) tile = (int)from;
+        if (tile_end > to) tile_end = (int)to;
+    }
+
+    // Moves of a tile into LDS: this lane's row and chunk of each.
+    const int32_t* table = a.c.table + b * a.c.table_ld;
+    const T* k_head = static_cast<const T*>(a.c.k) + head * a.c.k_head;
+    const T* v_head = static_cast<const T*>(a.c.v) + head * a.c.v_head;
+    constexpr int MOVES = S::MOVES;
+    auto row_of = [&](int q) { return ((wave * MOVES + q) * 64 + lane) / CHUNKS; };
+    const int dim = (int)a.c.dim;
+    int ids[MOVES];   // pages of the next tile's rows, -1 where there is none
+    auto look_up = [&](int t) {
+#pragma unroll
+        for (int q = 0; q < MOVES; ++q) {
+            const int64_t pos = (int64_t)t * KEYS + row_of(q);
+            ids[q] = pos < hi ? table[divided((uint32_t)pos, p.size)] : -1;
+        }
+    };
+    auto stage = [&](int t, int buf) {
+        char* to_k = s_tiles + buf * 2 * S::TILE;
+        char* to_v = to_k + S::TILE;
+#pragma unroll
+        for (int q = 0; q < MOVES; ++q) {
+            const int row = row_of(q), at = (wave * MOVES + q) * 64 + lane, chunk = at % CHUNKS;
+            const int ck = (chunk ^ key_swizzle<CHUNKS>(row)) * VEC, cv = (chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * VEC;
+            const bool there = (uint32_t)ids[q] < (uint32_t)a.c.pages;
+            if (chunk == 0) s_gone[buf][row] = !there;
+            const uint32_t pos = (uint32_t)(t * (int64_t)KEYS + row);
+            const int64_t place = there ? pos - divided(pos, p.size) * p.size.d : 0, page = there ? ids[q] : 0;
+            const T* k = k_head + page * a.c.k_page + place * a.c.k_token;
+            const T* v = v_head + page * a.c.v_page + place * a.c.v_token;
+            if (p.direct) {
+                if (there) {
+                    // (the moves of lanes past dim are left out: zeros lie there)
+                    if (ck < dim) __builtin_amdgcn_global_load_lds(k + ck, to_k + (wave * MOVES + q) * 1024, 16, 0, 0);
+                    if (cv < dim) __builtin_amdgcn_global_load_lds(v + cv, to_v + (wave * MOVES + q) * 1024, 16, 0, 0);
+                } else {
+                    *reinterpret_cast<float4v*>(to_k + at * 16) = float4v{};
+                    *reinterpret_cast<float4v*>(to_v + at * 16) = float4v{};
+                }
+            } else {
+                auto read = [&](const T* x, int c) {
+                    Pack<T, VEC> w;
+                    if (there && c + VEC <= dim) return load_pack<T, VEC>(x + c);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) w.v[e] = there && c + e < dim ? x[c + e] : (T)0.0f;
+                    return w;
+                };
+                *reinterpret_cast<Pack<T, VEC>*>(to_k + at * 16) = read(k, ck);
+                *reinterpret_cast<Pack<T, VEC>*>(to_v + at * 16) = read(v, cv);
+            }
+        }
+    };
+    if (p.direct && dim < DP) {
+        for (int i = threadIdx.x; i < 4 * S::TILE / 16; i += S::THREADS) reinterpret_cast<float4v*>(s_tiles)[i] = float4v{};
+        __syncthreads();
+    }
+    if (tile < tile_end) {
+        look_up(tile);
+        stage(tile, 0);
+        if (tile + 1 < tile_end) look_up(tile + 1);
+    }
+
+    // This lane's row: its queries, and the positions that it sees.
+    const int row = rw * 32 + mine;
+    const bool real = row < rows;
+    const int64_t r = row0 + (real ? row : rows - 1);
+    const int token = task.first + (int)(r / G), q_head = head * G + (int)(r % G);
+    const int64_t position = task.position + r / G;
+    // [low, limit] within the tiles' positions, which are below 2^31
+    const int limit = position < 0 ? -1 : (int)(position < hi ? position : hi - 1), low = (int)(position - window + 1 > 0 ? position - window + 1 : 0);
+    int limit_min = limit, limit_max = limit, low_max = low;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        limit_min = min(limit_min, __shfl_xor(limit_min, o));
+        limit_max = max(limit_max, __shfl_xor(limit_max, o));
+        low_max = max(low_max, __shfl_xor(low_max, o));
+    }
+    constexpr int STEPS = CHUNKS / 2;
+    Frag q[STEPS];
+    {
+        const T* x = static_cast<const T*>(a.q.p) + (int64_t)token * a.q.token + q_head * a.q.head;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int c = (2 * s + half) * VEC;
+            if (real && c + VEC <= dim) {
+                const Pack<T, VEC> w = load_pack<T, VEC>(x + c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) q[s][e] = w.v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) q[s][e] = real && c + e < dim ? x[c + e] : (T)0.0f;
+            }
+        }
+    }
+    float16v o[DTILES];
+#pragma unroll
+    for (int d = 0; d < DTILES; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+    const float inf = __builtin_inff(), scale = a.scale * LOG2E;
+    float top = -inf, sum = 0.0f;   // the row's maximum score, and this lane's part of its sum
+
+    int buf = 0;
+    for (; tile < tile_end; ++tile, buf ^= 1) {
+        // this tile has landed, and everyone is done with the last one
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tile + 1 < tile_end) {
+            stage(tile + 1, buf ^ 1);
+            if (tile + 2 < tile_end) look_up(tile + 2);
+        }
+        const int key0 = tile * KEYS + kw * SUBS * 32;
+        if (rw * 32 >= rows || key0 > limit_max) continue;
+        const char* s_k = s_tiles + buf * 2 * S::TILE + kw * SUBS * 32 * S::ROW;
+        const char* s_v = s_k + S::TILE;
+        uint32_t gone[SUBS];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) gone[u] = (uint32_t)__ballot(s_gone[buf][(kw * SUBS + u) * 32 + mine]);
+        float16v sc[SUBS];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[u][e] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const int at = u * 32 + mine;
+                const Frag k = *reinterpret_cast<const Frag*>(s_k + at * S::ROW + ((2 * s + half) ^ key_swizzle<CHUNKS>(at)) * 16);
+                sc[u] = M::mma(k, q[s], sc[u]);
+            }
+        }
+        bool masked = key0 + SUBS * 32 - 1 > limit_min || key0 < low_max;
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) masked |= gone[u] != 0;
+        auto seen = [&](int u, int at) {   // whether this row sees key `at` of the 32
+            const int key = key0 + u * 32 + at;
+            return key <= limit && key >= low && !(gone[u] >> at & 1);
+        };
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!seen(u, 8 * (e >> 2) + 4 * half + (e & 3))) sc[u][e] = -inf;
+        }
+        float most = sc[0][0];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, sc[u][e]);
+        most = fmaxf(most, __shfl_xor(most, 32));
+        if (__any(most > top)) {
+            const float next = fmaxf(top, most);
+            const float f = top == -inf ? 0.0f : __builtin_amdgcn_exp2f((top - next) * scale);
+            top = next;
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < DTILES; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] *= f;
+        }
+        // p = 2^(s scale - base); any base near the maximum serves, as long as all of a row's p have it
+        const float base = top == -inf ? 0.0f : top * scale - M::SHIFT;
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                sc[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][e], scale, -base));
+                sum += sc[u][e];
+            }
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+            // Where rows see different keys, a NaN or an infinity among the values must not reach, as 0 times it, a row
+            // that does not see it: such values are left out of the product, and added where they are seen.
+            uint32_t odd = 0;
+            if (masked) {
+                for (int i = lane; i < 32 * CHUNKS; i += 64) {
+                    const Pack<T, VEC> w = *reinterpret_cast<const Pack<T, VEC>*>(s_v + u * 32 * S::ROW + i * 16);
+                    bool fine = true;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) fine &= is_finite(w.v[e]);
+                    if (!fine) odd |= 1u << (i / CHUNKS);
+                }
+#pragma unroll
+                for (int x = 32; x > 0; x >>= 1) odd |= __shfl_xor(odd, x);
+            }
+            if constexpr (S::SIZE == 2) {
+                const int i = lane & 15, at = (lane >> 4 & 1) * 16 + 4 * (i & 3);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    Frag w;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = (T)sc[u][8 * s + e];
+                    const int key = u * 32 + 16 * s + 4 * half + (i >> 2);
+#pragma unroll
+                    for (int d = 0; d < DTILES; ++d) {
+                        const int c = d * 4 + (at >> 3);
+                        union {
+                            short4v part[2];
+                            Frag whole;
+                            uint16_t bits[8];
+                        } v;
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+                            v.part[n] = read_transposed(s_v + (key + 8 * n) * S::ROW +
+                                                        (c ^ value_swizzle<CHUNKS, S::SIZE>(key + 8 * n)) * 16 + (at & 4) * 2);
+                        if (odd) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (!is_finite(v.whole[e])) v.bits[e] = 0;
+                        }
+                        o[d] = M::mma(v.whole, w, o[d]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = u * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+#pragma unroll
+                    for (int d = 0; d < DTILES; ++d) {
+                        const int c = d * 8 + (mine >> 2);
+                        float v = *reinterpret_cast<const float*>(s_v + key * S::ROW +
+                                                                  (c ^ value_swizzle<CHUNKS, S::SIZE>(key)) * 16 + (mine & 3) * 4);
+                        if (odd && !is_finite(v)) v = 0.0f;
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[u][e], o[d], 0, 0, 0);
+                    }
+                }
+            }
+            while (odd) {
+                const int at = __builtin_ctz(odd);
+                odd &= odd - 1;
+                if (!seen(u, at)) continue;
+                const int key = u * 32 + at;
+#pragma unroll
+                for (int d = 0; d < DTILES; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int x = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
+                        const T v = *reinterpret_cast<const T*>(s_v + key * S::ROW +
+                                                                ((x / VEC) ^ value_swizzle<CHUNKS, S::SIZE>(key)) * 16 + x % VEC * S::SIZE);
+                        if (!is_finite(v)) o[d][e] += (float)v;
+                    }
+            }
+        }
+    }
+    sum += __shfl_xor(sum, 32);
+
+    // Out: rows of this workgroup, whole, or this piece's sums.
+    const bool whole = pieces == 1;
+    const int64_t rows_at = ((int64_t)slot * heads + head) * S::ROWS;   // of the pieces
+    auto put = [&](int row_, int d, float4v v, float top_, float sum_) {   // four values from column d on
+        const int64_t r_ = row0 + row_;
+        if (!whole) {
+            *reinterpret_cast<float4v*>(p.sums + (rows_at + row_) * DP + d) = v;
+            if (d == 0) {
+                p.stats[(rows_at + row_) * 2] = top_;
+                p.stats[(rows_at + row_) * 2 + 1] = sum_;
+            }
+            return;
+        }
+        const int64_t token_ = task.first + r_ / G, head_ = head * G + r_ % G;
+        const float f = sum_ == 0.0f ? 0.0f : 1.0f / sum_;   // a NaN stays one
+        T* y = static_cast<T*>(a.out.p) + token_ * a.out.token + head_ * a.out.head + d;
+        if (d + 4 <= dim) {
+            Pack<T, 4> w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w.v[e] = rounded<T>(v[e] * f);
+            store_pack<T, 4>(y, w);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (d + e < dim) y[e] = rounded<T>(v[e] * f);
+        }
+        if (d == 0 && a.lse)
+            a.lse[token_ * a.q_heads + head_] = sum_ == 0.0f ? -inf : (top_ * scale - M::SHIFT + __log2f(sum_)) * LN2;
+    };
+    if constexpr (KW == 1) {
+        if (!real) return;
+#pragma unroll
+        for (int d = 0; d < DTILES; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                put(row, 32 * d + 8 * g + 4 * half, float4v{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]}, top, sum);
+    } else {
+        // the waves' sums over their keys, joined in order
+        __syncthreads();
+        float* s_out = reinterpret_cast<float*>(s_tiles);   // [wave][32][OUT_LD]
+#pragma unroll
+        for (int d = 0; d < DTILES; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4v*>(&s_out[(wave * 32 + mine) * S::OUT_LD + 32 * d + 8 * g + 4 * half]) =
+                    float4v{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+        if (half == 0) {
+            s_stats[wave][mine][0] = top;
+            s_stats[wave][mine][1] = sum;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * (DP / 4); i += S::THREADS) {
+            const int row_ = i / (DP / 4), d = i % (DP / 4) * 4, w0 = row_ / 32;
+            float most = -inf;
+#pragma unroll
+            for (int w = 0; w < KW; ++w) most = fmaxf(most, s_stats[w * RW + w0][row_ & 31][0]);
+            float4v v = {};
+            float total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < KW; ++w) {
+                const float t = s_stats[w * RW + w0][row_ & 31][0], f = t == -inf ? 0.0f : __builtin_amdgcn_exp2f((t - most) * scale);
+                total += s_stats[w * RW + w0][row_ & 31][1] * f;
+                const float4v x = *reinterpret_cast<const float4v*>(&s_out[((w * RW + w0) * 32 + (row_ & 31)) * S::OUT_LD + d]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += x[e] * f;
+            }
+            put(row_, d, v, most, total);
+        }
+    }
+#endif
+}
+
+// Joins the pieces of rows that were cut: a wave takes a row.
+template <int DT>
+__global__ __launch_bounds__(256) void k_join(AttendArgs a, Plan p, int dp) {
+    using T = typename Elem<DT>::T;
+    __shared__ int64_t s_scratch[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int token = blockIdx.x;
+    const int b = sequence_of(a.c.starts, (int)a.c.batch, token);
+    if (b < 0 || b >= a.c.batch) return;
+    const int tiles = piece_tiles<256>(a, p, s_scratch);
+    const Task task = task_of(a, p, b);
+    const int pieces = pieces_of(task, tiles);
+    if (pieces == 1 || token < task.first || token >= task.first + task.count) return;
+    int64_t before = 0;
+    for (int i = threadIdx.x; i < b; i += 256) {
+        const Task t = task_of(a, p, i);
+        before += (int64_t)t.row_tiles * pieces_of(t, tiles);
+    }
+    before = block_total<256>(before, s_scratch);
+    const float inf = __builtin_inff(), scale = a.scale * LOG2E;
+    const int dim = (int)a.c.dim, heads = (int)a.c.heads;
+    for (int q_head = blockIdx.y * 4 + wave; q_head < a.q_heads; q_head += gridDim.y * 4) {
+        const int64_t r = (int64_t)(token - task.first) * p.group + q_head % p.group;
+        const int64_t slot0 = before + (int64_t)(task.row_tiles - 1 - r / p.rows) * pieces;
+        if (slot0 + pieces > p.slots) return;   // starts that do not go up
+        const int64_t at0 = (slot0 * heads + q_head / p.group) * p.rows + r % p.rows, step = (int64_t)heads * p.rows;
+        float top = -inf;
+        for (int k = lane; k < pieces; k += 64) top = fmaxf(top, p.stats[(at0 + k * step) * 2]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        float v[4] = {}, sum = 0.0f;
+        for (int k = 0; k < pieces; ++k) {
+            const int64_t at = at0 + k * step;
+            const float t = p.stats[at * 2], s = p.stats[at * 2 + 1];
+            if (t == -inf && s == 0.0f) continue;   // sees nothing: its sums are zeros
+            const float f = __builtin_amdgcn_exp2f((t - top) * scale);
+            sum += s * f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e * 64 < dp && e * 64 + lane < dim) v[e] += p.sums[at * dp + e * 64 + lane] * f;
+        }
+        T* y = static_cast<T*>(a.out.p) + (int64_t)token * a.out.token + q_head * a.out.head;
+        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e * 64 + lane < dim) y[e * 64 + lane] = rounded<T>(v[e] * f);
+        if (lane == 0 && a.lse)
+            a.lse[(int64_t)token * a.q_heads + q_head] = sum == 0.0f ? -inf : (top * scale - Mat<DT>::SHIFT + __log2f(sum)) * LN2;
+    }
+}
+
+int padded(int64_t dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+
+// Sizes that a call's plan and its workspace share.
+struct Sizes {
+    bool few;                 // rows of a sequence, in the mean: one wave's, which split the keys
+    int rows, keys, target, dp;
+    int64_t slots;
+};
+Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads, int64_t dim, int type) {
+    Sizes s;
+    const int64_t G = q_heads / heads;
+    s.dp = padded(dim);
+    const int row = s.dp * elem_size(type);
+    s.few = n * G <= 32 * (batch < n ? batch : n);
+    s.rows = s.few ? 32 : 128;
+    s.keys = s.few ? (row <= 256 ? 128 : row <= 512 ? 64 : 32) : row <= 512 ? 64 : 32;
+    const int64_t most = batch < n ? batch : n;               // sequences with new tokens
+    const int64_t units = std::min<int64_t>(n * G, n * G / s.rows + most);   // tiles of rows
+    const int64_t total = s.few ? 2048 : 768;
+    s.target = 0;
+    if (units * heads < total && positions > LEAST_TILES * s.keys) s.target = (int)((total + heads - 1) / heads);
+    s.slots = units + s.target;
+    return s;
+}
+
+template <int DT, int DP, int RW, int KW>
+hipError_t attend(const AttendArgs& a, const Plan& p, hipStream_t stream) {
+    using S = Shape<DT, DP, RW, KW>;
+    static std::atomic<uint64_t> prepared{0};
+    hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_attend<S>), -1, S::LDS, prepared);
+    if (e != hipSuccess) return e;
+    const int64_t groups = (int64_t)p.slots * a.c.heads;
+    if (groups > (((int64_t)1 << 32) - 1) / S::THREADS) return hipErrorInvalidValue;
+    k_attend<S><<<(unsigned)groups, S::THREADS, S::LDS, stream>>>(a, p);
+    return hipGetLastError();
+}
+
+template <int DT, int DP>
+hipError_t attend_rows(const AttendArgs& a, const Plan& p, bool few, hipStream_t stream) {
+    constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), KW = ROW <= 256 ? 4 : ROW <= 512 ? 2 : 1;
+    return few ? attend<DT, DP, 1, KW>(a, p, stream) : attend<DT, DP, 4, 1>(a, p, stream);
+}
+
+}  // namespace
+
+int64_t paged_attention_workspace(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads, int64_t dim,
+                                  int type) {
+    if (n == 0 || batch == 0) return 0;
+    const Sizes s = sizes_of(n, batch, positions, q_heads, heads, dim, type);
+    return s.target ? s.slots * heads * s.rows * (s.dp + 2) * 4 : 0;
+}
+
+hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStream_t stream) {
+    return with_type((int)a.c.type, [&](auto type) -> hipError_t {
+        constexpr int DT = type.value;
+        const Sizes s = sizes_of(a.n, a.c.batch, a.c.width * a.c.page_size, a.q_heads, a.c.heads, a.c.dim, DT);
+        const int size = elem_size(DT);
+        uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v);
+        for (int64_t d : {a.c.dim, a.c.k_page, a.c.k_token, a.c.k_head, a.c.v_page, a.c.v_token, a.c.v_head}) bits |= (uintptr_t)(d * size);
+        Plan p;
+        p.size = divider(a.c.page_size);
+        p.group = (int)(a.q_heads / a.c.heads);
+        p.rows = s.rows;
+        p.keys = s.keys;
+        p.target = s.target;
+        p.slots = (int)s.slots;
+        p.direct = bits % 16 == 0;
+        p.sums = static_cast<float*>(workspace);
+        p.stats = p.sums + (s.target ? s.slots * a.c.heads * s.rows * s.dp : 0);
+        hipError_t e;
+        switch (s.dp) {
+            case 32: e = attend_rows<DT, 32>(a, p, s.few, stream); break;
+            case 64: e = attend_rows<DT, 64>(a, p, s.few, stream); break;
+            case 128: e = attend_rows<DT, 128>(a, p, s.few, stream); break;
+            default: e = attend_rows<DT, 256>(a, p, s.few, stream); break;
+        }
+        if (e != hipSuccess || !s.target) return e;
+        const dim3 grid((unsigned)a.n, (unsigned)((a.q_heads + 3) / 4));
+        k_join<DT><<<grid, 256, 0, stream>>>(a, p, s.dp);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace at

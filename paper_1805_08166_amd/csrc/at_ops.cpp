@@ -1,6 +1,7 @@
 // C entry points of the sequence-model operators: argument checks, then the
-// launchers of at_embed.hip, at_logprobs.hip and at_ortho.hip on the current
-// device.  Nothing is enqueued when an argument is refused.
+// launchers of at_embed.hip, at_logprobs.hip, at_ortho.hip, at_append.hip,
+// at_attend.hip and at_adjust.hip on the current device.  Nothing is enqueued when an argument is refused.
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -72,6 +73,43 @@ at_status ortho_args(const char* fn, int64_t batch, int64_t rows, int64_t cols, 
     if (batch < 0 || rows < 0 || cols < 0) return refuse(AT_E_INVALID, fn, "negative size");
     if (batch > 65535 || rows > 65536 || cols > 65536)
         return refuse(AT_E_UNSUPPORTED, fn, "more than 65535 matrices, or more than 65536 rows or columns");
+    return AT_OK;
+}
+
+// Whether rows of `dim` elements, `count` of them `stride` apart along each axis, lie
+// apart from one another: along axes in the order of their strides each steps over
+// everything before it.
+struct Axis {
+    int64_t count, stride;
+};
+bool apart(int64_t dim, Axis a, Axis b, Axis c) {
+    Axis axes[3] = {a, b, c};
+    std::sort(axes, axes + 3, [](const Axis& x, const Axis& y) { return x.stride < y.stride; });
+    __int128 extent = dim;
+    for (const Axis& x : axes) {
+        if (x.count <= 1) continue;
+        if (x.stride < extent) return false;
+        extent += (__int128)(x.count - 1) * x.stride;
+    }
+    return true;
+}
+
+at_status paged_args(const char* fn, const at_paged* c) {
+    if (!c) return refuse(AT_E_INVALID, fn, "NULL cache");
+    if (!type_ok((int)c->type) || c->type != (int)c->type) return refuse(AT_E_INVALID, fn, "unknown element type");
+    if (c->pages < 0 || c->page_size < 1 || c->heads < 1 || c->dim < 1 || c->batch < 0 || c->width < 0)
+        return refuse(AT_E_INVALID, fn, "negative or zero size");
+    if (c->pages > SIZE_MAX_31 || c->page_size > SIZE_MAX_31 || c->width > SIZE_MAX_31 || c->batch >= (int64_t)1 << 24)
+        return refuse(AT_E_UNSUPPORTED, fn, "pages, page size and table width must be below 2^31, the batch below 2^24");
+    if (c->heads > 65535 || c->dim > 256) return refuse(AT_E_UNSUPPORTED, fn, "more than 65535 heads or 256 values a head");
+    for (int64_t s : {c->k_page, c->k_token, c->k_head, c->v_page, c->v_token, c->v_head, c->table_ld})
+        if (s < 0) return refuse(AT_E_INVALID, fn, "negative stride");
+    if (c->batch == 0) return AT_OK;
+    if (!c->starts || !c->lengths || (c->width > 0 && !c->table)) return refuse(AT_E_INVALID, fn, "NULL batch");
+    if (c->pages > 0 && (!c->k || !c->v)) return refuse(AT_E_INVALID, fn, "NULL cache");
+    if (!aligned_t(c->k, (int)c->type) || !aligned_t(c->v, (int)c->type) || !aligned(c->table, 4) || !aligned(c->starts, 4) ||
+        !aligned(c->lengths, 4))
+        return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
     return AT_OK;
 }
 
@@ -207,6 +245,107 @@ at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx
     const OrthoArgs o{x, xtype, xbatch, ldx,   batch, rows,  cols,   steps, a,
                       b, c,     eps,    scale, out,   otype, obatch, ldo,   fp16_products};
     return done(launch_ortho(o, workspace, (hipStream_t)stream), fn);
+}
+
+at_status at_paged_append(const at_paged* cache, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                          int64_t v_token, int64_t v_head, int64_t n, const void* q, int64_t q_token, int64_t q_head,
+                          int64_t q_heads, void* q_out, int64_t o_token, int64_t o_head, const void* k_weight,
+                          const void* q_weight, float eps, const double* freqs, int64_t rot, int interleaved,
+                          float rot_scale, at_stream_t stream) {
+    const char* fn = "at_paged_append";
+    const at_status st = paged_args(fn, cache);
+    if (st != AT_OK) return st;
+    if (n < 0 || q_heads < 0) return refuse(AT_E_INVALID, fn, "negative size");
+    if (n > SIZE_MAX_31 || q_heads > 65535) return refuse(AT_E_UNSUPPORTED, fn, "2^31 tokens or 65536 query heads");
+    if (!q) q_heads = 0;
+    if (rot < 0 || rot > cache->dim || rot % 2) return refuse(AT_E_INVALID, fn, "rot is even, from 0 to dim");
+    if (!std::isfinite(rot_scale)) return refuse(AT_E_INVALID, fn, "rot_scale must be finite");
+    if (!std::isfinite(eps) || eps < 0.0f) return refuse(AT_E_INVALID, fn, "eps must be finite and not negative");
+    for (int64_t s : {k_token, k_head, v_token, v_head, q_token, q_head, o_token, o_head})
+        if (s < 0) return refuse(AT_E_INVALID, fn, "negative stride");
+    for (int of_v = 0; of_v < 2; ++of_v)
+        if (!apart(cache->dim, {cache->pages, of_v ? cache->v_page : cache->k_page},
+                   {cache->page_size, of_v ? cache->v_token : cache->k_token}, {cache->heads, of_v ? cache->v_head : cache->k_head}))
+            return refuse(AT_E_INVALID, fn, "rows of the cache overlap");
+    if (q_heads && !apart(cache->dim, {n, o_token}, {q_heads, o_head}, {1, 0}))
+        return refuse(AT_E_INVALID, fn, "rows of q_out overlap");
+    if (n == 0 || cache->batch == 0) return AT_OK;
+    if (!k || !v || (q_heads && !q_out) || (rot && !freqs)) return refuse(AT_E_INVALID, fn, "NULL buffer");
+    const int type = (int)cache->type;
+    if (!aligned_t(k, type) || !aligned_t(v, type) || !aligned_t(q, type) || !aligned_t(q_out, type) ||
+        !aligned_t(k_weight, type) || !aligned_t(q_weight, type) || !aligned(freqs, 8))
+        return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
+    const AppendArgs a{*cache, {k, k_token, k_head}, {v, v_token, v_head}, {q, q_token, q_head}, {q_out, o_token, o_head}, n, q_heads,
+                       k_weight, q_weight, eps, freqs, (int)rot, interleaved != 0, rot_scale};
+    return done(launch_paged_append(a, (hipStream_t)stream), fn);
+}
+
+at_status at_paged_attention_workspace(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads,
+                                       int64_t dim, int type, int64_t* bytes) {
+    const char* fn = "at_paged_attention_workspace";
+    if (!bytes) return refuse(AT_E_INVALID, fn, "NULL output");
+    if (!type_ok(type)) return refuse(AT_E_INVALID, fn, "unknown element type");
+    if (n < 0 || batch < 0 || positions < 0 || heads < 1 || q_heads < heads || q_heads % heads || dim < 1)
+        return refuse(AT_E_INVALID, fn, "negative size, or query heads that are no multiple of the heads");
+    if (n > SIZE_MAX_31 || batch >= (int64_t)1 << 24 || q_heads > 65535 || dim > 256)
+        return refuse(AT_E_UNSUPPORTED, fn, "2^31 tokens, 2^24 sequences, 65536 heads or more than 256 values a head");
+    *bytes = paged_attention_workspace(n, batch, positions, q_heads, heads, dim, type);
+    return AT_OK;
+}
+
+at_status at_paged_attention(const at_paged* cache, const void* q, int64_t q_token, int64_t q_head, int64_t n,
+                             int64_t q_heads, float scale, int64_t window, void* out, int64_t o_token, int64_t o_head,
+                             float* lse, void* workspace, int64_t workspace_bytes, at_stream_t stream) {
+    const char* fn = "at_paged_attention";
+    at_status st = paged_args(fn, cache);
+    if (st != AT_OK) return st;
+    if (n < 0) return refuse(AT_E_INVALID, fn, "negative size");
+    if (q_heads < cache->heads || q_heads % cache->heads) return refuse(AT_E_INVALID, fn, "query heads are no multiple of the cache's");
+    if (n > SIZE_MAX_31 || q_heads > 65535) return refuse(AT_E_UNSUPPORTED, fn, "2^31 tokens or 65536 query heads");
+    if (!std::isfinite(scale) || scale <= 0.0f) return refuse(AT_E_INVALID, fn, "scale must be positive and finite");
+    if (window < 0) return refuse(AT_E_INVALID, fn, "negative window");
+    if (q_token < 0 || q_head < 0 || o_token < 0 || o_head < 0) return refuse(AT_E_INVALID, fn, "negative stride");
+    if (!apart(cache->dim, {n, o_token}, {q_heads, o_head}, {1, 0})) return refuse(AT_E_INVALID, fn, "output rows overlap");
+    if (n == 0 || cache->batch == 0) return AT_OK;
+    if (!q || !out) return refuse(AT_E_INVALID, fn, "NULL buffer");
+    const int type = (int)cache->type;
+    if (!aligned_t(q, type) || !aligned_t(out, type) || !aligned(lse, 4))
+        return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
+    st = workspace_args(fn, workspace, workspace_bytes,
+                        paged_attention_workspace(n, cache->batch, cache->width * cache->page_size, q_heads, cache->heads, cache->dim, type));
+    if (st != AT_OK) return st;
+    const AttendArgs a{*cache, {q, q_token, q_head}, {out, o_token, o_head}, lse, n, q_heads, scale, window};
+    return done(launch_paged_attention(a, workspace, (hipStream_t)stream), fn);
+}
+
+at_status at_adjust_logits(const void* logits, int type, int64_t ld, int64_t n, int64_t vocab, void* out, int64_t ldo,
+                           int itype, const void* past, int64_t ldp, int64_t past_len, const int32_t* lengths,
+                           const int32_t* prompt_lengths, const float* repetition, const float* frequency,
+                           const float* presence, const void* bias_tokens, const float* bias, int64_t n_bias,
+                           int64_t bias_ld, const int32_t* mask, int64_t mask_ld, int64_t mask_count,
+                           const int32_t* mask_rows, const int32_t* valid, at_stream_t stream) {
+    const char* fn = "at_adjust_logits";
+    const at_status st = row_args(fn, type, ld, n, vocab, itype, 1.0f);
+    if (st != AT_OK) return st;
+    if (past_len < 0 || n_bias < 0 || mask_count < 0) return refuse(AT_E_INVALID, fn, "negative size");
+    if (past_len > SIZE_MAX_31 || n_bias > SIZE_MAX_31 || mask_count > SIZE_MAX_31)
+        return refuse(AT_E_UNSUPPORTED, fn, "sizes must be below 2^31");
+    if (ldo < vocab && n > 1) return refuse(AT_E_INVALID, fn, "output rows overlap (stride below vocab)");
+    if (ldp < 0 || bias_ld < 0 || mask_ld < 0) return refuse(AT_E_INVALID, fn, "negative stride");
+    if (!past) past_len = 0;
+    if (!bias_tokens && !bias) n_bias = 0;
+    if (!mask) mask_count = 0;
+    if (n == 0 || vocab == 0) return AT_OK;
+    if (out == logits && ld != ldo && n > 1) return refuse(AT_E_INVALID, fn, "in place with another stride");
+    if (!logits || !out || (n_bias && (!bias_tokens || !bias))) return refuse(AT_E_INVALID, fn, "NULL buffer");
+    const int64_t token = itype == AT_I64 ? 8 : 4;
+    if (!aligned_t(logits, type) || !aligned_t(out, type) || !aligned(past, token) || !aligned(bias_tokens, token) ||
+        !aligned(lengths, 4) || !aligned(prompt_lengths, 4) || !aligned(repetition, 4) || !aligned(frequency, 4) ||
+        !aligned(presence, 4) || !aligned(bias, 4) || !aligned(mask, 4) || !aligned(mask_rows, 4) || !aligned(valid, 4))
+        return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
+    const AdjustArgs a{logits, type, ld, n, vocab, out, ldo, itype, past, ldp, past_len, lengths, prompt_lengths, repetition, frequency,
+                       presence, bias_tokens, bias, n_bias, bias_ld, mask, mask_ld, mask_count, mask_rows, valid};
+    return done(launch_adjust(a, (hipStream_t)stream), fn);
 }
 
 }  // extern "C"

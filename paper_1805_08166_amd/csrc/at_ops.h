@@ -163,4 +163,57 @@ struct OrthoArgs {
 int64_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, bool fp16_products);
 hipError_t launch_ortho(const OrthoArgs& a, void* workspace, hipStream_t stream);
 
+// Rows of heads by token: element [token][head][0] is at p + token * token_ld + head * head_ld.
+template <class P>
+struct Heads {
+    P p;
+    int64_t token, head;
+};
+
+struct AppendArgs {
+    at_paged c;
+    Heads<const void*> k, v, q;
+    Heads<void*> q_out;
+    int64_t n, q_heads;
+    const void *k_weight, *q_weight;
+    float eps;
+    const double* freqs;
+    int rot, interleaved;
+    float rot_scale;
+};
+hipError_t launch_paged_append(const AppendArgs& a, hipStream_t stream);
+
+struct AttendArgs {
+    at_paged c;
+    Heads<const void*> q;
+    Heads<void*> out;
+    float* lse;
+    int64_t n, q_heads;
+    float scale;
+    int64_t window;
+};
+int64_t paged_attention_workspace(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads, int64_t dim,
+                                  int type);
+hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStream_t stream);
+
+struct AdjustArgs {
+    const void* logits;
+    int type;
+    int64_t ld, n, vocab;
+    void* out;
+    int64_t ldo;
+    int wide;
+    const void* past;
+    int64_t ldp, past_len;
+    const int32_t *lengths, *prompt_lengths;
+    const float *repetition, *frequency, *presence;
+    const void* bias_tokens;
+    const float* bias;
+    int64_t n_bias, bias_ld;
+    const int32_t* mask;
+    int64_t mask_ld, mask_count;
+    const int32_t *mask_rows, *valid;
+};
+hipError_t launch_adjust(const AdjustArgs& a, hipStream_t stream);
+
 }  // namespace at
