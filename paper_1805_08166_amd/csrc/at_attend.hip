@@ -76,7 +76,7 @@ struct Plan {
     int keys;            // of a tile
     int target;          // pieces a head that the keys are cut into, about; 0: whole sequences
     int slots;           // pieces a head, at most
-    int direct;          // rows of the cache can be moved to LDS 16 aligned bytes at a time
+    int even;            // rows of the cache are whole aligned 16 bytes, and those of a move lie in one page
     float* sums;         // [slot][head][row][dim padded]
     float* stats;        // [slot][head][row][2]: maximum and sum
 };
@@ -149,6 +149,9 @@ struct Shape {
     static constexpr int ROWS = ROW_WAVES * 32;
     static constexpr int TILE = KEYS * ROW;            // bytes of a tile of keys or values
     static constexpr int MOVES = TILE / 1024 / WAVES;  // of a wave, a KB each
+    static constexpr int MOVE_ROWS = 64 / CHUNKS;
+    static constexpr int IDS = KEYS > 64 ? 2 : 1;      // words of a lane that hold a tile's page numbers
+    static constexpr int WAVES_EU = ROW <= 256 ? 2 : 1;
     static constexpr int OUT_LD = DP + 4;
     static constexpr int JOIN = KEY_WAVES > 1 ? WAVES * 32 * OUT_LD * 4 : 0;
     static constexpr int LDS = 4 * TILE > JOIN ? 4 * TILE : JOIN;
@@ -174,13 +177,16 @@ __device__ __forceinline__ short4v read_transposed(const char* p) {
         (__attribute__((address_space(3))) short4v*)(__attribute__((address_space(3))) char*)p);
 }
 
+// A value that all lanes have, as the compiler cannot tell.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 template <class T>
 __device__ __forceinline__ bool is_finite(T v) {
     return __builtin_isfinite((float)v);
 }
 
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
+__global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a, Plan p) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host needs its launch stub only, and does not know all of the device's instructions
     constexpr int DT = S::DT, DP = S::DP, RW = S::ROW_WAVES, KW = S::KEY_WAVES;
     using T = typename Elem<DT>::T;
@@ -188,18 +194,20 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
     using Frag = typename M::Frag;
     constexpr int VEC = S::VEC, SUBS = S::SUBS, KEYS = S::KEYS, CHUNKS = S::CHUNKS, DTILES = DP / 32;
     extern __shared__ char s_tiles[];          // [2][keys, values][KEYS][DP]
-    __shared__ uint32_t s_gone[2][KEYS];       // whether a tile's row is not there
     __shared__ int64_t s_scratch[S::WAVES];
-    __shared__ int s_place[2];
+    __shared__ int s_place[2], s_odd;
     __shared__ float s_stats[S::WAVES][32][2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, mine = lane & 31;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, mine = lane & 31;
     const int rw = wave % RW, kw = wave / RW;
     const int heads = (int)a.c.heads, head = blockIdx.x % heads, slot = blockIdx.x / heads;
 
     // Which sequence, tile of rows and piece of keys.
     const int tiles = piece_tiles<S::THREADS>(a, p, s_scratch);
     {
-        if (threadIdx.x == 0) s_place[0] = -1;
+        if (threadIdx.x == 0) {
+            s_place[0] = -1;
+            s_odd = 0;
+        }
         const int batch = (int)a.c.batch, each = (batch + S::THREADS - 1) / S::THREADS;
         const int b0 = threadIdx.x * each, b1 = b0 + each < batch ? b0 + each : batch;
         int64_t here = 0;
@@ -231,11 +239,11 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
         }
         __syncthreads();
     }
-    const int b = s_place[0];
+    const int b = uniform(s_place[0]);
     if (b < 0) return;
     const Task task = task_of(a, p, b);
-    const int pieces = pieces_of(task, tiles), piece = s_place[1] % pieces;
-    const int row_tile = task.row_tiles - 1 - s_place[1] / pieces;   // a prompt's longest first
+    const int pieces = pieces_of(task, tiles), in_task = uniform(s_place[1]), piece = in_task % pieces;
+    const int row_tile = task.row_tiles - 1 - in_task / pieces;   // a prompt's longest first
 
     // Rows of this workgroup, and the keys that they see.
     const int G = p.group;
@@ -243,54 +251,77 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
     const int rows = (int)(all_rows - row0 < S::ROWS ? all_rows - row0 : S::ROWS);
     const int64_t first_pos = task.position + row0 / G, last_pos = task.position + (row0 + rows - 1) / G;
     const int64_t window = a.window > 0 ? a.window : (int64_t)1 << 40;
-    int64_t lo = first_pos - window + 1, hi = last_pos + 1;   // positions [lo, hi)
+    int64_t lo = first_pos - window + 1, hi64 = last_pos + 1;   // positions [lo, hi)
     lo = lo < 0 ? 0 : lo;
-    hi = hi < task.length ? hi : task.length;
-    int tile = (int)((lo < hi ? lo : 0) / KEYS), tile_end = (int)(hi > lo ? (hi + KEYS - 1) / KEYS : 0);
+    hi64 = hi64 < task.length ? hi64 : task.length;
+    const int hi = hi64 < 0 ? 0 : (int)hi64;
+    int tile = (int)((lo < hi ? lo : 0) / KEYS), tile_end = lo < hi ? (hi + KEYS - 1) / KEYS : 0;
     {
         const int64_t from = (int64_t)task.lo + (int64_t)piece * tiles, to = from + tiles;
         if (tile < from) tile = (int)from;
         if (tile_end > to) tile_end = (int)to;
     }
 
-    // Moves of a tile into LDS: this lane's row and chunk of each.
+    // Page numbers of a tile, one a lane, from that of its first position on.
     const int32_t* table = a.c.table + b * a.c.table_ld;
-    const T* k_head = static_cast<const T*>(a.c.k) + head * a.c.k_head;
-    const T* v_head = static_cast<const T*>(a.c.v) + head * a.c.v_head;
-    constexpr int MOVES = S::MOVES;
-    auto row_of = [&](int q) { return ((wave * MOVES + q) * 64 + lane) / CHUNKS; };
-    const int dim = (int)a.c.dim;
-    int ids[MOVES];   // pages of the next tile's rows, -1 where there is none
-    auto look_up = [&](int t) {
-#pragma unroll
-        for (int q = 0; q < MOVES; ++q) {
-            const int64_t pos = (int64_t)t * KEYS + row_of(q);
-            ids[q] = pos < hi ? table[divided((uint32_t)pos, p.size)] : -1;
-        }
+    const int used_pages = (int)divided((uint32_t)(hi + p.size.d - 1 < hi ? hi : hi + p.size.d - 1), p.size);   // pages below hi
+    struct Ids {
+        int v[S::IDS];
+        uint64_t bad[S::IDS];   // those that are not there
     };
-    auto stage = [&](int t, int buf) {
-        char* to_k = s_tiles + buf * 2 * S::TILE;
-        char* to_v = to_k + S::TILE;
+    auto look_up = [&](int t) {
+        Ids r;
+        const int first = (int)divided((uint32_t)(t * KEYS), p.size);
 #pragma unroll
-        for (int q = 0; q < MOVES; ++q) {
-            const int row = row_of(q), at = (wave * MOVES + q) * 64 + lane, chunk = at % CHUNKS;
-            const int ck = (chunk ^ key_swizzle<CHUNKS>(row)) * VEC, cv = (chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * VEC;
-            const bool there = (uint32_t)ids[q] < (uint32_t)a.c.pages;
-            if (chunk == 0) s_gone[buf][row] = !there;
-            const uint32_t pos = (uint32_t)(t * (int64_t)KEYS + row);
-            const int64_t place = there ? pos - divided(pos, p.size) * p.size.d : 0, page = there ? ids[q] : 0;
-            const T* k = k_head + page * a.c.k_page + place * a.c.k_token;
-            const T* v = v_head + page * a.c.v_page + place * a.c.v_token;
-            if (p.direct) {
-                if (there) {
+        for (int i = 0; i < S::IDS; ++i) {
+            const int at = first + i * 64 + lane;
+            r.v[i] = at < used_pages ? table[at] : 0;
+            r.bad[i] = __ballot((uint32_t)r.v[i] >= (uint32_t)a.c.pages && at < used_pages);
+        }
+        return r;
+    };
+    // A tile into LDS, a KB a move: even: all rows of a move lie in one page, whose address is the wave's.
+    constexpr int MOVES = S::MOVES, MOVE_ROWS = S::MOVE_ROWS;
+    const int dim = (int)a.c.dim;
+    const char* k_head = static_cast<const char*>(a.c.k) + (int64_t)head * a.c.k_head * S::SIZE;
+    const char* v_head = static_cast<const char*>(a.c.v) + (int64_t)head * a.c.v_head * S::SIZE;
+    const int lane_row = lane / CHUNKS, lane_chunk = lane % CHUNKS;
+    const uint32_t k_lane = (uint32_t)(lane_row * a.c.k_token * S::SIZE), v_lane = (uint32_t)(lane_row * a.c.v_token * S::SIZE);
+    auto stage = [&](int t, int buf, const Ids& ids) {
+        char* to_k = s_tiles + buf * 2 * S::TILE + wave * MOVES * 1024;
+        char* to_v = to_k + S::TILE;
+        const int first = (int)divided((uint32_t)(t * KEYS), p.size);
+        if (p.even) {
+#pragma unroll
+            for (int q = 0; q < MOVES; ++q) {
+                const int row0_ = (wave * MOVES + q) * MOVE_ROWS, pos = t * KEYS + row0_;
+                const int at = (int)divided((uint32_t)pos, p.size) - first;
+                const int id = __builtin_amdgcn_readlane(S::IDS > 1 && at >= 64 ? ids.v[S::IDS - 1] : ids.v[0], at & 63);
+                const int row = row0_ + lane_row;
+                const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row)) * 16, cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * 16;
+                const int64_t place = pos - (int64_t)(at + first) * p.size.d;
+                if ((uint32_t)id < (uint32_t)a.c.pages && pos + lane_row < hi) {
+                    const char* k = k_head + (id * a.c.k_page + place * a.c.k_token) * S::SIZE;
+                    const char* v = v_head + (id * a.c.v_page + place * a.c.v_token) * S::SIZE;
                     // (the moves of lanes past dim are left out: zeros lie there)
-                    if (ck < dim) __builtin_amdgcn_global_load_lds(k + ck, to_k + (wave * MOVES + q) * 1024, 16, 0, 0);
-                    if (cv < dim) __builtin_amdgcn_global_load_lds(v + cv, to_v + (wave * MOVES + q) * 1024, 16, 0, 0);
+                    if (DP == dim || (int)ck < dim * S::SIZE) __builtin_amdgcn_global_load_lds(k + (k_lane + ck), to_k + q * 1024, 16, 0, 0);
+                    if (DP == dim || (int)cv < dim * S::SIZE) __builtin_amdgcn_global_load_lds(v + (v_lane + cv), to_v + q * 1024, 16, 0, 0);
                 } else {
-                    *reinterpret_cast<float4v*>(to_k + at * 16) = float4v{};
-                    *reinterpret_cast<float4v*>(to_v + at * 16) = float4v{};
+                    *reinterpret_cast<float4v*>(to_k + q * 1024 + lane * 16) = float4v{};
+                    *reinterpret_cast<float4v*>(to_v + q * 1024 + lane * 16) = float4v{};
                 }
-            } else {
+            }
+        } else {
+#pragma unroll 1
+            for (int q = 0; q < MOVES; ++q) {
+                const int row = (wave * MOVES + q) * MOVE_ROWS + lane_row, pos = t * KEYS + row;
+                const uint32_t at = divided((uint32_t)pos, p.size);
+                const int id = pos < hi ? table[at] : -1;
+                const bool there = (uint32_t)id < (uint32_t)a.c.pages;
+                const int64_t place = there ? pos - (int64_t)at * p.size.d : 0, page = there ? id : 0;
+                const T* k = reinterpret_cast<const T*>(k_head) + page * a.c.k_page + place * a.c.k_token;
+                const T* v = reinterpret_cast<const T*>(v_head) + page * a.c.v_page + place * a.c.v_token;
+                const int ck = (lane_chunk ^ key_swizzle<CHUNKS>(row)) * VEC, cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * VEC;
                 auto read = [&](const T* x, int c) {
                     Pack<T, VEC> w;
                     if (there && c + VEC <= dim) return load_pack<T, VEC>(x + c);
@@ -298,19 +329,20 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
                     for (int e = 0; e < VEC; ++e) w.v[e] = there && c + e < dim ? x[c + e] : (T)0.0f;
                     return w;
                 };
-                *reinterpret_cast<Pack<T, VEC>*>(to_k + at * 16) = read(k, ck);
-                *reinterpret_cast<Pack<T, VEC>*>(to_v + at * 16) = read(v, cv);
+                *reinterpret_cast<Pack<T, VEC>*>(to_k + q * 1024 + lane * 16) = read(k, ck);
+                *reinterpret_cast<Pack<T, VEC>*>(to_v + q * 1024 + lane * 16) = read(v, cv);
             }
         }
     };
-    if (p.direct && dim < DP) {
+    if (p.even && dim < DP) {
         for (int i = threadIdx.x; i < 4 * S::TILE / 16; i += S::THREADS) reinterpret_cast<float4v*>(s_tiles)[i] = float4v{};
         __syncthreads();
     }
+    Ids here = {}, next = {};
     if (tile < tile_end) {
-        look_up(tile);
-        stage(tile, 0);
-        if (tile + 1 < tile_end) look_up(tile + 1);
+        here = look_up(tile);
+        stage(tile, 0, here);
+        if (tile + 1 < tile_end) next = look_up(tile + 1);
     }
 
     // This lane's row: its queries, and the positions that it sees.
@@ -321,13 +353,20 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
     const int64_t position = task.position + r / G;
     // [low, limit] within the tiles' positions, which are below 2^31
     const int limit = position < 0 ? -1 : (int)(position < hi ? position : hi - 1), low = (int)(position - window + 1 > 0 ? position - window + 1 : 0);
-    int limit_min = limit, limit_max = limit, low_max = low;
+    // of a row's position: the last position it sees, and the first
+    auto limit_of = [&](int64_t at) { return uniform(at < 0 ? -1 : (int)(at < hi ? at : hi - 1)); };
+    auto low_of = [&](int64_t at) { return uniform((int)(at - window + 1 > 0 ? at - window + 1 : 0)); };
+    const int wave_first = rw * 32 < rows ? rw * 32 : rows - 1, wave_last = rw * 32 + 31 < rows ? rw * 32 + 31 : rows - 1;
+    const int64_t wave_from = task.position + (row0 + wave_first) / G, wave_to = task.position + (row0 + wave_last) / G;
+    const int limit_min = limit_of(wave_from), limit_max = limit_of(wave_to), low_max = low_of(wave_to);
+    // Whether some row of this workgroup does not see all of a tile.
+    const int all_limit = limit_of(first_pos), all_low = low_of(last_pos);
+    auto partly_seen = [&](int t, const uint64_t (&bad)[S::IDS]) {
+        bool any = t * KEYS + KEYS - 1 > all_limit || t * KEYS < all_low;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        limit_min = min(limit_min, __shfl_xor(limit_min, o));
-        limit_max = max(limit_max, __shfl_xor(limit_max, o));
-        low_max = max(low_max, __shfl_xor(low_max, o));
-    }
+        for (int i = 0; i < S::IDS; ++i) any |= bad[i] != 0;
+        return any;
+    };
     constexpr int STEPS = CHUNKS / 2;
     Frag q[STEPS];
     {
@@ -353,42 +392,76 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
     const float inf = __builtin_inff(), scale = a.scale * LOG2E;
     float top = -inf, sum = 0.0f;   // the row's maximum score, and this lane's part of its sum
 
+    // Where this lane reads: a chunk of key `mine`, by XOR with a step's chunks; the values of four rows by 16 lanes.
+    const int k_at = mine * S::ROW + ((half ^ key_swizzle<CHUNKS>(mine)) * 16);
+    const int tr_row = 4 * half + (lane & 15) / 4, tr_chunk = (lane >> 4 & 1) * 2 + (lane >> 1 & 1), tr_byte = (lane & 1) * 8;
+    const int tile0 = tile;
     int buf = 0;
     for (; tile < tile_end; ++tile, buf ^= 1) {
         // this tile has landed, and everyone is done with the last one
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        uint64_t bad[S::IDS];
+#pragma unroll
+        for (int i = 0; i < S::IDS; ++i) bad[i] = here.bad[i];
+        if (partly_seen(tile, bad)) {
+            // A NaN or an infinity among the values must not reach, as 0 times it, a row that does not see it: it is
+            // left out here, by the lane that moved it, and added at the end where it is seen.
+            char* own = s_tiles + buf * 2 * S::TILE + S::TILE + wave * MOVES * 1024 + lane * 16;
+#pragma unroll 1
+            for (int q = 0; q < MOVES; ++q, own += 1024) {
+                Pack<T, VEC> w = *reinterpret_cast<const Pack<T, VEC>*>(own);
+                bool fine = true;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const bool f = is_finite(w.v[e]);
+                    fine &= f;
+                    w.v[e] = f ? w.v[e] : (T)0.0f;
+                }
+                if (!fine) {
+                    *reinterpret_cast<Pack<T, VEC>*>(own) = w;
+                    s_odd = 1;
+                }
+            }
+        }
         __syncthreads();
         if (tile + 1 < tile_end) {
-            stage(tile + 1, buf ^ 1);
-            if (tile + 2 < tile_end) look_up(tile + 2);
+            here = next;
+            stage(tile + 1, buf ^ 1, here);
+            if (tile + 2 < tile_end) next = look_up(tile + 2);
         }
         const int key0 = tile * KEYS + kw * SUBS * 32;
         if (rw * 32 >= rows || key0 > limit_max) continue;
         const char* s_k = s_tiles + buf * 2 * S::TILE + kw * SUBS * 32 * S::ROW;
         const char* s_v = s_k + S::TILE;
-        uint32_t gone[SUBS];
-#pragma unroll
-        for (int u = 0; u < SUBS; ++u) gone[u] = (uint32_t)__ballot(s_gone[buf][(kw * SUBS + u) * 32 + mine]);
         float16v sc[SUBS];
 #pragma unroll
-        for (int u = 0; u < SUBS; ++u) {
+        for (int u = 0; u < SUBS; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[u][e] = 0.0f;
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                const int at = u * 32 + mine;
-                const Frag k = *reinterpret_cast<const Frag*>(s_k + at * S::ROW + ((2 * s + half) ^ key_swizzle<CHUNKS>(at)) * 16);
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                const Frag k = *reinterpret_cast<const Frag*>(s_k + (k_at ^ s * 32) + u * 32 * S::ROW);
                 sc[u] = M::mma(k, q[s], sc[u]);
             }
-        }
-        bool masked = key0 + SUBS * 32 - 1 > limit_min || key0 < low_max;
+        uint32_t gone[SUBS] = {};   // keys whose page is not there
+        bool any_bad = false;
 #pragma unroll
-        for (int u = 0; u < SUBS; ++u) masked |= gone[u] != 0;
+        for (int i = 0; i < S::IDS; ++i) any_bad |= bad[i] != 0;
         auto seen = [&](int u, int at) {   // whether this row sees key `at` of the 32
             const int key = key0 + u * 32 + at;
             return key <= limit && key >= low && !(gone[u] >> at & 1);
         };
-        if (masked) {
+        if (key0 + SUBS * 32 - 1 > limit_min || key0 < low_max || any_bad) {
+            if (any_bad) {
+                const uint32_t first = divided((uint32_t)(tile * KEYS), p.size);
+#pragma unroll
+                for (int u = 0; u < SUBS; ++u) {
+                    const uint32_t at = divided((uint32_t)(key0 + u * 32 + mine), p.size) - first;
+                    gone[u] = (uint32_t)__ballot((S::IDS > 1 && at >= 64 ? bad[S::IDS - 1] : bad[0]) >> (at & 63) & 1);
+                }
+            }
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
@@ -402,9 +475,9 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
             for (int e = 0; e < 16; ++e) most = fmaxf(most, sc[u][e]);
         most = fmaxf(most, __shfl_xor(most, 32));
         if (__any(most > top)) {
-            const float next = fmaxf(top, most);
-            const float f = top == -inf ? 0.0f : __builtin_amdgcn_exp2f((top - next) * scale);
-            top = next;
+            const float over = fmaxf(top, most);
+            const float f = top == -inf ? 0.0f : __builtin_amdgcn_exp2f((top - over) * scale);
+            top = over;
             sum *= f;
 #pragma unroll
             for (int d = 0; d < DTILES; ++d)
@@ -422,75 +495,62 @@ __global__ __launch_bounds__(S::THREADS) void k_attend(AttendArgs a, Plan p) {
             }
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
-            // Where rows see different keys, a NaN or an infinity among the values must not reach, as 0 times it, a row
-            // that does not see it: such values are left out of the product, and added where they are seen.
-            uint32_t odd = 0;
-            if (masked) {
-                for (int i = lane; i < 32 * CHUNKS; i += 64) {
-                    const Pack<T, VEC> w = *reinterpret_cast<const Pack<T, VEC>*>(s_v + u * 32 * S::ROW + i * 16);
-                    bool fine = true;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) fine &= is_finite(w.v[e]);
-                    if (!fine) odd |= 1u << (i / CHUNKS);
-                }
-#pragma unroll
-                for (int x = 32; x > 0; x >>= 1) odd |= __shfl_xor(odd, x);
-            }
             if constexpr (S::SIZE == 2) {
-                const int i = lane & 15, at = (lane >> 4 & 1) * 16 + 4 * (i & 3);
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     Frag w;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) w[e] = (T)sc[u][8 * s + e];
-                    const int key = u * 32 + 16 * s + 4 * half + (i >> 2);
 #pragma unroll
                     for (int d = 0; d < DTILES; ++d) {
-                        const int c = d * 4 + (at >> 3);
                         union {
                             short4v part[2];
                             Frag whole;
-                            uint16_t bits[8];
                         } v;
 #pragma unroll
                         for (int n = 0; n < 2; ++n)
-                            v.part[n] = read_transposed(s_v + (key + 8 * n) * S::ROW +
-                                                        (c ^ value_swizzle<CHUNKS, S::SIZE>(key + 8 * n)) * 16 + (at & 4) * 2);
-                        if (odd) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (!is_finite(v.whole[e])) v.bits[e] = 0;
-                        }
+                            v.part[n] = read_transposed(s_v + (u * 32 + 16 * s + 8 * n) * S::ROW + tr_row * S::ROW +
+                                                        ((d * 4 + tr_chunk) ^ value_swizzle<CHUNKS, 2>(tr_row)) * 16 + tr_byte);
                         o[d] = M::mma(v.whole, w, o[d]);
                     }
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = u * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+                    const int key = u * 32 + 8 * (e >> 2) + (e & 3);   // and four on in the other half, whose chunks are swizzled
 #pragma unroll
                     for (int d = 0; d < DTILES; ++d) {
-                        const int c = d * 8 + (mine >> 2);
-                        float v = *reinterpret_cast<const float*>(s_v + key * S::ROW +
-                                                                  (c ^ value_swizzle<CHUNKS, S::SIZE>(key)) * 16 + (mine & 3) * 4);
-                        if (odd && !is_finite(v)) v = 0.0f;
+                        const float v = *reinterpret_cast<const float*>(
+                            s_v + key * S::ROW + half * 4 * S::ROW +
+                            ((d * 8 + mine / 4) ^ value_swizzle<CHUNKS, 4>(4 * half + (e & 3))) * 16 + mine % 4 * 4);
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[u][e], o[d], 0, 0, 0);
                     }
                 }
             }
-            while (odd) {
-                const int at = __builtin_ctz(odd);
-                odd &= odd - 1;
-                if (!seen(u, at)) continue;
-                const int key = u * 32 + at;
+        }
+    }
+    if (tile0 < tile_end && uniform(s_odd)) {
+        // values that are not finite, in tiles that some row does not see all of
+#pragma unroll 1
+        for (int t = tile0; t < tile_end; ++t) {
+            if (!partly_seen(t, look_up(t).bad)) continue;
+#pragma unroll 1
+            for (int i = 0; i < SUBS * 32; ++i) {
+                const int key = t * KEYS + kw * SUBS * 32 + i;
+                if (key >= hi) break;
+                const uint32_t at = divided((uint32_t)key, p.size);
+                const int id = uniform(table[at]);
+                if ((uint32_t)id >= (uint32_t)a.c.pages) continue;
+                const T* v = reinterpret_cast<const T*>(v_head) + id * a.c.v_page + (key - (int64_t)at * p.size.d) * a.c.v_token;
+                const bool seen = key <= limit && key >= low;
 #pragma unroll
                 for (int d = 0; d < DTILES; ++d)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int x = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
-                        const T v = *reinterpret_cast<const T*>(s_v + key * S::ROW +
-                                                                ((x / VEC) ^ value_swizzle<CHUNKS, S::SIZE>(key)) * 16 + x % VEC * S::SIZE);
-                        if (!is_finite(v)) o[d][e] += (float)v;
+                        const float w = x < dim ? (float)v[x] : 0.0f;
+                        if (seen && !is_finite(w)) o[d][e] += w;
+                        __builtin_amdgcn_sched_barrier(0);   // rare: in few registers
                     }
             }
         }
@@ -686,7 +746,9 @@ hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStrea
         p.keys = s.keys;
         p.target = s.target;
         p.slots = (int)s.slots;
-        p.direct = bits % 16 == 0;
+        const int move_rows = 1024 / (s.dp * size);
+        const bool near = (a.c.k_token | a.c.v_token) < (int64_t)1 << 25;   // distances within a move are 32-bit
+        p.even = bits % 16 == 0 && near && a.c.page_size % move_rows == 0;
         p.sums = static_cast<float*>(workspace);
         p.stats = p.sums + (s.target ? s.slots * a.c.heads * s.rows * s.dp : 0);
         hipError_t e;
