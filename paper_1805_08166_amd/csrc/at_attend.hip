@@ -71,12 +71,13 @@ struct Mat<AT_F32> {
 // How a call is laid out; the same for both kernels.
 struct Plan {
     Divider size;        // of a page
-    int group;           // G, query heads of a cache head
+    Divider group;       // G, query heads of a cache head
     int rows;            // of a tile
     int keys;            // of a tile
     int target;          // pieces a head that the keys are cut into, about; 0: whole sequences
     int slots;           // pieces a head, at most
-    int even;            // rows of the cache are whole aligned 16 bytes, and those of a move lie in one page
+    int direct;          // rows of the cache are whole aligned 16 bytes
+    int even;            // and those of a move lie in one page
     float* sums;         // [slot][head][row][dim padded]
     float* stats;        // [slot][head][row][2]: maximum and sum
 };
@@ -96,7 +97,7 @@ __device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int 
     const int64_t room = a.c.width * a.c.page_size, l = a.c.lengths[b];
     t.position = l - s.count;
     t.length = (int)(l < 0 ? 0 : l < room ? l : room);
-    t.row_tiles = (int)(((int64_t)s.count * p.group + p.rows - 1) / p.rows);
+    t.row_tiles = (int)(((uint32_t)s.count * p.group.d + p.rows - 1) / p.rows);   // fewer than 2^31 rows, tiles of at most 128
     int64_t lo = a.window > 0 ? t.position - a.window + 1 : 0;
     lo = lo < 0 ? 0 : lo < t.length ? lo : t.length;
     t.lo = (int)(lo / p.keys);
@@ -139,7 +140,10 @@ __device__ __forceinline__ int pieces_of(const Task& t, int tiles) {
 template <int DT_, int DP_, int ROW_WAVES_, int KEY_WAVES_>
 struct Shape {
     static constexpr int DT = DT_, DP = DP_;
-    static constexpr int ROW_WAVES = ROW_WAVES_, KEY_WAVES = KEY_WAVES_, WAVES = ROW_WAVES * KEY_WAVES;
+    // Heads above 128 are halved by columns of the output: two waves compute the same weights, each for its half of the
+    // values, as one wave's registers do not hold the queries and all of the output.
+    static constexpr int COL_WAVES = DP > 128 ? 2 : 1, COLS = DP / COL_WAVES;
+    static constexpr int ROW_WAVES = ROW_WAVES_, KEY_WAVES = KEY_WAVES_, WAVES = ROW_WAVES * KEY_WAVES * COL_WAVES;
     static constexpr int THREADS = WAVES * 64;
     static constexpr int SIZE = sizeof(typename Elem<DT>::T), VEC = 16 / SIZE;
     static constexpr int CHUNKS = DP / VEC;            // of 16 bytes in a row
@@ -152,7 +156,7 @@ struct Shape {
     static constexpr int MOVE_ROWS = 64 / CHUNKS;
     static constexpr int IDS = KEYS > 64 ? 2 : 1;      // words of a lane that hold a tile's page numbers
     static constexpr int WAVES_EU = ROW <= 256 ? 2 : 1;
-    static constexpr int OUT_LD = DP + 4;
+    static constexpr int OUT_LD = COLS + 4;
     static constexpr int JOIN = KEY_WAVES > 1 ? WAVES * 32 * OUT_LD * 4 : 0;
     static constexpr int LDS = 4 * TILE > JOIN ? 4 * TILE : JOIN;
     static_assert(MOVES >= 1 && CHUNKS <= 64, "whole moves");
@@ -177,6 +181,14 @@ __device__ __forceinline__ short4v read_transposed(const char* p) {
         (__attribute__((address_space(3))) short4v*)(__attribute__((address_space(3))) char*)p);
 }
 
+// f of the values of lanes i and i + 32, in both.
+template <class F>
+__device__ __forceinline__ float halves(float v, F&& f) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    const uint32_t low = r[0], high = r[1];
+    return f(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
+}
 // A value that all lanes have, as the compiler cannot tell.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -192,17 +204,18 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     using T = typename Elem<DT>::T;
     using M = Mat<DT>;
     using Frag = typename M::Frag;
-    constexpr int VEC = S::VEC, SUBS = S::SUBS, KEYS = S::KEYS, CHUNKS = S::CHUNKS, DTILES = DP / 32;
-    extern __shared__ char s_tiles[];          // [2][keys, values][KEYS][DP]
+    constexpr int VEC = S::VEC, SUBS = S::SUBS, KEYS = S::KEYS, CHUNKS = S::CHUNKS, COLS = S::COLS, DTILES = COLS / 32;
+    extern __shared__ __attribute__((aligned(1024))) char s_tiles[];   // [2][keys, values][KEYS][DP]
     __shared__ int64_t s_scratch[S::WAVES];
     __shared__ int s_place[2], s_odd;
     __shared__ float s_stats[S::WAVES][32][2];
+    __shared__ __attribute__((aligned(16))) float s_fix[S::WAVES][COLS];   // values of a key that are not finite
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, mine = lane & 31;
-    const int rw = wave % RW, kw = wave / RW;
+    const int rw = wave % RW, kw = wave / RW % KW, col0 = wave / (RW * KW) * COLS;
     const int heads = (int)a.c.heads, head = blockIdx.x % heads, slot = blockIdx.x / heads;
 
     // Which sequence, tile of rows and piece of keys.
-    const int tiles = piece_tiles<S::THREADS>(a, p, s_scratch);
+    const int tiles = uniform(piece_tiles<S::THREADS>(a, p, s_scratch));
     {
         if (threadIdx.x == 0) {
             s_place[0] = -1;
@@ -246,10 +259,10 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int row_tile = task.row_tiles - 1 - in_task / pieces;   // a prompt's longest first
 
     // Rows of this workgroup, and the keys that they see.
-    const int G = p.group;
-    const int64_t row0 = (int64_t)row_tile * S::ROWS, all_rows = (int64_t)task.count * G;
-    const int rows = (int)(all_rows - row0 < S::ROWS ? all_rows - row0 : S::ROWS);
-    const int64_t first_pos = task.position + row0 / G, last_pos = task.position + (row0 + rows - 1) / G;
+    const int G = p.group.d, row0 = row_tile * S::ROWS, all_rows = task.count * G;
+    const int rows = all_rows - row0 < S::ROWS ? all_rows - row0 : S::ROWS;
+    auto token_of_row = [&](int r) { return (int)divided((uint32_t)r, p.group); };   // within the sequence
+    const int64_t first_pos = task.position + token_of_row(row0), last_pos = task.position + token_of_row(row0 + rows - 1);
     const int64_t window = a.window > 0 ? a.window : (int64_t)1 << 40;
     int64_t lo = first_pos - window + 1, hi64 = last_pos + 1;   // positions [lo, hi)
     lo = lo < 0 ? 0 : lo;
@@ -264,10 +277,14 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
 
     // Page numbers of a tile, one a lane, from that of its first position on.
     const int32_t* table = a.c.table + b * a.c.table_ld;
-    const int used_pages = (int)divided((uint32_t)(hi + p.size.d - 1 < hi ? hi : hi + p.size.d - 1), p.size);   // pages below hi
+    const uint32_t pages = (uint32_t)a.c.pages;
+    const int used_pages = hi > 0 ? (int)divided((uint32_t)hi - 1, p.size) + 1 : 0;   // with positions below hi
     struct Ids {
         int v[S::IDS];
-        uint64_t bad[S::IDS];   // those that are not there
+    };
+    struct Bad {   // those that are not there
+        uint64_t v[S::IDS];
+        __device__ bool any() const { return S::IDS > 1 ? (v[0] | v[S::IDS - 1]) != 0 : v[0] != 0; }
     };
     auto look_up = [&](int t) {
         Ids r;
@@ -276,39 +293,67 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         for (int i = 0; i < S::IDS; ++i) {
             const int at = first + i * 64 + lane;
             r.v[i] = at < used_pages ? table[at] : 0;
-            r.bad[i] = __ballot((uint32_t)r.v[i] >= (uint32_t)a.c.pages && at < used_pages);
         }
         return r;
     };
-    // A tile into LDS, a KB a move: even: all rows of a move lie in one page, whose address is the wave's.
+    auto bad_of = [&](int t, const Ids& ids) {
+        Bad r;
+        const int first = (int)divided((uint32_t)(t * KEYS), p.size);
+#pragma unroll
+        for (int i = 0; i < S::IDS; ++i) r.v[i] = __ballot((uint32_t)ids.v[i] >= pages && first + i * 64 + lane < used_pages);
+        return r;
+    };
+    auto id_of = [&](const Ids& ids, uint32_t at) {   // the `at`-th of a tile's page numbers
+        return (uint32_t)__builtin_amdgcn_readlane(S::IDS > 1 && at >= 64 ? ids.v[S::IDS - 1] : ids.v[0], at & 63);
+    };
+    // A tile into LDS, a KB a move.
     constexpr int MOVES = S::MOVES, MOVE_ROWS = S::MOVE_ROWS;
     const int dim = (int)a.c.dim;
     const char* k_head = static_cast<const char*>(a.c.k) + (int64_t)head * a.c.k_head * S::SIZE;
     const char* v_head = static_cast<const char*>(a.c.v) + (int64_t)head * a.c.v_head * S::SIZE;
     const int lane_row = lane / CHUNKS, lane_chunk = lane % CHUNKS;
     const uint32_t k_lane = (uint32_t)(lane_row * a.c.k_token * S::SIZE), v_lane = (uint32_t)(lane_row * a.c.v_token * S::SIZE);
-    auto stage = [&](int t, int buf, const Ids& ids) {
-        char* to_k = s_tiles + buf * 2 * S::TILE + wave * MOVES * 1024;
+    auto stage = [&](int t, char* to, const Ids& ids) {
+        char* to_k = to + wave * MOVES * 1024;
         char* to_v = to_k + S::TILE;
         const int first = (int)divided((uint32_t)(t * KEYS), p.size);
-        if (p.even) {
+        if (DP > 128 || p.direct) {
+            const int row0_ = wave * MOVES * MOVE_ROWS;
+            // The place of a position that lies in page `id`, an address that the wave has.
+            auto place_of = [&](const char* head, int64_t page_step, int64_t token_step, uint32_t id, int pos, uint32_t at) {
+                const uint64_t x = (uint64_t)head + (id * (uint64_t)page_step + (pos - at * p.size.d) * (uint64_t)token_step) * S::SIZE;
+                uint32_t low = uniform((int)x), high = uniform((int)(x >> 32));
+                asm("" : "+s"(low), "+s"(high));   // or each move's lanes would keep an address of their own
+                return reinterpret_cast<const char*>((uint64_t)high << 32 | low);
+            };
+            if (p.even && dim == DP && hi - t * KEYS >= KEYS && !bad_of(t, ids).any()) {
 #pragma unroll
-            for (int q = 0; q < MOVES; ++q) {
-                const int row0_ = (wave * MOVES + q) * MOVE_ROWS, pos = t * KEYS + row0_;
-                const int at = (int)divided((uint32_t)pos, p.size) - first;
-                const int id = __builtin_amdgcn_readlane(S::IDS > 1 && at >= 64 ? ids.v[S::IDS - 1] : ids.v[0], at & 63);
-                const int row = row0_ + lane_row;
-                const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row)) * 16, cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * 16;
-                const int64_t place = pos - (int64_t)(at + first) * p.size.d;
-                if ((uint32_t)id < (uint32_t)a.c.pages && pos + lane_row < hi) {
-                    const char* k = k_head + (id * a.c.k_page + place * a.c.k_token) * S::SIZE;
-                    const char* v = v_head + (id * a.c.v_page + place * a.c.v_token) * S::SIZE;
-                    // (the moves of lanes past dim are left out: zeros lie there)
-                    if (DP == dim || (int)ck < dim * S::SIZE) __builtin_amdgcn_global_load_lds(k + (k_lane + ck), to_k + q * 1024, 16, 0, 0);
-                    if (DP == dim || (int)cv < dim * S::SIZE) __builtin_amdgcn_global_load_lds(v + (v_lane + cv), to_v + q * 1024, 16, 0, 0);
-                } else {
-                    *reinterpret_cast<float4v*>(to_k + q * 1024 + lane * 16) = float4v{};
-                    *reinterpret_cast<float4v*>(to_v + q * 1024 + lane * 16) = float4v{};
+                for (int q = 0; q < MOVES; ++q) {
+                    // all rows of the move are there, in one page
+                    const int row = row0_ + q * MOVE_ROWS, pos = t * KEYS + row;
+                    const uint32_t at = divided((uint32_t)pos, p.size), id = id_of(ids, at - first);
+                    const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row + lane_row)) * 16;
+                    const uint32_t cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row + lane_row)) * 16;
+                    __builtin_amdgcn_global_load_lds(place_of(k_head, a.c.k_page, a.c.k_token, id, pos, at) + (k_lane + ck), to_k + q * 1024, 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds(place_of(v_head, a.c.v_page, a.c.v_token, id, pos, at) + (v_lane + cv), to_v + q * 1024, 16, 0, 0);
+                }
+            } else {
+                // row by row, with zeros for those that are not there (past dim, zeros lie in LDS already)
+#pragma unroll 1
+                for (int i = 0; i < MOVES * MOVE_ROWS; ++i) {
+                    const int q = i / MOVE_ROWS, row = row0_ + i, pos = t * KEYS + row;
+                    const uint32_t at = divided((uint32_t)pos, p.size), id = id_of(ids, at - first);
+                    const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row)) * 16, cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * 16;
+                    if (lane_row != i % MOVE_ROWS) continue;
+                    if (pos < hi && id < pages) {
+                        const char* k = place_of(k_head, a.c.k_page, a.c.k_token, id, pos, at);
+                        const char* v = place_of(v_head, a.c.v_page, a.c.v_token, id, pos, at);
+                        if ((int)ck < dim * S::SIZE) __builtin_amdgcn_global_load_lds(k + ck, to_k + q * 1024, 16, 0, 0);
+                        if ((int)cv < dim * S::SIZE) __builtin_amdgcn_global_load_lds(v + cv, to_v + q * 1024, 16, 0, 0);
+                    } else {
+                        *reinterpret_cast<float4v*>(to_k + q * 1024 + lane * 16) = float4v{};
+                        *reinterpret_cast<float4v*>(to_v + q * 1024 + lane * 16) = float4v{};
+                    }
                 }
             }
         } else {
@@ -317,7 +362,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                 const int row = (wave * MOVES + q) * MOVE_ROWS + lane_row, pos = t * KEYS + row;
                 const uint32_t at = divided((uint32_t)pos, p.size);
                 const int id = pos < hi ? table[at] : -1;
-                const bool there = (uint32_t)id < (uint32_t)a.c.pages;
+                const bool there = (uint32_t)id < pages;
                 const int64_t place = there ? pos - (int64_t)at * p.size.d : 0, page = there ? id : 0;
                 const T* k = reinterpret_cast<const T*>(k_head) + page * a.c.k_page + place * a.c.k_token;
                 const T* v = reinterpret_cast<const T*>(v_head) + page * a.c.v_page + place * a.c.v_token;
@@ -334,39 +379,34 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
             }
         }
     };
-    if (p.even && dim < DP) {
+    if (p.direct && dim < DP) {
         for (int i = threadIdx.x; i < 4 * S::TILE / 16; i += S::THREADS) reinterpret_cast<float4v*>(s_tiles)[i] = float4v{};
         __syncthreads();
     }
-    Ids here = {}, next = {};
+    Ids here = {}, next = {};   // of this tile and the next one
     if (tile < tile_end) {
         here = look_up(tile);
-        stage(tile, 0, here);
+        stage(tile, s_tiles, here);
         if (tile + 1 < tile_end) next = look_up(tile + 1);
     }
 
     // This lane's row: its queries, and the positions that it sees.
     const int row = rw * 32 + mine;
     const bool real = row < rows;
-    const int64_t r = row0 + (real ? row : rows - 1);
-    const int token = task.first + (int)(r / G), q_head = head * G + (int)(r % G);
-    const int64_t position = task.position + r / G;
+    const int r = row0 + (real ? row : rows - 1), nth = token_of_row(r);
+    const int token = task.first + nth, q_head = head * G + r - nth * G;
+    const int64_t position = task.position + nth;
     // [low, limit] within the tiles' positions, which are below 2^31
     const int limit = position < 0 ? -1 : (int)(position < hi ? position : hi - 1), low = (int)(position - window + 1 > 0 ? position - window + 1 : 0);
     // of a row's position: the last position it sees, and the first
     auto limit_of = [&](int64_t at) { return uniform(at < 0 ? -1 : (int)(at < hi ? at : hi - 1)); };
     auto low_of = [&](int64_t at) { return uniform((int)(at - window + 1 > 0 ? at - window + 1 : 0)); };
     const int wave_first = rw * 32 < rows ? rw * 32 : rows - 1, wave_last = rw * 32 + 31 < rows ? rw * 32 + 31 : rows - 1;
-    const int64_t wave_from = task.position + (row0 + wave_first) / G, wave_to = task.position + (row0 + wave_last) / G;
+    const int64_t wave_from = task.position + token_of_row(row0 + wave_first), wave_to = task.position + token_of_row(row0 + wave_last);
     const int limit_min = limit_of(wave_from), limit_max = limit_of(wave_to), low_max = low_of(wave_to);
     // Whether some row of this workgroup does not see all of a tile.
     const int all_limit = limit_of(first_pos), all_low = low_of(last_pos);
-    auto partly_seen = [&](int t, const uint64_t (&bad)[S::IDS]) {
-        bool any = t * KEYS + KEYS - 1 > all_limit || t * KEYS < all_low;
-#pragma unroll
-        for (int i = 0; i < S::IDS; ++i) any |= bad[i] != 0;
-        return any;
-    };
+    auto partly_seen = [&](int t, const Bad& bad) { return t * KEYS + KEYS - 1 > all_limit || t * KEYS < all_low || bad.any(); };
     constexpr int STEPS = CHUNKS / 2;
     Frag q[STEPS];
     {
@@ -396,84 +436,87 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int k_at = mine * S::ROW + ((half ^ key_swizzle<CHUNKS>(mine)) * 16);
     const int tr_row = 4 * half + (lane & 15) / 4, tr_chunk = (lane >> 4 & 1) * 2 + (lane >> 1 & 1), tr_byte = (lane & 1) * 8;
     const int tile0 = tile;
-    int buf = 0;
-    for (; tile < tile_end; ++tile, buf ^= 1) {
-        // this tile has landed, and everyone is done with the last one
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        uint64_t bad[S::IDS];
-#pragma unroll
-        for (int i = 0; i < S::IDS; ++i) bad[i] = here.bad[i];
-        if (partly_seen(tile, bad)) {
-            // A NaN or an infinity among the values must not reach, as 0 times it, a row that does not see it: it is
-            // left out here, by the lane that moved it, and added at the end where it is seen.
-            char* own = s_tiles + buf * 2 * S::TILE + S::TILE + wave * MOVES * 1024 + lane * 16;
-#pragma unroll 1
-            for (int q = 0; q < MOVES; ++q, own += 1024) {
-                Pack<T, VEC> w = *reinterpret_cast<const Pack<T, VEC>*>(own);
-                bool fine = true;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const bool f = is_finite(w.v[e]);
-                    fine &= f;
-                    w.v[e] = f ? w.v[e] : (T)0.0f;
-                }
-                if (!fine) {
-                    *reinterpret_cast<Pack<T, VEC>*>(own) = w;
-                    s_odd = 1;
-                }
-            }
-        }
-        __syncthreads();
+    // Products of a tile with this wave's rows, while the next one moves into the other buffer: the two lie apart, or the
+    // compiler would wait for the moves before it reads.
+    auto step = [&](const char* __restrict__ from, char* __restrict__ to, const Bad& bad) {
         if (tile + 1 < tile_end) {
+            stage(tile + 1, to, next);
             here = next;
-            stage(tile + 1, buf ^ 1, here);
             if (tile + 2 < tile_end) next = look_up(tile + 2);
         }
         const int key0 = tile * KEYS + kw * SUBS * 32;
-        if (rw * 32 >= rows || key0 > limit_max) continue;
-        const char* s_k = s_tiles + buf * 2 * S::TILE + kw * SUBS * 32 * S::ROW;
+        if (rw * 32 >= rows || key0 > limit_max) return;
+        const char* s_k = from + kw * SUBS * 32 * S::ROW;
         const char* s_v = s_k + S::TILE;
+        // Fragments are read AHEAD steps before the products that use them; other work may move between, reads and products not.
+        constexpr int ORDERED = 0x2 | 0x4;   // vector and scalar arithmetic may cross
         float16v sc[SUBS];
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[u][e] = 0.0f;
+        constexpr int AHEAD = 1;
+        Frag k[AHEAD + 1][SUBS];
+        auto read_keys = [&](int s) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int u = 0; u < SUBS; ++u) {
-                const Frag k = *reinterpret_cast<const Frag*>(s_k + (k_at ^ s * 32) + u * 32 * S::ROW);
-                sc[u] = M::mma(k, q[s], sc[u]);
-            }
-        uint32_t gone[SUBS] = {};   // keys whose page is not there
-        bool any_bad = false;
-#pragma unroll
-        for (int i = 0; i < S::IDS; ++i) any_bad |= bad[i] != 0;
-        auto seen = [&](int u, int at) {   // whether this row sees key `at` of the 32
-            const int key = key0 + u * 32 + at;
-            return key <= limit && key >= low && !(gone[u] >> at & 1);
+            for (int u = 0; u < SUBS; ++u)
+                k[s % (AHEAD + 1)][u] = *reinterpret_cast<const Frag*>(s_k + (k_at ^ s * 32) + u * 32 * S::ROW);
         };
-        if (key0 + SUBS * 32 - 1 > limit_min || key0 < low_max || any_bad) {
-            if (any_bad) {
+#pragma unroll
+        for (int s = 0; s < AHEAD && s < STEPS; ++s) read_keys(s);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (s + AHEAD < STEPS) read_keys(s + AHEAD);
+            __builtin_amdgcn_sched_barrier(ORDERED);
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) sc[u] = M::mma(k[s % (AHEAD + 1)][u], q[s], sc[u]);
+            __builtin_amdgcn_sched_barrier(ORDERED);
+        }
+        // 16-bit values: groups of 16 keys, all columns, one group ahead.
+        constexpr int GROUPS = 2 * SUBS, ROWS_V = S::SIZE == 2 ? DTILES : 1;
+        Frag v[2][ROWS_V];
+        auto read_values = [&](int g) {
+            if constexpr (S::SIZE == 2) {
+#pragma unroll
+                for (int d = 0; d < DTILES; ++d) {
+                    union {
+                        short4v part[2];
+                        Frag whole;
+                    } w;
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        w.part[n] = read_transposed(s_v + (g * 16 + 8 * n) * S::ROW + tr_row * S::ROW +
+                                                    ((col0 / 8 + d * 4 + tr_chunk) ^ value_swizzle<CHUNKS, 2>(tr_row)) * 16 + tr_byte);
+                    v[g & 1][d] = w.whole;
+                }
+            }
+        };
+        read_values(0);
+        __builtin_amdgcn_sched_barrier(ORDERED);
+        if (key0 + SUBS * 32 - 1 > limit_min || key0 < low_max || bad.any()) {
+            uint32_t gone[SUBS] = {};   // keys whose page is not there
+            if (bad.any()) {
                 const uint32_t first = divided((uint32_t)(tile * KEYS), p.size);
 #pragma unroll
                 for (int u = 0; u < SUBS; ++u) {
                     const uint32_t at = divided((uint32_t)(key0 + u * 32 + mine), p.size) - first;
-                    gone[u] = (uint32_t)__ballot((S::IDS > 1 && at >= 64 ? bad[S::IDS - 1] : bad[0]) >> (at & 63) & 1);
+                    gone[u] = (uint32_t)__ballot((S::IDS > 1 && at >= 64 ? bad.v[S::IDS - 1] : bad.v[0]) >> (at & 63) & 1);
                 }
             }
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (!seen(u, 8 * (e >> 2) + 4 * half + (e & 3))) sc[u][e] = -inf;
+                for (int e = 0; e < 16; ++e) {
+                    const int at = 8 * (e >> 2) + 4 * half + (e & 3), key = key0 + u * 32 + at;
+                    if (key > limit || key < low || (gone[u] >> at & 1)) sc[u][e] = -inf;
+                }
         }
         float most = sc[0][0];
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, sc[u][e]);
-        most = fmaxf(most, __shfl_xor(most, 32));
+        most = halves(most, [](float x, float y) { return fmaxf(x, y); });
         if (__any(most > top)) {
             const float over = fmaxf(top, most);
             const float f = top == -inf ? 0.0f : __builtin_amdgcn_exp2f((top - over) * scale);
@@ -493,75 +536,103 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                 sc[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][e], scale, -base));
                 sum += sc[u][e];
             }
+        if constexpr (S::SIZE == 2) {
 #pragma unroll
-        for (int u = 0; u < SUBS; ++u) {
-            if constexpr (S::SIZE == 2) {
+            for (int g = 0; g < GROUPS; ++g) {
+                if (g + 1 < GROUPS) read_values(g + 1);
+                __builtin_amdgcn_sched_barrier(ORDERED);
+                Frag w;
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    Frag w;
+                for (int e = 0; e < 8; ++e) w[e] = (T)sc[g / 2][8 * (g & 1) + e];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = (T)sc[u][8 * s + e];
+                for (int d = 0; d < DTILES; ++d) o[d] = M::mma(v[g & 1][d], w, o[d]);
+                __builtin_amdgcn_sched_barrier(ORDERED);
+            }
+        } else {
 #pragma unroll
-                    for (int d = 0; d < DTILES; ++d) {
-                        union {
-                            short4v part[2];
-                            Frag whole;
-                        } v;
-#pragma unroll
-                        for (int n = 0; n < 2; ++n)
-                            v.part[n] = read_transposed(s_v + (u * 32 + 16 * s + 8 * n) * S::ROW + tr_row * S::ROW +
-                                                        ((d * 4 + tr_chunk) ^ value_swizzle<CHUNKS, 2>(tr_row)) * 16 + tr_byte);
-                        o[d] = M::mma(v.whole, w, o[d]);
-                    }
-                }
-            } else {
+            for (int u = 0; u < SUBS; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int key = u * 32 + 8 * (e >> 2) + (e & 3);   // and four on in the other half, whose chunks are swizzled
 #pragma unroll
                     for (int d = 0; d < DTILES; ++d) {
-                        const float v = *reinterpret_cast<const float*>(
+                        const float x = *reinterpret_cast<const float*>(
                             s_v + key * S::ROW + half * 4 * S::ROW +
-                            ((d * 8 + mine / 4) ^ value_swizzle<CHUNKS, 4>(4 * half + (e & 3))) * 16 + mine % 4 * 4);
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[u][e], o[d], 0, 0, 0);
+                            ((col0 / 4 + d * 8 + mine / 4) ^ value_swizzle<CHUNKS, 4>(4 * half + (e & 3))) * 16 + mine % 4 * 4);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sc[u][e], o[d], 0, 0, 0);
                     }
+                }
+        }
+    };
+    char* from = s_tiles;
+    char* to = s_tiles + 2 * S::TILE;
+    for (; tile < tile_end; ++tile) {
+        // this tile has landed, and everyone is done with the last one
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        const Bad bad = bad_of(tile, here);
+        if (partly_seen(tile, bad)) {
+            // A NaN or an infinity among the values must not reach, as 0 times it, a row that does not see it: it is
+            // left out here, by the lane that moved it, and added at the end where it is seen.
+            char* own = from + S::TILE + wave * MOVES * 1024 + lane * 16;
+#pragma unroll 1
+            for (int q = 0; q < MOVES; ++q, own += 1024) {
+                Pack<T, VEC> w = *reinterpret_cast<const Pack<T, VEC>*>(own);
+                bool fine = true;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const bool f = is_finite(w.v[e]);
+                    fine &= f;
+                    w.v[e] = f ? w.v[e] : (T)0.0f;
+                }
+                if (!fine) {
+                    *reinterpret_cast<Pack<T, VEC>*>(own) = w;
+                    s_odd = 1;
                 }
             }
         }
+        __syncthreads();
+        step(from, to, bad);
+        char* t = from;
+        from = to;
+        to = t;
     }
     if (tile0 < tile_end && uniform(s_odd)) {
         // values that are not finite, in tiles that some row does not see all of
 #pragma unroll 1
         for (int t = tile0; t < tile_end; ++t) {
-            if (!partly_seen(t, look_up(t).bad)) continue;
+            if (!partly_seen(t, bad_of(t, look_up(t)))) continue;
 #pragma unroll 1
             for (int i = 0; i < SUBS * 32; ++i) {
                 const int key = t * KEYS + kw * SUBS * 32 + i;
                 if (key >= hi) break;
                 const uint32_t at = divided((uint32_t)key, p.size);
                 const int id = uniform(table[at]);
-                if ((uint32_t)id >= (uint32_t)a.c.pages) continue;
+                if ((uint32_t)id >= pages) continue;
                 const T* v = reinterpret_cast<const T*>(v_head) + id * a.c.v_page + (key - (int64_t)at * p.size.d) * a.c.v_token;
                 const bool seen = key <= limit && key >= low;
+#pragma unroll 1
+                for (int x = lane; x < COLS; x += 64) {   // 0 in the place of finite ones
+                    const float w = col0 + x < dim ? (float)v[col0 + x] : 0.0f;
+                    s_fix[wave][x] = is_finite(w) ? 0.0f : w;
+                }
 #pragma unroll
                 for (int d = 0; d < DTILES; ++d)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int x = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
-                        const float w = x < dim ? (float)v[x] : 0.0f;
-                        if (seen && !is_finite(w)) o[d][e] += w;
+                    for (int g = 0; g < 4; ++g) {
+                        const float4v w = *reinterpret_cast<const float4v*>(&s_fix[wave][32 * d + 8 * g + 4 * half]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[d][4 * g + e] += seen ? w[e] : 0.0f;
                         __builtin_amdgcn_sched_barrier(0);   // rare: in few registers
                     }
             }
         }
     }
-    sum += __shfl_xor(sum, 32);
+    sum = halves(sum, [](float x, float y) { return x + y; });
 
     // Out: rows of this workgroup, whole, or this piece's sums.
     const bool whole = pieces == 1;
     const int64_t rows_at = ((int64_t)slot * heads + head) * S::ROWS;   // of the pieces
     auto put = [&](int row_, int d, float4v v, float top_, float sum_) {   // four values from column d on
-        const int64_t r_ = row0 + row_;
         if (!whole) {
             *reinterpret_cast<float4v*>(p.sums + (rows_at + row_) * DP + d) = v;
             if (d == 0) {
@@ -570,7 +641,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
             }
             return;
         }
-        const int64_t token_ = task.first + r_ / G, head_ = head * G + r_ % G;
+        const int nth_ = token_of_row(row0 + row_);
+        const int64_t token_ = task.first + nth_, head_ = head * G + row0 + row_ - nth_ * G;
         const float f = sum_ == 0.0f ? 0.0f : 1.0f / sum_;   // a NaN stays one
         T* y = static_cast<T*>(a.out.p) + token_ * a.out.token + head_ * a.out.head + d;
         if (d + 4 <= dim) {
@@ -592,7 +664,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         for (int d = 0; d < DTILES; ++d)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                put(row, 32 * d + 8 * g + 4 * half, float4v{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]}, top, sum);
+                put(row, col0 + 32 * d + 8 * g + 4 * half, float4v{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]}, top, sum);
     } else {
         // the waves' sums over their keys, joined in order
         __syncthreads();
@@ -609,7 +681,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         }
         __syncthreads();
         for (int i = threadIdx.x; i < rows * (DP / 4); i += S::THREADS) {
-            const int row_ = i / (DP / 4), d = i % (DP / 4) * 4, w0 = row_ / 32;
+            const int row_ = i / (DP / 4), d = i % (DP / 4) * 4, w0 = row_ / 32 + d / COLS * RW * KW;
             float most = -inf;
 #pragma unroll
             for (int w = 0; w < KW; ++w) most = fmaxf(most, s_stats[w * RW + w0][row_ & 31][0]);
@@ -619,7 +691,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
             for (int w = 0; w < KW; ++w) {
                 const float t = s_stats[w * RW + w0][row_ & 31][0], f = t == -inf ? 0.0f : __builtin_amdgcn_exp2f((t - most) * scale);
                 total += s_stats[w * RW + w0][row_ & 31][1] * f;
-                const float4v x = *reinterpret_cast<const float4v*>(&s_out[((w * RW + w0) * 32 + (row_ & 31)) * S::OUT_LD + d]);
+                const float4v x = *reinterpret_cast<const float4v*>(&s_out[((w * RW + w0) * 32 + (row_ & 31)) * S::OUT_LD + d % COLS]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += x[e] * f;
             }
@@ -651,10 +723,10 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a, Plan p, int dp) {
     const float inf = __builtin_inff(), scale = a.scale * LOG2E;
     const int dim = (int)a.c.dim, heads = (int)a.c.heads;
     for (int q_head = blockIdx.y * 4 + wave; q_head < a.q_heads; q_head += gridDim.y * 4) {
-        const int64_t r = (int64_t)(token - task.first) * p.group + q_head % p.group;
+        const int G = p.group.d, head = (int)divided((uint32_t)q_head, p.group), r = (token - task.first) * G + q_head - head * G;
         const int64_t slot0 = before + (int64_t)(task.row_tiles - 1 - r / p.rows) * pieces;
         if (slot0 + pieces > p.slots) return;   // starts that do not go up
-        const int64_t at0 = (slot0 * heads + q_head / p.group) * p.rows + r % p.rows, step = (int64_t)heads * p.rows;
+        const int64_t at0 = (slot0 * heads + head) * p.rows + r % p.rows, step = (int64_t)heads * p.rows;
         float top = -inf;
         for (int k = lane; k < pieces; k += 64) top = fmaxf(top, p.stats[(at0 + k * step) * 2]);
 #pragma unroll
@@ -694,7 +766,7 @@ Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int
     s.dp = padded(dim);
     const int row = s.dp * elem_size(type);
     s.few = n * G <= 32 * (batch < n ? batch : n);
-    s.rows = s.few ? 32 : 128;
+    s.rows = s.few ? 32 : s.dp > 128 ? 64 : 128;
     s.keys = s.few ? (row <= 256 ? 128 : row <= 512 ? 64 : 32) : row <= 512 ? 64 : 32;
     const int64_t most = batch < n ? batch : n;               // sequences with new tokens
     const int64_t units = std::min<int64_t>(n * G, n * G / s.rows + most);   // tiles of rows
@@ -719,11 +791,23 @@ hipError_t attend(const AttendArgs& a, const Plan& p, hipStream_t stream) {
 
 template <int DT, int DP>
 hipError_t attend_rows(const AttendArgs& a, const Plan& p, bool few, hipStream_t stream) {
-    constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), KW = ROW <= 256 ? 4 : ROW <= 512 ? 2 : 1;
-    return few ? attend<DT, DP, 1, KW>(a, p, stream) : attend<DT, DP, 4, 1>(a, p, stream);
+    constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), KW = ROW <= 256 ? 4 : ROW <= 512 ? 2 : 1, RW = DP > 128 ? 2 : 4;
+    return few ? attend<DT, DP, 1, KW>(a, p, stream) : attend<DT, DP, RW, 1>(a, p, stream);
 }
 
 }  // namespace
+
+namespace {
+// Rows of the cache are moved to LDS 16 aligned bytes at a time, and distances within a move are 32-bit.
+bool moves_directly(const at_paged& c) {
+    const int size = elem_size((int)c.type);
+    uintptr_t bits = reinterpret_cast<uintptr_t>(c.k) | reinterpret_cast<uintptr_t>(c.v);
+    for (int64_t d : {c.dim, c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head}) bits |= (uintptr_t)(d * size);
+    return bits % 16 == 0 && (c.k_token | c.v_token) < (int64_t)1 << 25;
+}
+}  // namespace
+
+bool paged_attention_takes(const at_paged& c) { return c.dim <= 128 || moves_directly(c); }
 
 int64_t paged_attention_workspace(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads, int64_t dim,
                                   int type) {
@@ -737,18 +821,16 @@ hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStrea
         constexpr int DT = type.value;
         const Sizes s = sizes_of(a.n, a.c.batch, a.c.width * a.c.page_size, a.q_heads, a.c.heads, a.c.dim, DT);
         const int size = elem_size(DT);
-        uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v);
-        for (int64_t d : {a.c.dim, a.c.k_page, a.c.k_token, a.c.k_head, a.c.v_page, a.c.v_token, a.c.v_head}) bits |= (uintptr_t)(d * size);
         Plan p;
         p.size = divider(a.c.page_size);
-        p.group = (int)(a.q_heads / a.c.heads);
+        p.group = divider(a.q_heads / a.c.heads);
         p.rows = s.rows;
         p.keys = s.keys;
         p.target = s.target;
         p.slots = (int)s.slots;
         const int move_rows = 1024 / (s.dp * size);
-        const bool near = (a.c.k_token | a.c.v_token) < (int64_t)1 << 25;   // distances within a move are 32-bit
-        p.even = bits % 16 == 0 && near && a.c.page_size % move_rows == 0;
+        p.direct = moves_directly(a.c);
+        p.even = a.c.page_size % move_rows == 0;
         p.sums = static_cast<float*>(workspace);
         p.stats = p.sums + (s.target ? s.slots * a.c.heads * s.rows * s.dp : 0);
         hipError_t e;

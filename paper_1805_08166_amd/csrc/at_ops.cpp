@@ -287,8 +287,8 @@ at_status at_paged_attention_workspace(int64_t n, int64_t batch, int64_t positio
     if (!type_ok(type)) return refuse(AT_E_INVALID, fn, "unknown element type");
     if (n < 0 || batch < 0 || positions < 0 || heads < 1 || q_heads < heads || q_heads % heads || dim < 1)
         return refuse(AT_E_INVALID, fn, "negative size, or query heads that are no multiple of the heads");
-    if (n > SIZE_MAX_31 || batch >= (int64_t)1 << 24 || q_heads > 65535 || dim > 256)
-        return refuse(AT_E_UNSUPPORTED, fn, "2^31 tokens, 2^24 sequences, 65536 heads or more than 256 values a head");
+    if (n > SIZE_MAX_31 || batch >= (int64_t)1 << 24 || q_heads > 65535 || n * q_heads > SIZE_MAX_31 || dim > 256)
+        return refuse(AT_E_UNSUPPORTED, fn, "2^24 sequences, 65536 heads, 2^31 of all tokens or more than 256 values a head");
     *bytes = paged_attention_workspace(n, batch, positions, q_heads, heads, dim, type);
     return AT_OK;
 }
@@ -300,8 +300,9 @@ at_status at_paged_attention(const at_paged* cache, const void* q, int64_t q_tok
     at_status st = paged_args(fn, cache);
     if (st != AT_OK) return st;
     if (n < 0) return refuse(AT_E_INVALID, fn, "negative size");
+    if (n > SIZE_MAX_31) return refuse(AT_E_UNSUPPORTED, fn, "2^31 tokens");
     if (q_heads < cache->heads || q_heads % cache->heads) return refuse(AT_E_INVALID, fn, "query heads are no multiple of the cache's");
-    if (n > SIZE_MAX_31 || q_heads > 65535) return refuse(AT_E_UNSUPPORTED, fn, "2^31 tokens or 65536 query heads");
+    if (q_heads > 65535 || n * q_heads > SIZE_MAX_31) return refuse(AT_E_UNSUPPORTED, fn, "65536 query heads, or 2^31 of all tokens");
     if (!std::isfinite(scale) || scale <= 0.0f) return refuse(AT_E_INVALID, fn, "scale must be positive and finite");
     if (window < 0) return refuse(AT_E_INVALID, fn, "negative window");
     if (q_token < 0 || q_head < 0 || o_token < 0 || o_head < 0) return refuse(AT_E_INVALID, fn, "negative stride");
@@ -311,6 +312,8 @@ at_status at_paged_attention(const at_paged* cache, const void* q, int64_t q_tok
     const int type = (int)cache->type;
     if (!aligned_t(q, type) || !aligned_t(out, type) || !aligned(lse, 4))
         return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
+    if (!paged_attention_takes(*cache))
+        return refuse(AT_E_UNSUPPORTED, fn, "heads above 128 values need a cache of whole, 16-byte aligned 16 bytes");
     st = workspace_args(fn, workspace, workspace_bytes,
                         paged_attention_workspace(n, cache->batch, cache->width * cache->page_size, q_heads, cache->heads, cache->dim, type));
     if (st != AT_OK) return st;

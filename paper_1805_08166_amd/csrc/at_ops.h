@@ -194,6 +194,7 @@ struct AttendArgs {
 };
 int64_t paged_attention_workspace(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads, int64_t dim,
                                   int type);
+bool paged_attention_takes(const at_paged& c);   // its heads and distances
 hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStream_t stream);
 
 struct AdjustArgs {

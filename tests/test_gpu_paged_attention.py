@@ -39,11 +39,31 @@ def check(P, R, x, scale=None, window=0, gone=None, **kw):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("dim", [1, 3, 16, 31, 32, 40, 64, 80, 100, 128, 192, 255, 256])
+@pytest.mark.parametrize("dim", [1, 3, 16, 31, 32, 40, 64, 80, 100, 127, 128, 136, 192, 248, 256])
 def test_head_sizes(P, R, kind, dim):
     """Single tokens and prompts, each head size of every padding, sizes that are no multiple of 16 bytes."""
     check(P, R, R.Batch(kind, [1, 1, 1], [0, 5, 300], 4, 2, dim, page=16, seed=dim))
     check(P, R, R.Batch(kind, [70, 1, 33], [0, 5, 200], 4, 2, dim, page=16, seed=dim + 1))
+
+
+@pytest.mark.parametrize("kind,dim", [("f32", 255), ("bf16", 255), ("f16", 132)])
+def test_large_heads_of_odd_rows_are_refused(P, R, kind, dim):
+    for new in ([1], [70]):
+        x = R.Batch(kind, new, [40], 4, 2, dim)
+        with pytest.raises(P.ATError) as e:
+            x.attend(P)
+        assert e.value.status == -2
+    x = R.Batch(kind, [1], [40], 4, 2, 192, spread="odd")
+    with pytest.raises(P.ATError):
+        x.attend(P)
+
+
+@pytest.mark.parametrize("page", [1, 3])
+def test_large_heads_in_odd_pages(P, R, page):
+    """Two rows of a move to LDS in different pages."""
+    for kind, dim in (("bf16", 256), ("f16", 160), ("f32", 192)):
+        check(P, R, R.Batch(kind, [1, 1], [300, 9], 4, 2, dim, page=page, seed=dim))
+        check(P, R, R.Batch(kind, [70, 3], [30, 100], 4, 2, dim, page=page, seed=dim))
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
@@ -57,7 +77,7 @@ def test_head_groups(P, R, kind, heads, kv):
 @pytest.mark.parametrize("spread", ["tokens", "heads", "odd"])
 def test_pages_and_layouts(P, R, page, spread):
     """Pages that end inside tiles, and every distance between pages, places and heads."""
-    for kind, dim in (("bf16", 64), ("f32", 48)):
+    for kind, dim in (("bf16", 64), ("f32", 48), ("bf16", 128)):
         check(P, R, R.Batch(kind, [1, 1, 1], [0, 257, 640], 8, 2, dim, page=page, spread=spread, seed=page))
         check(P, R, R.Batch(kind, [129, 65], [63, 0], 8, 2, dim, page=page, spread=spread, seed=page + 1))
 

@@ -75,6 +75,10 @@ REFUSED = [(f, dict(a), s) for f in (append, attend) for a, s in CACHE_REFUSED] 
     (attend, dict(window=-1), INVALID), (attend, dict(q=None), INVALID), (attend, dict(out=None), INVALID), (attend, dict(out=ODD), INVALID),
     (attend, dict(lse=P16 + 2), INVALID), (attend, dict(o_token=31), INVALID), (attend, dict(o_head=4), INVALID),
     (attend, dict(q_token=-1), INVALID),
+    # heads above 128 values, whose rows are not whole 16 bytes or do not lie at such addresses
+    (attend, dict(c_dim=132, c_k_head=132, c_k_token=264, c_v_head=132, c_v_token=264, q_head=132, q_token=528, o_head=132, o_token=528), UNSUPPORTED),
+    (attend, dict(c_dim=136, c_k_head=136, c_k_token=273, c_v_head=136, c_v_token=272, q_head=136, q_token=544, o_head=136, o_token=544), UNSUPPORTED),
+    (attend, dict(c_dim=136, c_k=P16 + 2, c_k_head=136, c_k_token=272, c_v_head=136, c_v_token=272, q_head=136, q_token=544, o_head=136, o_token=544), UNSUPPORTED),
     # long tables of few rows take a workspace
     (attend, dict(c_width=4096, c_table_ld=4096, ws=None), INVALID), (attend, dict(c_width=4096, c_table_ld=4096, wb=64), INVALID),
     (attend, dict(c_width=4096, c_table_ld=4096, ws=P16 + 8), INVALID),
