@@ -81,7 +81,7 @@ struct Plan {
     float* sums;         // [slot][head][row][dim padded]
     float* stats;        // [slot][head][row][2]: maximum and sum
 };
-constexpr int LEAST_TILES = 4;   // of a piece
+constexpr int LEAST_TILES = 2;   // of a piece
 
 // What a sequence has to do: tiles of rows, and the key tiles [lo, hi) that any of them sees.
 struct Task {
@@ -105,36 +105,124 @@ __device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int 
     return t;
 }
 
-// Sum over a workgroup, in every thread.  Ends with all threads past their reads of scratch.
-template <int THREADS>
-__device__ __forceinline__ int64_t block_total(int64_t v, int64_t* scratch) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    if (THREADS == 64) return v;
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0;
-    for (int w = 0; w < THREADS / 64; ++w) v += scratch[w];
-    __syncthreads();
+// Sums of a wave's lanes up to each one, by moves within the vector unit.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved_lanes(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+    v += moved_lanes<0x111, 0xf>(v);   // within rows of 16: from 1, 2, 4 and 8 lanes below
+    v += moved_lanes<0x112, 0xf>(v);
+    v += moved_lanes<0x114, 0xf>(v);
+    v += moved_lanes<0x118, 0xf>(v);
+    v += moved_lanes<0x142, 0xa>(v);   // the last lane of a row to the next one, then that of two
+    v += moved_lanes<0x143, 0xc>(v);
     return v;
 }
-
-// Key tiles of a piece.  A sequence counts once for every tile of its rows.
-template <int THREADS>
-__device__ __forceinline__ int piece_tiles(const AttendArgs& a, const Plan& p, int64_t* scratch) {
-    if (p.target == 0) return 1 << 30;
-    int64_t work = 0;
-    for (int b = threadIdx.x; b < a.c.batch; b += THREADS) {
-        const Task t = task_of(a, p, b);
-        work += (int64_t)t.row_tiles * (t.hi - t.lo);
-    }
-    work = block_total<THREADS>(work, scratch);
-    const int64_t each = (work + p.target - 1) / p.target;
-    return (int)(each < LEAST_TILES ? LEAST_TILES : each < (1 << 30) ? each : 1 << 30);
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved_lanes(float v) {
+    return __builtin_bit_cast(float, moved_lanes<CTRL, ROWS>(__builtin_bit_cast(int, v)));
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved_lanes(double v) {
+    const int64_t w = __builtin_bit_cast(int64_t, v);
+    const uint32_t low = (uint32_t)moved_lanes<CTRL, ROWS>((int)w), high = (uint32_t)moved_lanes<CTRL, ROWS>((int)(w >> 32));
+    return __builtin_bit_cast(double, (int64_t)((uint64_t)high << 32 | low));
+}
+// The whole sum, in the last lane.
+template <class F>
+__device__ __forceinline__ F last_sum(F v) {
+    v += moved_lanes<0x111, 0xf>(v);
+    v += moved_lanes<0x112, 0xf>(v);
+    v += moved_lanes<0x114, 0xf>(v);
+    v += moved_lanes<0x118, 0xf>(v);
+    v += moved_lanes<0x142, 0xa>(v);
+    v += moved_lanes<0x143, 0xc>(v);
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, last_sum(v)), 63));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    const int64_t w = __builtin_bit_cast(int64_t, last_sum(v));
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)w, 63), high = (uint32_t)__builtin_amdgcn_readlane((int)(w >> 32), 63);
+    return __builtin_bit_cast(double, (int64_t)((uint64_t)high << 32 | low));
+}
+
+// Key tiles of a piece, of all sequences' row tiles times their key tiles: whole numbers, which 64 bits add exactly in
+// any order, so that both kernels find the same.  More than the quotient, as the workspace has room for `target` pieces
+// and one for each tile of rows.
+__device__ __forceinline__ int piece_tiles(double work, const Plan& p) {
+    const double each = work / (double)p.target;
+    return each < (double)LEAST_TILES ? LEAST_TILES : each < 0x1p30 ? (int)each + 1 : 1 << 30;
+}
+__device__ __forceinline__ double work_of(const Task& t) { return (double)t.row_tiles * (double)(t.hi - t.lo); }
 __device__ __forceinline__ int pieces_of(const Task& t, int tiles) {
-    const int n = (t.hi - t.lo + tiles - 1) / tiles;
+    const int n = (int)((uint32_t)(t.hi - t.lo + tiles - 1) / (uint32_t)tiles);   // below 2^31
     return n < 1 ? 1 : n;
+}
+
+// A piece's place: a sequence, and the piece's number among those of the sequence.
+struct Place {
+    int b, number, tiles;   // b < 0: none
+};
+// Where piece `slot` lies, or (b >= 0) how many pieces lie before sequence b's, as -number.  All threads get the answer.
+template <int THREADS, bool FIRST_OF>
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, int slot, int b, int* scratch) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, batch = (int)a.c.batch;
+    if (batch <= 64) {   // a lane a sequence, each wave for itself
+        Task t = {};
+        if (lane < batch) t = task_of(a, p, lane);
+        const int tiles = p.target ? piece_tiles(wave_sum(work_of(t)), p) : 1 << 30;
+        const int n = t.row_tiles * pieces_of(t, tiles), upto = wave_scan(n);
+        if (FIRST_OF) return {b, __builtin_amdgcn_readlane(upto - n, b), tiles};
+        const uint64_t past = __ballot(upto > slot && lane < batch);
+        if (!past) return {-1, 0, tiles};
+        const int first = __builtin_ctzll(past);
+        return {first, slot - __builtin_amdgcn_readlane(upto - n, first), tiles};
+    }
+    // a run of sequences a thread
+    const int each = (batch + THREADS - 1) / THREADS, b0 = threadIdx.x * each, b1 = b0 + each < batch ? b0 + each : batch;
+    constexpr int WAVES = THREADS / 64;
+    int tiles = 1 << 30;
+    if (p.target) {
+        double work = 0.0;
+        for (int i = b0; i < b1; ++i) work += work_of(task_of(a, p, i));
+        work = wave_sum(work);
+        double* sums = reinterpret_cast<double*>(scratch);
+        if (lane == 0) sums[wave] = work;
+        __syncthreads();
+        work = 0.0;
+        for (int w = 0; w < WAVES; ++w) work += sums[w];
+        __syncthreads();
+        tiles = piece_tiles(work, p);
+    }
+    int here = 0;
+    for (int i = b0; i < b1; ++i) {
+        const Task t = task_of(a, p, i);
+        here += t.row_tiles * pieces_of(t, tiles);
+    }
+    int upto = wave_scan(here);
+    if (lane == 63) scratch[wave] = upto;
+    if (threadIdx.x == 0) scratch[WAVES] = -1;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += scratch[w];
+    int rest = slot - (upto - here);
+    if (FIRST_OF ? b >= b0 && b < b1 : rest >= 0 && rest < here) {
+        if (FIRST_OF) rest = upto - here;
+        for (int i = b0; i < b1; ++i) {
+            const Task t = task_of(a, p, i);
+            const int n = t.row_tiles * pieces_of(t, tiles);
+            if (FIRST_OF ? i == b : rest < n) {
+                scratch[WAVES] = i;
+                scratch[WAVES + 1] = rest;
+                break;
+            }
+            rest += FIRST_OF ? n : -n;
+        }
+    }
+    __syncthreads();
+    return {scratch[WAVES], scratch[WAVES + 1], tiles};
 }
 
 template <int DT_, int DP_, int ROW_WAVES_, int KEY_WAVES_>
@@ -206,8 +294,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     using Frag = typename M::Frag;
     constexpr int VEC = S::VEC, SUBS = S::SUBS, KEYS = S::KEYS, CHUNKS = S::CHUNKS, COLS = S::COLS, DTILES = COLS / 32;
     extern __shared__ __attribute__((aligned(1024))) char s_tiles[];   // [2][keys, values][KEYS][DP]
-    __shared__ int64_t s_scratch[S::WAVES];
-    __shared__ int s_place[2], s_odd;
+    __shared__ __attribute__((aligned(8))) int s_scratch[2 * S::WAVES + 2];
+    __shared__ int s_odd[S::WAVES];
     __shared__ float s_stats[S::WAVES][32][2];
     __shared__ __attribute__((aligned(16))) float s_fix[S::WAVES][COLS];   // values of a key that are not finite
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, mine = lane & 31;
@@ -215,48 +303,14 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int heads = (int)a.c.heads, head = blockIdx.x % heads, slot = blockIdx.x / heads;
 
     // Which sequence, tile of rows and piece of keys.
-    const int tiles = uniform(piece_tiles<S::THREADS>(a, p, s_scratch));
-    {
-        if (threadIdx.x == 0) {
-            s_place[0] = -1;
-            s_odd = 0;
-        }
-        const int batch = (int)a.c.batch, each = (batch + S::THREADS - 1) / S::THREADS;
-        const int b0 = threadIdx.x * each, b1 = b0 + each < batch ? b0 + each : batch;
-        int64_t here = 0;
-        for (int b = b0; b < b1; ++b) {
-            const Task t = task_of(a, p, b);
-            here += (int64_t)t.row_tiles * pieces_of(t, tiles);
-        }
-        int64_t upto = here;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t v = __shfl_up(upto, o);
-            if (lane >= o) upto += v;
-        }
-        if (lane == 63) s_scratch[wave] = upto;
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) upto += s_scratch[w];
-        int64_t rest = slot - (upto - here);
-        if (rest >= 0 && rest < here) {
-            for (int b = b0; b < b1; ++b) {
-                const Task t = task_of(a, p, b);
-                const int64_t n = (int64_t)t.row_tiles * pieces_of(t, tiles);
-                if (rest < n) {
-                    s_place[0] = b;
-                    s_place[1] = (int)rest;
-                    break;
-                }
-                rest -= n;
-            }
-        }
-        __syncthreads();
-    }
-    const int b = uniform(s_place[0]);
+    const Place place = place_of<S::THREADS, false>(a, p, slot, 0, s_scratch);
+    const int b = uniform(place.b), in_task = uniform(place.number), tiles = uniform(place.tiles);
     if (b < 0) return;
     const Task task = task_of(a, p, b);
-    const int pieces = pieces_of(task, tiles), in_task = uniform(s_place[1]), piece = in_task % pieces;
+    const int pieces = pieces_of(task, tiles), piece = in_task % pieces;
     const int row_tile = task.row_tiles - 1 - in_task / pieces;   // a prompt's longest first
+    if (row_tile < 0) return;                                     // starts that do not go up
+    if (lane == 0) s_odd[wave] = 0;
 
     // Rows of this workgroup, and the keys that they see.
     const int G = p.group.d, row0 = row_tile * S::ROWS, all_rows = task.count * G;
@@ -317,7 +371,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         char* to_k = to + wave * MOVES * 1024;
         char* to_v = to_k + S::TILE;
         const int first = (int)divided((uint32_t)(t * KEYS), p.size);
-        if (DP > 128 || p.direct) {
+        if (DP > 128 || __builtin_expect(p.direct, 1)) {
             const int row0_ = wave * MOVES * MOVE_ROWS;
             // The place of a position that lies in page `id`, an address that the wave has.
             auto place_of = [&](const char* head, int64_t page_step, int64_t token_step, uint32_t id, int pos, uint32_t at) {
@@ -326,7 +380,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                 asm("" : "+s"(low), "+s"(high));   // or each move's lanes would keep an address of their own
                 return reinterpret_cast<const char*>((uint64_t)high << 32 | low);
             };
-            if (p.even && dim == DP && hi - t * KEYS >= KEYS && !bad_of(t, ids).any()) {
+            if (__builtin_expect(p.even && dim == DP && hi - t * KEYS >= KEYS && !bad_of(t, ids).any(), 1)) {
 #pragma unroll
                 for (int q = 0; q < MOVES; ++q) {
                     // all rows of the move are there, in one page
@@ -379,17 +433,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
             }
         }
     };
-    if (p.direct && dim < DP) {
-        for (int i = threadIdx.x; i < 4 * S::TILE / 16; i += S::THREADS) reinterpret_cast<float4v*>(s_tiles)[i] = float4v{};
-        __syncthreads();
-    }
     Ids here = {}, next = {};   // of this tile and the next one
-    if (tile < tile_end) {
-        here = look_up(tile);
-        stage(tile, s_tiles, here);
-        if (tile + 1 < tile_end) next = look_up(tile + 1);
-    }
-
+    if (tile < tile_end) here = look_up(tile);
     // This lane's row: its queries, and the positions that it sees.
     const int row = rw * 32 + mine;
     const bool real = row < rows;
@@ -411,19 +456,33 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     Frag q[STEPS];
     {
         const T* x = static_cast<const T*>(a.q.p) + (int64_t)token * a.q.token + q_head * a.q.head;
+        if (__builtin_expect(dim == DP, 1)) {   // (rows past the last one repeat it)
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int c = (2 * s + half) * VEC;
-            if (real && c + VEC <= dim) {
-                const Pack<T, VEC> w = load_pack<T, VEC>(x + c);
+            for (int s = 0; s < STEPS; ++s) {
+                const Pack<T, VEC> w = load_pack<T, VEC>(x + (2 * s + half) * VEC);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) q[s][e] = w.v[e];
-            } else {
+            }
+        } else {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) q[s][e] = real && c + e < dim ? x[c + e] : (T)0.0f;
+            for (int s = 0; s < STEPS; ++s) {
+                const int c = (2 * s + half) * VEC;
+                if (c + VEC <= dim) {
+                    const Pack<T, VEC> w = load_pack<T, VEC>(x + c);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) q[s][e] = w.v[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) q[s][e] = c + e < dim ? x[c + e] : (T)0.0f;
+                }
             }
         }
     }
+    if (p.direct && dim < DP) {
+        for (int i = threadIdx.x; i < 4 * S::TILE / 16; i += S::THREADS) reinterpret_cast<float4v*>(s_tiles)[i] = float4v{};
+        __syncthreads();
+    }
+
     float16v o[DTILES];
 #pragma unroll
     for (int d = 0; d < DTILES; ++d)
@@ -435,7 +494,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     // Where this lane reads: a chunk of key `mine`, by XOR with a step's chunks; the values of four rows by 16 lanes.
     const int k_at = mine * S::ROW + ((half ^ key_swizzle<CHUNKS>(mine)) * 16);
     const int tr_row = 4 * half + (lane & 15) / 4, tr_chunk = (lane >> 4 & 1) * 2 + (lane >> 1 & 1), tr_byte = (lane & 1) * 8;
-    const int tile0 = tile;
+    const int tile0 = tile;   // the first one
     // Products of a tile with this wave's rows, while the next one moves into the other buffer: the two lie apart, or the
     // compiler would wait for the moves before it reads.
     auto step = [&](const char* __restrict__ from, char* __restrict__ to, const Bad& bad) {
@@ -493,7 +552,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         };
         read_values(0);
         __builtin_amdgcn_sched_barrier(ORDERED);
-        if (key0 + SUBS * 32 - 1 > limit_min || key0 < low_max || bad.any()) {
+        if (__builtin_expect(key0 + SUBS * 32 - 1 > limit_min || key0 < low_max || bad.any(), 0)) {
             uint32_t gone[SUBS] = {};   // keys whose page is not there
             if (bad.any()) {
                 const uint32_t first = divided((uint32_t)(tile * KEYS), p.size);
@@ -566,11 +625,15 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     };
     char* from = s_tiles;
     char* to = s_tiles + 2 * S::TILE;
+    if (tile < tile_end) {
+        stage(tile, s_tiles, here);
+        if (tile + 1 < tile_end) next = look_up(tile + 1);
+    }
     for (; tile < tile_end; ++tile) {
         // this tile has landed, and everyone is done with the last one
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         const Bad bad = bad_of(tile, here);
-        if (partly_seen(tile, bad)) {
+        if (__builtin_expect(partly_seen(tile, bad), 0)) {
             // A NaN or an infinity among the values must not reach, as 0 times it, a row that does not see it: it is
             // left out here, by the lane that moved it, and added at the end where it is seen.
             char* own = from + S::TILE + wave * MOVES * 1024 + lane * 16;
@@ -586,7 +649,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                 }
                 if (!fine) {
                     *reinterpret_cast<Pack<T, VEC>*>(own) = w;
-                    s_odd = 1;
+                    s_odd[wave] = 1;
                 }
             }
         }
@@ -596,7 +659,12 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         from = to;
         to = t;
     }
-    if (tile0 < tile_end && uniform(s_odd)) {
+    int odd = 0;
+    if (tile0 < tile_end) {
+#pragma unroll
+        for (int w = 0; w < S::WAVES; ++w) odd |= s_odd[w];   // written before the last tile's barrier
+    }
+    if (__builtin_expect(uniform(odd), 0)) {
         // values that are not finite, in tiles that some row does not see all of
 #pragma unroll 1
         for (int t = tile0; t < tile_end; ++t) {
@@ -701,55 +769,83 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
 #endif
 }
 
-// Joins the pieces of rows that were cut: a wave takes a row.
-template <int DT>
+// Joins the pieces of rows that were cut: a wave takes a row, its lanes the pieces' weights, then COLS columns each.
+template <int DT, int COLS>
 __global__ __launch_bounds__(256) void k_join(AttendArgs a, Plan p, int dp) {
     using T = typename Elem<DT>::T;
-    __shared__ int64_t s_scratch[4];
+    __shared__ __attribute__((aligned(8))) int s_scratch[10];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int token = blockIdx.x;
-    const int b = sequence_of(a.c.starts, (int)a.c.batch, token);
+    const int b = uniform(sequence_of(a.c.starts, (int)a.c.batch, token));
     if (b < 0 || b >= a.c.batch) return;
-    const int tiles = piece_tiles<256>(a, p, s_scratch);
+    const Place place = place_of<256, true>(a, p, 0, b, s_scratch);
     const Task task = task_of(a, p, b);
-    const int pieces = pieces_of(task, tiles);
+    const int pieces = uniform(pieces_of(task, place.tiles));
     if (pieces == 1 || token < task.first || token >= task.first + task.count) return;
-    int64_t before = 0;
-    for (int i = threadIdx.x; i < b; i += 256) {
-        const Task t = task_of(a, p, i);
-        before += (int64_t)t.row_tiles * pieces_of(t, tiles);
-    }
-    before = block_total<256>(before, s_scratch);
     const float inf = __builtin_inff(), scale = a.scale * LOG2E;
-    const int dim = (int)a.c.dim, heads = (int)a.c.heads;
-    for (int q_head = blockIdx.y * 4 + wave; q_head < a.q_heads; q_head += gridDim.y * 4) {
-        const int G = p.group.d, head = (int)divided((uint32_t)q_head, p.group), r = (token - task.first) * G + q_head - head * G;
-        const int64_t slot0 = before + (int64_t)(task.row_tiles - 1 - r / p.rows) * pieces;
-        if (slot0 + pieces > p.slots) return;   // starts that do not go up
-        const int64_t at0 = (slot0 * heads + head) * p.rows + r % p.rows, step = (int64_t)heads * p.rows;
-        float top = -inf;
-        for (int k = lane; k < pieces; k += 64) top = fmaxf(top, p.stats[(at0 + k * step) * 2]);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        float v[4] = {}, sum = 0.0f;
-        for (int k = 0; k < pieces; ++k) {
-            const int64_t at = at0 + k * step;
-            const float t = p.stats[at * 2], s = p.stats[at * 2 + 1];
-            if (t == -inf && s == 0.0f) continue;   // sees nothing: its sums are zeros
-            const float f = __builtin_amdgcn_exp2f((t - top) * scale);
-            sum += s * f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e * 64 < dp && e * 64 + lane < dim) v[e] += p.sums[at * dp + e * 64 + lane] * f;
+    const int dim = (int)a.c.dim, heads = (int)a.c.heads, q_head = blockIdx.y * 4 + wave;
+    if (q_head >= a.q_heads) return;
+    const int G = p.group.d, head = (int)divided((uint32_t)q_head, p.group), r = (token - task.first) * G + q_head - head * G;
+    const int64_t slot0 = uniform(place.number) + (int64_t)(task.row_tiles - 1 - r / p.rows) * pieces;
+    if (slot0 < 0 || slot0 + pieces > p.slots) return;   // starts that do not go up
+    const int64_t at0 = (slot0 * heads + head) * p.rows + r % p.rows, step = (int64_t)heads * p.rows;
+    const bool here = lane * COLS < dp;
+    struct Stats {
+        float top, sum;
+    };
+    auto stats_of = [&](int k) {   // of a lane's piece
+        Stats t = {-inf, 0.0f};
+        if (k < pieces) {
+            t.top = p.stats[(at0 + k * step) * 2];
+            t.sum = p.stats[(at0 + k * step) * 2 + 1];
         }
-        T* y = static_cast<T*>(a.out.p) + (int64_t)token * a.out.token + q_head * a.out.head;
-        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+        return t;
+    };
+    // Sums are read AT_ONCE pieces at a time, the first ones beside the weights.
+    constexpr int AT_ONCE = 16;
+    const float* from = p.sums + at0 * dp + (here ? lane * COLS : 0);
+    Pack<float, COLS> x[AT_ONCE];
+    auto read = [&](int k0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e * 64 + lane < dim) y[e * 64 + lane] = rounded<T>(v[e] * f);
-        if (lane == 0 && a.lse)
-            a.lse[(int64_t)token * a.q_heads + q_head] = sum == 0.0f ? -inf : (top * scale - Mat<DT>::SHIFT + __log2f(sum)) * LN2;
+        for (int k = 0; k < AT_ONCE; ++k) x[k] = load_pack<float, COLS>(from + (k0 + k < pieces ? k0 + k : pieces - 1) * step * dp);
+    };
+    Stats t = stats_of(lane);
+    read(0);
+    float top = t.top;
+    for (int k = lane + 64; k < pieces; k += 64) top = fmaxf(top, stats_of(k).top);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float v[COLS] = {}, sum = 0.0f, f = 0.0f;
+    for (int k0 = 0; k0 < pieces; k0 += AT_ONCE) {
+        if (k0 % 64 == 0) {
+            if (k0) t = stats_of(k0 + lane);
+            // a piece that sees nothing has a maximum of -inf, and its sums are zeros
+            f = t.top == -inf && t.sum == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((t.top - top) * scale);
+            sum += wave_sum(t.sum * f);
+        }
+        if (k0) read(k0);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (k0 + k >= pieces) break;
+            const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (k0 + k) & 63));
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) v[c] += x[k].v[c] * w;
+        }
     }
+    T* y = static_cast<T*>(a.out.p) + (int64_t)token * a.out.token + q_head * a.out.head + lane * COLS;
+    const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (lane * COLS + COLS <= dim) {
+        Pack<T, COLS> w;
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) w.v[c] = rounded<T>(v[c] * over);
+        store_pack<T, COLS>(y, w);
+    } else {
+#pragma unroll
+        for (int c = 0; c < COLS; ++c)
+            if (lane * COLS + c < dim) y[c] = rounded<T>(v[c] * over);
+    }
+    if (lane == 0 && a.lse)
+        a.lse[(int64_t)token * a.q_heads + q_head] = sum == 0.0f ? -inf : (top * scale - Mat<DT>::SHIFT + __log2f(sum)) * LN2;
 }
 
 int padded(int64_t dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
@@ -767,7 +863,7 @@ Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int
     const int row = s.dp * elem_size(type);
     s.few = n * G <= 32 * (batch < n ? batch : n);
     s.rows = s.few ? 32 : s.dp > 128 ? 64 : 128;
-    s.keys = s.few ? (row <= 256 ? 128 : row <= 512 ? 64 : 32) : row <= 512 ? 64 : 32;
+    s.keys = s.few ? (row <= 512 ? 64 : 32) : row <= 512 ? 64 : 32;
     const int64_t most = batch < n ? batch : n;               // sequences with new tokens
     const int64_t units = std::min<int64_t>(n * G, n * G / s.rows + most);   // tiles of rows
     const int64_t total = s.few ? 2048 : 768;
@@ -791,7 +887,7 @@ hipError_t attend(const AttendArgs& a, const Plan& p, hipStream_t stream) {
 
 template <int DT, int DP>
 hipError_t attend_rows(const AttendArgs& a, const Plan& p, bool few, hipStream_t stream) {
-    constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), KW = ROW <= 256 ? 4 : ROW <= 512 ? 2 : 1, RW = DP > 128 ? 2 : 4;
+    constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), KW = ROW <= 512 ? 2 : 1, RW = DP > 128 ? 2 : 4;
     return few ? attend<DT, DP, 1, KW>(a, p, stream) : attend<DT, DP, RW, 1>(a, p, stream);
 }
 
@@ -842,7 +938,12 @@ hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStrea
         }
         if (e != hipSuccess || !s.target) return e;
         const dim3 grid((unsigned)a.n, (unsigned)((a.q_heads + 3) / 4));
-        k_join<DT><<<grid, 256, 0, stream>>>(a, p, s.dp);
+        if (s.dp <= 64)
+            k_join<DT, 1><<<grid, 256, 0, stream>>>(a, p, s.dp);
+        else if (s.dp == 128)
+            k_join<DT, 2><<<grid, 256, 0, stream>>>(a, p, s.dp);
+        else
+            k_join<DT, 4><<<grid, 256, 0, stream>>>(a, p, s.dp);
         return hipGetLastError();
     });
 }
