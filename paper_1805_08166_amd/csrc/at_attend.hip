@@ -42,8 +42,8 @@ struct Mat;
 template <>
 struct Mat<AT_BF16> {
     typedef __bf16 Frag __attribute__((ext_vector_type(8)));
-    // P is rounded to bf16 (its largest value is 1): half a step is 2^-9 of it, like that of the values it multiplies.
-    static constexpr float SHIFT = 0.0f;
+    // P is rounded to bf16, off by half a step, 2^-9 of it at most, as the values that it multiplies are.
+    static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
@@ -51,8 +51,8 @@ struct Mat<AT_BF16> {
 template <>
 struct Mat<AT_F16> {
     typedef _Float16 Frag __attribute__((ext_vector_type(8)));
-    // P times 2^14, so that fp16's smallest normal value is 2^-28 of a row's largest.
-    static constexpr float SHIFT = 14.0f;
+    // P times 2^11, at most 2^15 with the slack of its maximum: below 2^-14 steps are 2^-24, off by 2^-36 of the largest at most.
+    static constexpr float SHIFT = 11.0f, SLACK = 4.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
     }
@@ -60,7 +60,7 @@ struct Mat<AT_F16> {
 template <>
 struct Mat<AT_F32> {
     typedef float Frag __attribute__((ext_vector_type(4)));
-    static constexpr float SHIFT = 0.0f;
+    static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
@@ -77,7 +77,7 @@ struct Plan {
     int target;          // pieces a head that the keys are cut into, about; 0: whole sequences
     int slots;           // pieces a head, at most
     int direct;          // rows of the cache are whole aligned 16 bytes
-    int even;            // and those of a move lie in one page
+    int run;             // moves whose rows lie in one page: all of a wave's, 1, or 0 where those of one need not
     float* sums;         // [slot][head][row][dim padded]
     float* stats;        // [slot][head][row][2]: maximum and sum
 };
@@ -97,7 +97,7 @@ __device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int 
     const int64_t room = a.c.width * a.c.page_size, l = a.c.lengths[b];
     t.position = l - s.count;
     t.length = (int)(l < 0 ? 0 : l < room ? l : room);
-    t.row_tiles = (int)(((uint32_t)s.count * p.group.d + p.rows - 1) / p.rows);   // fewer than 2^31 rows, tiles of at most 128
+    t.row_tiles = (int)(((uint32_t)s.count * p.group.d + p.rows - 1) / p.rows);   // fewer than 2^31 rows, tiles of at most 256
     int64_t lo = a.window > 0 ? t.position - a.window + 1 : 0;
     lo = lo < 0 ? 0 : lo < t.length ? lo : t.length;
     t.lo = (int)(lo / p.keys);
@@ -350,11 +350,10 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         }
         return r;
     };
-    auto bad_of = [&](int t, const Ids& ids) {
+    auto bad_of = [&](const Ids& ids) {   // (lanes past the last page have number 0)
         Bad r;
-        const int first = (int)divided((uint32_t)(t * KEYS), p.size);
 #pragma unroll
-        for (int i = 0; i < S::IDS; ++i) r.v[i] = __ballot((uint32_t)ids.v[i] >= pages && first + i * 64 + lane < used_pages);
+        for (int i = 0; i < S::IDS; ++i) r.v[i] = __ballot((uint32_t)ids.v[i] >= pages);
         return r;
     };
     auto id_of = [&](const Ids& ids, uint32_t at) {   // the `at`-th of a tile's page numbers
@@ -366,30 +365,49 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const char* k_head = static_cast<const char*>(a.c.k) + (int64_t)head * a.c.k_head * S::SIZE;
     const char* v_head = static_cast<const char*>(a.c.v) + (int64_t)head * a.c.v_head * S::SIZE;
     const int lane_row = lane / CHUNKS, lane_chunk = lane % CHUNKS;
-    const uint32_t k_lane = (uint32_t)(lane_row * a.c.k_token * S::SIZE), v_lane = (uint32_t)(lane_row * a.c.v_token * S::SIZE);
-    auto stage = [&](int t, char* to, const Ids& ids) {
+    const uint32_t k_lane = lane_row * (uint32_t)a.c.k_token * S::SIZE, v_lane = lane_row * (uint32_t)a.c.v_token * S::SIZE;
+    // in bytes; those of tokens are below 2^27 where moves go directly
+    const uint64_t k_page = (uint64_t)a.c.k_page * S::SIZE, v_page = (uint64_t)a.c.v_page * S::SIZE;
+    const uint32_t k_token = (uint32_t)a.c.k_token * S::SIZE, v_token = (uint32_t)a.c.v_token * S::SIZE;
+    auto stage = [&](int t, char* to, const Ids& ids, const Bad& bad) {
         char* to_k = to + wave * MOVES * 1024;
         char* to_v = to_k + S::TILE;
         const int first = (int)divided((uint32_t)(t * KEYS), p.size);
         if (DP > 128 || __builtin_expect(p.direct, 1)) {
             const int row0_ = wave * MOVES * MOVE_ROWS;
             // The place of a position that lies in page `id`, an address that the wave has.
-            auto place_of = [&](const char* head, int64_t page_step, int64_t token_step, uint32_t id, int pos, uint32_t at) {
-                const uint64_t x = (uint64_t)head + (id * (uint64_t)page_step + (pos - at * p.size.d) * (uint64_t)token_step) * S::SIZE;
+            auto address = [&](const char* head, uint64_t page_step, uint32_t token_step, uint32_t id, int pos, uint32_t at) {
+                const uint64_t x = (uint64_t)head + id * page_step + (uint64_t)(pos - at * p.size.d) * token_step;
                 uint32_t low = uniform((int)x), high = uniform((int)(x >> 32));
                 asm("" : "+s"(low), "+s"(high));   // or each move's lanes would keep an address of their own
                 return reinterpret_cast<const char*>((uint64_t)high << 32 | low);
             };
-            if (__builtin_expect(p.even && dim == DP && hi - t * KEYS >= KEYS && !bad_of(t, ids).any(), 1)) {
-#pragma unroll
-                for (int q = 0; q < MOVES; ++q) {
-                    // all rows of the move are there, in one page
-                    const int row = row0_ + q * MOVE_ROWS, pos = t * KEYS + row;
+            if (__builtin_expect(p.run && dim == DP && hi - t * KEYS >= KEYS && !bad.any(), 1)) {
+                // all rows of a move are there, in one page
+                auto move = [&](int q, const char* k, const char* v) {
+                    const int row = row0_ + q * MOVE_ROWS + lane_row;
+                    const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row)) * 16, cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * 16;
+                    __builtin_amdgcn_global_load_lds(k + (k_lane + ck), to_k + q * 1024, 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds(v + (v_lane + cv), to_v + q * 1024, 16, 0, 0);
+                };
+                if (p.run > 1) {
+                    const int pos = t * KEYS + row0_;
                     const uint32_t at = divided((uint32_t)pos, p.size), id = id_of(ids, at - first);
-                    const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row + lane_row)) * 16;
-                    const uint32_t cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row + lane_row)) * 16;
-                    __builtin_amdgcn_global_load_lds(place_of(k_head, a.c.k_page, a.c.k_token, id, pos, at) + (k_lane + ck), to_k + q * 1024, 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds(place_of(v_head, a.c.v_page, a.c.v_token, id, pos, at) + (v_lane + cv), to_v + q * 1024, 16, 0, 0);
+                    const char* k = address(k_head, k_page, k_token, id, pos, at);
+                    const char* v = address(v_head, v_page, v_token, id, pos, at);
+#pragma unroll
+                    for (int q = 0; q < MOVES; ++q) {
+                        move(q, k, v);
+                        k += MOVE_ROWS * k_token;
+                        v += MOVE_ROWS * v_token;
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < MOVES; ++q) {
+                        const int pos = t * KEYS + row0_ + q * MOVE_ROWS;
+                        const uint32_t at = divided((uint32_t)pos, p.size), id = id_of(ids, at - first);
+                        move(q, address(k_head, k_page, k_token, id, pos, at), address(v_head, v_page, v_token, id, pos, at));
+                    }
                 }
             } else {
                 // row by row, with zeros for those that are not there (past dim, zeros lie in LDS already)
@@ -400,8 +418,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                     const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row)) * 16, cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * 16;
                     if (lane_row != i % MOVE_ROWS) continue;
                     if (pos < hi && id < pages) {
-                        const char* k = place_of(k_head, a.c.k_page, a.c.k_token, id, pos, at);
-                        const char* v = place_of(v_head, a.c.v_page, a.c.v_token, id, pos, at);
+                        const char* k = address(k_head, k_page, k_token, id, pos, at);
+                        const char* v = address(v_head, v_page, v_token, id, pos, at);
                         if ((int)ck < dim * S::SIZE) __builtin_amdgcn_global_load_lds(k + ck, to_k + q * 1024, 16, 0, 0);
                         if ((int)cv < dim * S::SIZE) __builtin_amdgcn_global_load_lds(v + cv, to_v + q * 1024, 16, 0, 0);
                     } else {
@@ -433,8 +451,9 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
             }
         }
     };
-    Ids here = {}, next = {};   // of this tile and the next one
-    if (tile < tile_end) here = look_up(tile);
+    Ids next = {};           // of the next tile, and those of them that are not there
+    Bad bad_next = {};
+    if (tile < tile_end) next = look_up(tile);
     // This lane's row: its queries, and the positions that it sees.
     const int row = rw * 32 + mine;
     const bool real = row < rows;
@@ -489,7 +508,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
     const float inf = __builtin_inff(), scale = a.scale * LOG2E;
-    float top = -inf, sum = 0.0f;   // the row's maximum score, and this lane's part of its sum
+    float top = -inf, sum = 0.0f;   // about the row's maximum score, and this lane's part of its sum
 
     // Where this lane reads: a chunk of key `mine`, by XOR with a step's chunks; the values of four rows by 16 lanes.
     const int k_at = mine * S::ROW + ((half ^ key_swizzle<CHUNKS>(mine)) * 16);
@@ -499,8 +518,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     // compiler would wait for the moves before it reads.
     auto step = [&](const char* __restrict__ from, char* __restrict__ to, const Bad& bad) {
         if (tile + 1 < tile_end) {
-            stage(tile + 1, to, next);
-            here = next;
+            bad_next = bad_of(next);
+            stage(tile + 1, to, next, bad_next);
             if (tile + 2 < tile_end) next = look_up(tile + 2);
         }
         const int key0 = tile * KEYS + kw * SUBS * 32;
@@ -576,7 +595,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, sc[u][e]);
         most = halves(most, [](float x, float y) { return fmaxf(x, y); });
-        if (__any(most > top)) {
+        if (__any(most * scale > top * scale + M::SLACK)) {
             const float over = fmaxf(top, most);
             const float f = top == -inf ? 0.0f : __builtin_amdgcn_exp2f((top - over) * scale);
             top = over;
@@ -586,32 +605,46 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[d][e] *= f;
         }
-        // p = 2^(s scale - base); any base near the maximum serves, as long as all of a row's p have it
+        // p = 2^(s scale - base); any base near the maximum serves, as long as all of a row's p have it: sums are scaled
+        // down only when a maximum is M::SLACK above the one in use
         const float base = top == -inf ? 0.0f : top * scale - M::SHIFT;
-#pragma unroll
-        for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                sc[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][e], scale, -base));
-                sum += sc[u][e];
-            }
+        auto weight = [&](int u, int e) { sc[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][e], scale, -base)); };
         if constexpr (S::SIZE == 2) {
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                if (g + 1 < GROUPS) read_values(g + 1);
-                __builtin_amdgcn_sched_barrier(ORDERED);
+            // The weights of a group of 16 keys, rounded, and their sum, which lse has to hold in 32 bits: before rounding.
+            auto rounded_weights = [&](int g) {
                 Frag w;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = (T)sc[g / 2][8 * (g & 1) + e];
 #pragma unroll
-                for (int d = 0; d < DTILES; ++d) o[d] = M::mma(v[g & 1][d], w, o[d]);
-                __builtin_amdgcn_sched_barrier(ORDERED);
+                for (int e = 0; e < 8; e += 2) sum += sc[g / 2][8 * (g & 1) + e] + sc[g / 2][8 * (g & 1) + e + 1];
+                return w;
+            };
+#pragma unroll
+            for (int e = 0; e < 8; ++e) weight(0, e);
+            Frag w = rounded_weights(0);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                if (g + 1 < GROUPS) read_values(g + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                // between a group's products the next one's exponentials
+#pragma unroll
+                for (int d = 0; d < DTILES; ++d) {
+                    o[d] = M::mma(v[g & 1][d], w, o[d]);
+                    if (g + 1 < GROUPS) {
+#pragma unroll
+                        for (int e = 8 * d / DTILES; e < 8 * (d + 1) / DTILES; ++e) weight((g + 1) / 2, 8 * ((g + 1) & 1) + e);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (g + 1 < GROUPS) w = rounded_weights(g + 1);
             }
         } else {
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
+                    weight(u, e);
+                    sum += sc[u][e];
                     const int key = u * 32 + 8 * (e >> 2) + (e & 3);   // and four on in the other half, whose chunks are swizzled
 #pragma unroll
                     for (int d = 0; d < DTILES; ++d) {
@@ -626,13 +659,14 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     char* from = s_tiles;
     char* to = s_tiles + 2 * S::TILE;
     if (tile < tile_end) {
-        stage(tile, s_tiles, here);
+        bad_next = bad_of(next);
+        stage(tile, s_tiles, next, bad_next);
         if (tile + 1 < tile_end) next = look_up(tile + 1);
     }
     for (; tile < tile_end; ++tile) {
         // this tile has landed, and everyone is done with the last one
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        const Bad bad = bad_of(tile, here);
+        const Bad bad = bad_next;
         if (__builtin_expect(partly_seen(tile, bad), 0)) {
             // A NaN or an infinity among the values must not reach, as 0 times it, a row that does not see it: it is
             // left out here, by the lane that moved it, and added at the end where it is seen.
@@ -668,7 +702,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         // values that are not finite, in tiles that some row does not see all of
 #pragma unroll 1
         for (int t = tile0; t < tile_end; ++t) {
-            if (!partly_seen(t, bad_of(t, look_up(t)))) continue;
+            if (!partly_seen(t, bad_of(look_up(t)))) continue;
 #pragma unroll 1
             for (int i = 0; i < SUBS * 32; ++i) {
                 const int key = t * KEYS + kw * SUBS * 32 + i;
@@ -850,23 +884,25 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a, Plan p, int dp) {
 
 int padded(int64_t dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
-// Sizes that a call's plan and its workspace share.
+// Sizes that a call's plan and its workspace share.  The host knows the rows of a sequence in the mean only:
+//   FEW   up to 32, one wave's: waves split the keys
+//   MANY  256 and more, heads of 128 to 256 bytes: eight waves of rows, which share a tile's moves
+//   SOME  between: four waves of rows, two for heads above 128
+enum { FEW, SOME, MANY };
 struct Sizes {
-    bool few;                 // rows of a sequence, in the mean: one wave's, which split the keys
-    int rows, keys, target, dp;
+    int shape, rows, keys, target, dp;
     int64_t slots;
 };
 Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads, int64_t dim, int type) {
     Sizes s;
-    const int64_t G = q_heads / heads;
+    const int64_t G = q_heads / heads, most = batch < n ? batch : n;   // sequences with new tokens, at most
     s.dp = padded(dim);
     const int row = s.dp * elem_size(type);
-    s.few = n * G <= 32 * (batch < n ? batch : n);
-    s.rows = s.few ? 32 : s.dp > 128 ? 64 : 128;
-    s.keys = s.few ? (row <= 512 ? 64 : 32) : row <= 512 ? 64 : 32;
-    const int64_t most = batch < n ? batch : n;               // sequences with new tokens
+    s.shape = n * G <= 32 * most ? FEW : n * G >= 256 * most && row >= 128 && row <= 256 ? MANY : SOME;
+    s.rows = s.shape == FEW ? 32 : s.shape == MANY ? 256 : s.dp > 128 ? 64 : 128;
+    s.keys = row <= 512 ? 64 : 32;
     const int64_t units = std::min<int64_t>(n * G, n * G / s.rows + most);   // tiles of rows
-    const int64_t total = s.few ? 2048 : 768;
+    const int64_t total = s.shape == FEW ? 2048 : 768;
     s.target = 0;
     if (units * heads < total && positions > LEAST_TILES * s.keys) s.target = (int)((total + heads - 1) / heads);
     s.slots = units + s.target;
@@ -874,8 +910,9 @@ Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int
 }
 
 template <int DT, int DP, int RW, int KW>
-hipError_t attend(const AttendArgs& a, const Plan& p, hipStream_t stream) {
+hipError_t attend(const AttendArgs& a, Plan p, hipStream_t stream) {
     using S = Shape<DT, DP, RW, KW>;
+    p.run = a.c.page_size % (S::MOVES * S::MOVE_ROWS) == 0 ? S::MOVES : a.c.page_size % S::MOVE_ROWS == 0;
     static std::atomic<uint64_t> prepared{0};
     hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_attend<S>), -1, S::LDS, prepared);
     if (e != hipSuccess) return e;
@@ -886,9 +923,13 @@ hipError_t attend(const AttendArgs& a, const Plan& p, hipStream_t stream) {
 }
 
 template <int DT, int DP>
-hipError_t attend_rows(const AttendArgs& a, const Plan& p, bool few, hipStream_t stream) {
+hipError_t attend_rows(const AttendArgs& a, const Plan& p, int shape, hipStream_t stream) {
     constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), KW = ROW <= 512 ? 2 : 1, RW = DP > 128 ? 2 : 4;
-    return few ? attend<DT, DP, 1, KW>(a, p, stream) : attend<DT, DP, RW, 1>(a, p, stream);
+    if (shape == FEW) return attend<DT, DP, 1, KW>(a, p, stream);
+    if constexpr (ROW >= 128 && ROW <= 256) {
+        if (shape == MANY) return attend<DT, DP, 8, 1>(a, p, stream);
+    }
+    return attend<DT, DP, RW, 1>(a, p, stream);
 }
 
 }  // namespace
@@ -924,17 +965,16 @@ hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStrea
         p.keys = s.keys;
         p.target = s.target;
         p.slots = (int)s.slots;
-        const int move_rows = 1024 / (s.dp * size);
         p.direct = moves_directly(a.c);
-        p.even = a.c.page_size % move_rows == 0;
+        p.run = 0;   // by the launch
         p.sums = static_cast<float*>(workspace);
         p.stats = p.sums + (s.target ? s.slots * a.c.heads * s.rows * s.dp : 0);
         hipError_t e;
         switch (s.dp) {
-            case 32: e = attend_rows<DT, 32>(a, p, s.few, stream); break;
-            case 64: e = attend_rows<DT, 64>(a, p, s.few, stream); break;
-            case 128: e = attend_rows<DT, 128>(a, p, s.few, stream); break;
-            default: e = attend_rows<DT, 256>(a, p, s.few, stream); break;
+            case 32: e = attend_rows<DT, 32>(a, p, s.shape, stream); break;
+            case 64: e = attend_rows<DT, 64>(a, p, s.shape, stream); break;
+            case 128: e = attend_rows<DT, 128>(a, p, s.shape, stream); break;
+            default: e = attend_rows<DT, 256>(a, p, s.shape, stream); break;
         }
         if (e != hipSuccess || !s.target) return e;
         const dim3 grid((unsigned)a.n, (unsigned)((a.q_heads + 3) / 4));

@@ -70,8 +70,8 @@ def attention64(x, scale, window=0, gone=None):
 
     Tolerances, with u = 2^-24, A = sum p |v| and S the largest sum |q_d k_d| scale of a row:
       scores   off by (D + 4) u S, in their products and sums, and 4 u S in their scaling and the maximum's;
-      weights  off by twice that relative, 4 u in 2^x, and half a step where they are rounded to the type (fp16: at least
-               2^-39 of the largest, its subnormal half step after 2^14);
+      weights  off by twice that relative, 4 u in 2^x, and half a step where they are rounded to the type (fp16: the largest
+               is kept at 2^11 or more, and half a subnormal step, 2^-25, is 2^-36 of that);
       sums     over L keys, of weights and of weighted values: 2 (L + 8) u;
       joining  pieces: 8 u;  the result: half a step of the type, of its subnormals for fp16 2^-25.
     """
@@ -105,10 +105,10 @@ def attention64(x, scale, window=0, gone=None):
         vmax = torch.nan_to_num(v).abs().amax(1, keepdim=True) if L else torch.zeros_like(A)
         score = (D + 8) * u * S
         rel = 2 * score + 2 * (L + 8) * u + 12 * u + (step(kind) if kind != "f32" else 0.0)
-        extra = L * 2.0 ** -39 * vmax + 2.0 ** -25 if kind == "f16" else 0.0
+        extra = L * 2.0 ** -36 * vmax + 2.0 ** -25 if kind == "f16" else 0.0
         tol[t] = (A * rel + extra).transpose(0, 1) + out[t].abs() * step(kind) * (1 + 2 ** -6)
         lse[t] = l[..., 0].T
-        tol_lse[t] = (score + (L + 16) * u)[..., 0].T + 4 * u * lse[t].abs().nan_to_num(posinf=0.0) + 2.0 ** -39 * L
+        tol_lse[t] = (score + (L + 16) * u)[..., 0].T + 4 * u * lse[t].abs().nan_to_num(posinf=0.0) + 2.0 ** -36 * L
     return out, lse, tol, tol_lse
 
 
