@@ -648,7 +648,7 @@ at_status at_paged_attention(const at_paged* cache, const void* q, int64_t q_tok
  * t / 32; mask_rows: device [n] int32, or NULL for row i of mask for row i;
  * rows outside [0, mask_count) have no mask.  valid: device [n] int32, the columns
  * that a row has (clamped to [0, vocab]; every column when NULL): others are neither read nor written.
- * n, vocab, past_len and n_bias are below 2^31. */
+ * past_len is below 2^30; n, vocab and n_bias are below 2^31. */
 at_status at_adjust_logits(const void* logits, int type, int64_t ld, int64_t n, int64_t vocab, void* out, int64_t ldo,
                            int itype, const void* past, int64_t ldp, int64_t past_len, const int32_t* lengths,
                            const int32_t* prompt_lengths, const float* repetition, const float* frequency,

@@ -331,8 +331,8 @@ at_status at_adjust_logits(const void* logits, int type, int64_t ld, int64_t n, 
     const at_status st = row_args(fn, type, ld, n, vocab, itype, 1.0f);
     if (st != AT_OK) return st;
     if (past_len < 0 || n_bias < 0 || mask_count < 0) return refuse(AT_E_INVALID, fn, "negative size");
-    if (past_len > SIZE_MAX_31 || n_bias > SIZE_MAX_31 || mask_count > SIZE_MAX_31)
-        return refuse(AT_E_UNSUPPORTED, fn, "sizes must be below 2^31");
+    if (past_len >= (int64_t)1 << 30 || n_bias > SIZE_MAX_31 || mask_count > SIZE_MAX_31)
+        return refuse(AT_E_UNSUPPORTED, fn, "the past must be below 2^30 tokens, other sizes below 2^31");
     if (ldo < vocab && n > 1) return refuse(AT_E_INVALID, fn, "output rows overlap (stride below vocab)");
     if (ldp < 0 || bias_ld < 0 || mask_ld < 0) return refuse(AT_E_INVALID, fn, "negative stride");
     if (!past) past_len = 0;

@@ -152,6 +152,33 @@ def test_rows(P, kind):
     Case(kind, 5, 700, past=40, seed=7, penalties=("freq",), prompt=False).check(P)
     Case(kind, 5, 700, past=40, seed=8, penalties=("pres",), lengths=False).check(P)
     Case(kind, 70, 30000, past=9000, biases=3, masks=3, seed=9, index="int32").check(P)
+    Case(kind, 300, 30001, past=33, biases=9, masks=3, seed=12, valid=True, pad=5).check(P)
+    # long rows: tables, more of the past than a table holds, pieces of a row
+    Case(kind, 130, 70001, past=3000, biases=256, masks=3, seed=13, valid=True).check(P)
+    Case(kind, 130, 40000, past=100, biases=257, seed=14).check(P)
+    Case(kind, 130, 40000, masks=2, seed=15, penalties=()).check(P)
+
+
+def test_long_rows(P):
+    """A table that is three quarters full, and a past that no table holds, of all different tokens and of few."""
+    import torch
+    for past in (12288, 12290):
+        for few in (False, True):
+            c = Case("bf16", 33, 131072, past=past, masks=2, seed=16, index="int32", lengths=False)
+            if not few:
+                c.a["past"][:] = np.random.default_rng(1).permutation(131072)[:past]
+            c.check(P)
+    # half a million columns and more: several pieces of the largest size
+    Case("f32", 9, 300001, past=500, biases=30, masks=2, seed=17).check(P)
+    Case("bf16", 5, 1100003, past=500, biases=30, masks=2, seed=18, valid=True).check(P)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("biases", [255, 256, 257, 3000])
+def test_many_biases(P, kind, biases):
+    """More biases of one segment than its list in LDS holds, many of them for the same tokens."""
+    for V in (100, 600):
+        Case(kind, 3, V, past=5, biases=biases, seed=biases).check(P)
 
 
 def test_one_token_many_times(P):

@@ -84,7 +84,7 @@ REFUSED = [(f, dict(a), s) for f in (append, attend) for a, s in CACHE_REFUSED] 
     (attend, dict(c_width=4096, c_table_ld=4096, ws=P16 + 8), INVALID),
     (adjust, dict(type=3), INVALID), (adjust, dict(itype=2), INVALID), (adjust, dict(n=-1), INVALID), (adjust, dict(ld=-1), INVALID),
     (adjust, dict(ldo=69), INVALID), (adjust, dict(out=P16, ldo=71), INVALID), (adjust, dict(past_len=-1), INVALID),
-    (adjust, dict(past_len=1 << 31), UNSUPPORTED), (adjust, dict(vocab=1 << 31, ldo=1 << 31), UNSUPPORTED),
+    (adjust, dict(past_len=1 << 30), UNSUPPORTED), (adjust, dict(n_bias=1 << 31), UNSUPPORTED), (adjust, dict(vocab=1 << 31, ldo=1 << 31), UNSUPPORTED),
     (adjust, dict(ldp=-1), INVALID), (adjust, dict(logits=None), INVALID), (adjust, dict(out=None), INVALID),
     (adjust, dict(bt=P16, n_bias=3), INVALID), (adjust, dict(bias=P16, n_bias=3), INVALID), (adjust, dict(past=P16 + 4), INVALID),
     (adjust, dict(out=ODD), INVALID), (adjust, dict(mask=P16 + 2), INVALID), (adjust, dict(valid=ODD), INVALID),
