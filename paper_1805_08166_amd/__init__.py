@@ -536,10 +536,11 @@ class _Torch:
         self.torch = torch
         self.types = {torch.float32: AT_F32, torch.bfloat16: AT_BF16, torch.float16: AT_F16}
         self.itypes = {torch.int32: AT_I32, torch.int64: AT_I64}
-        self.f32, self.i32 = torch.float32, torch.int32
+        self.f32, self.f64, self.i32 = torch.float32, torch.float64, torch.int32
         # the current stream's handle, without the object around it where torch has that
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.written = torch.autograd.graph.increment_version
 
 
@@ -612,7 +613,7 @@ def _call(func, device: int, stream, args, outs, workspace=None, need: int = 0):
     its pointer and size come before the stream."""
     T = _T()
     torch = T.torch
-    if torch.cuda.current_device() != device:
+    if T.device() != device:
         with torch.cuda.device(device):
             return _call(func, device, stream, args, outs, workspace, need)
     if need >= 0:
@@ -764,42 +765,62 @@ def at_orthogonalize(x, out, steps: int = 5, coef=NEWTON_SCHULZ, eps: float = 1e
 _PAGED = struct.Struct("=19q")
 
 
-def _heads(t, name, n=None, heads=None, dim=None, of=None):
-    """(pointer, token stride, head stride) of a device tensor [n, heads, dim]."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
+def _on_device(*tensors) -> int:
+    """The device that all of the tensors (None among them) are on."""
+    d = tensors[0].get_device()
+    if d < 0:
+        raise ValueError("the operators take device tensors")
+    for t in tensors:
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors are on different devices")
+    return d
+
+
+def _values(t, n, dtype, name):
+    """_vec of a tensor whose device _on_device looks at."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor of {n} values of {dtype}")
+    return t.data_ptr()
+
+
+def _heads(t, name, n, heads, dim, of):
+    """(pointer, token stride, head stride) of a tensor [n, heads, dim] of type `of`; None: any number."""
     sh = t.shape
-    if len(sh) != 3 or (n is not None and sh[0] != n) or (heads is not None and sh[1] != heads) or (
-            dim is not None and sh[2] != dim):
-        raise ValueError(f"{name} must be [{'n' if n is None else n}, {'heads' if heads is None else heads}, "
-                         f"{'dim' if dim is None else dim}], got {list(sh)}")
-    if of is not None and t.dtype != of:
+    if len(sh) != 3 or sh[2] != dim or (n is not None and sh[0] != n) or (heads is not None and sh[1] != heads):
+        raise ValueError(f"{name} must be [{'n' if n is None else n}, {'heads' if heads is None else heads}, {dim}], got {list(sh)}")
+    if t.dtype != of:
         raise ValueError(f"{name} must have the cache's type {of}, got {t.dtype}")
-    st = t.stride()
-    if sh[2] > 1 and st[2] != 1:
+    token, head, one = t.stride()
+    if one != 1 and dim > 1:
         raise ValueError(f"{name} must have contiguous heads")
-    return t.data_ptr(), st[0], st[1]
+    return t.data_ptr(), token, head
 
 
 def _paged(k_cache, v_cache, table, starts, lengths):
-    """The C side's at_paged of a cache and a batch."""
+    """The C side's at_paged of a cache and a batch, and the cache's type and shape, batch and table's width."""
     T = _T()
-    if not (k_cache.is_cuda and v_cache.is_cuda and table.is_cuda):
-        raise ValueError("the caches and the table must be device tensors")
-    sh = k_cache.shape
-    if len(sh) != 4 or v_cache.shape != sh or v_cache.dtype != k_cache.dtype:
+    sh, of = k_cache.shape, k_cache.dtype
+    if len(sh) != 4 or v_cache.shape != sh or v_cache.dtype != of:
         raise ValueError("the caches must be [pages, page_size, heads, dim] of one shape and type")
-    ks, vs = k_cache.stride(), v_cache.stride()
-    if sh[3] > 1 and (ks[3] != 1 or vs[3] != 1):
+    pages, size, heads, dim = sh
+    k0, k1, k2, k3 = k_cache.stride()
+    v0, v1, v2, v3 = v_cache.stride()
+    if dim > 1 and (k3 != 1 or v3 != 1):
         raise ValueError("the caches must have contiguous heads")
     if table.dim() != 2 or table.dtype != T.i32:
         raise ValueError("table must be int32 [batch, width]")
     batch, width = table.shape
-    if width > 1 and table.stride(1) != 1:
+    row, one = table.stride()
+    if width > 1 and one != 1:
         raise ValueError("table must have contiguous rows")
-    return _PAGED.pack(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                       _type(k_cache, "k_cache"), sh[0], sh[1], sh[2], sh[3], table.data_ptr(), table.stride(0), width,
-                       _vec(starts, batch + 1, T.i32, "starts"), _vec(lengths, batch, T.i32, "lengths"), batch)
+    type_ = T.types.get(of)
+    if type_ is None:
+        _type(k_cache, "k_cache")
+    return _PAGED.pack(k_cache.data_ptr(), v_cache.data_ptr(), k0, k1, k2, v0, v1, v2, type_, pages, size, heads, dim,
+                       table.data_ptr(), row, width, _values(starts, batch + 1, T.i32, "starts"),
+                       _values(lengths, batch, T.i32, "lengths"), batch), of, sh, batch, width
 
 
 def at_paged_append(k, v, k_cache, v_cache, table, starts, lengths, q=None, q_out=None, freqs=None,
@@ -814,24 +835,23 @@ def at_paged_append(k, v, k_cache, v_cache, table, starts, lengths, q=None, q_ou
     turning; pairs are (j, j + rot / 2), or (2j, 2j + 1) with interleaved; a
     turned pair is multiplied by rot_scale.  k_weight, q_weight: [dim], norm each head
     first.  All of one type: float32, bfloat16 or float16."""
-    T = _T()
-    paged = _paged(k_cache, v_cache, table, starts, lengths)
-    of, (_, _, heads, dim) = k_cache.dtype, k_cache.shape
-    n = k.shape[0]
-    kp, kt, kh = _heads(k, "k", n, heads, dim, of)
+    device = _on_device(k, v, k_cache, v_cache, table, starts, lengths, q, q_out, freqs, k_weight, q_weight)
+    paged, of, (_, _, heads, dim), _, _ = _paged(k_cache, v_cache, table, starts, lengths)
+    kp, kt, kh = _heads(k, "k", None, heads, dim, of)
+    n = len(k)
     vp, vt, vh = _heads(v, "v", n, heads, dim, of)
     qp, qt, qh, q_heads, op, ot, oh = None, 0, 0, 0, None, 0, 0
     if q is not None:
         if q_out is None:
             raise ValueError("q needs q_out")
-        q_heads = q.shape[1]
         qp, qt, qh = _heads(q, "q", n, None, dim, of)
+        q_heads = q.size(1)
         op, ot, oh = _heads(q_out, "q_out", n, q_heads, dim, of)
     rot = 2 * freqs.numel() if freqs is not None else 0
-    _call("at_paged_append", _one_device(k, v, k_cache, v_cache, table, starts, lengths, q, q_out, freqs, k_weight, q_weight),
-          stream, (paged, kp, kt, kh, vp, vt, vh, n, qp, qt, qh, q_heads, op, ot, oh, _vec(k_weight, dim, of, "k_weight"),
-                   _vec(q_weight, dim, of, "q_weight"), eps, _vec(freqs, rot // 2, T.torch.float64, "freqs"), rot,
-                   1 if interleaved else 0, rot_scale),
+    _call("at_paged_append", device, stream,
+          (paged, kp, kt, kh, vp, vt, vh, n, qp, qt, qh, q_heads, op, ot, oh, _values(k_weight, dim, of, "k_weight"),
+           _values(q_weight, dim, of, "q_weight"), eps, _values(freqs, rot // 2, _T().f64, "freqs"), rot,
+           1 if interleaved else 0, rot_scale),
           (k_cache, v_cache) if q is None else (k_cache, v_cache, q_out), need=-1)
 
 
@@ -847,16 +867,16 @@ def at_paged_attention(q, k_cache, v_cache, table, starts, lengths, out, scale=N
     the last `window` of them.  q, out: [n, q_heads, dim] of the caches' type;
     scale: 1 / sqrt(dim) where None; lse: float32 [n, q_heads] or None.  The
     caches, table, starts and lengths are those of at_paged_append."""
-    paged = _paged(k_cache, v_cache, table, starts, lengths)
-    of, (_, size, heads, dim) = k_cache.dtype, k_cache.shape
+    device = _on_device(q, k_cache, v_cache, table, starts, lengths, out, lse)
+    T = _T()
+    paged, of, (_, size, heads, dim), batch, width = _paged(k_cache, v_cache, table, starts, lengths)
     qp, qt, qh = _heads(q, "q", None, None, dim, of)
     n, q_heads = q.shape[:2]
     op, ot, oh = _heads(out, "out", n, q_heads, dim, of)
-    batch, width = table.shape
-    _call("at_paged_attention", _one_device(q, k_cache, v_cache, table, starts, lengths, out, lse), stream,
+    _call("at_paged_attention", device, stream,
           (paged, qp, qt, qh, n, q_heads, dim ** -0.5 if scale is None else scale, window, op, ot, oh,
-           _vec(lse, n * q_heads, _T().f32, "lse")), out if lse is None else (out, lse), workspace,
-          _bytes("at_paged_attention_workspace", n, batch, width * size, q_heads, heads, dim, _type(k_cache, "k_cache")))
+           _values(lse, n * q_heads, T.f32, "lse")), out if lse is None else (out, lse), workspace,
+          _bytes("at_paged_attention_workspace", n, batch, width * size, q_heads, heads, dim, T.types[of]))
 
 
 def at_adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None, repetition=None, presence=None,
@@ -869,6 +889,8 @@ def at_adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None
     int32 [masks, ceil(vocab / 32)], bit t of a row allows token t; mask_rows:
     int32 [n], each row's mask (-1 for none), or None for mask i for row i;
     valid: int32 [n], the columns that each row has."""
+    device = _on_device(logits, out, tokens, lengths, prompt_lengths, repetition, presence, frequency, bias_tokens, bias, mask,
+                        mask_rows, valid)
     T = _T()
     xp, xt, ld = _rows(logits, "logits")
     n, vocab = logits.shape
@@ -884,31 +906,34 @@ def at_adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None
         if tokens is not None and bti != ti:
             raise ValueError("bias_tokens must have the type of tokens")
         ti = bti
-        if bias is None or bias.shape != bias_tokens.shape or bias.dtype != T.f32 or bias.stride() != bias_tokens.stride():
+        if bias is None or bias.shape != bias_tokens.shape or bias.dtype != T.f32 or (
+                n > 1 and bias.stride(0) != ldb) or (n_bias > 1 and bias.stride(1) != 1):
             raise ValueError("bias must be float32, with the shape and strides of bias_tokens")
         b = bias.data_ptr()
     elif bias is not None:
         raise ValueError("bias needs bias_tokens")
     mp, ldm, masks = None, 0, 0
     if mask is not None:
-        if mask.dim() != 2 or mask.dtype != T.i32 or mask.shape[1] != (vocab + 31) // 32 or not mask.is_cuda or (
-                mask.shape[1] > 1 and mask.stride(1) != 1):
-            raise ValueError(f"mask must be an int32 device tensor [masks, {(vocab + 31) // 32}] with contiguous rows")
-        mp, ldm, masks = mask.data_ptr(), mask.stride(0), mask.shape[0]
-    _call("at_adjust_logits",
-          _one_device(logits, out, tokens, lengths, prompt_lengths, repetition, presence, frequency, bias_tokens, bias, mask,
-                      mask_rows, valid), stream,
-          (xp, xt, ld, n, vocab, op, ldo, ti, pp, ldp, past, _vec(lengths, n, T.i32, "lengths"),
-           _vec(prompt_lengths, n, T.i32, "prompt_lengths"), _vec(repetition, n, T.f32, "repetition"),
-           _vec(frequency, n, T.f32, "frequency"), _vec(presence, n, T.f32, "presence"), bt, b, n_bias, ldb, mp, ldm, masks,
-           _vec(mask_rows, n, T.i32, "mask_rows"), _vec(valid, n, T.i32, "valid")), out, need=-1)
+        words, sh = (vocab + 31) // 32, mask.shape
+        if len(sh) != 2 or mask.dtype != T.i32 or sh[1] != words or (words > 1 and mask.stride(1) != 1):
+            raise ValueError(f"mask must be an int32 device tensor [masks, {words}] with contiguous rows")
+        mp, ldm, masks = mask.data_ptr(), mask.stride(0), sh[0]
+    _call("at_adjust_logits", device, stream,
+          (xp, xt, ld, n, vocab, op, ldo, ti, pp, ldp, past, _values(lengths, n, T.i32, "lengths"),
+           _values(prompt_lengths, n, T.i32, "prompt_lengths"), _values(repetition, n, T.f32, "repetition"),
+           _values(frequency, n, T.f32, "frequency"), _values(presence, n, T.f32, "presence"), bt, b, n_bias, ldb, mp, ldm, masks,
+           _values(mask_rows, n, T.i32, "mask_rows"), _values(valid, n, T.i32, "valid")), out, need=-1)
 
 
 def _list(t, name, n):
-    """(pointer, token type, row stride, columns) of an int32 or int64 device tensor [n, columns]."""
+    """(pointer, token type, row stride, columns) of an int32 or int64 tensor [n, columns]."""
     ti = _T().itypes.get(t.dtype)
     if ti is None:
         raise ValueError(f"{name} must be int32 or int64, got {t.dtype}")
-    if not t.is_cuda or t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be a device tensor [{n}, ...] with contiguous rows")
-    return t.data_ptr(), ti, t.stride(0), t.shape[1]
+    sh = t.shape
+    if len(sh) != 2 or sh[0] != n:
+        raise ValueError(f"{name} must be [{n}, ...], got {list(sh)}")
+    row, one = t.stride()
+    if one != 1 and sh[1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), ti, row, sh[1]

@@ -406,8 +406,8 @@ hipError_t adjust(const AdjustArgs& a, int64_t run, hipStream_t stream) {
     const int64_t fit = (((int64_t)1 << 32) - 1) / THREADS / groups, most = fit > 0 ? fit : 1;
     for (int64_t row = 0; row < a.n; row += most) {
         const int64_t m = a.n - row < most ? a.n - row : most;
-        k_adjust<DT, THREADS, PACKS, HELD><<<(unsigned)(m * groups), THREADS, 0, stream>>>(a, row, (int)groups, (int)run);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_direct(&k_adjust<DT, THREADS, PACKS, HELD>, dim3((unsigned)(m * groups)), THREADS, 0, stream, a,
+                                           row, (int)groups, (int)run);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -425,8 +425,8 @@ hipError_t adjust_long(const AdjustArgs& a, int slots, hipStream_t stream) {
     const int64_t fit = (((int64_t)1 << 32) - 1) / LONG_THREADS / groups, most = fit > 0 ? fit : 1;
     for (int64_t row = 0; row < a.n; row += most) {
         const int64_t m = a.n - row < most ? a.n - row : most;
-        k_adjust_long<DT><<<(unsigned)(m * groups), LONG_THREADS, (size_t)slots * 8, stream>>>(a, row, (int)groups, piece, slots);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_direct(&k_adjust_long<DT>, dim3((unsigned)(m * groups)), LONG_THREADS, (size_t)slots * 8,
+                                           stream, a, row, (int)groups, piece, slots);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -209,13 +209,8 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t stream) {
         for (int64_t t = 0; t < a.n; t += GROUPS_MAX / parts) {
             const int64_t m = a.n - t < GROUPS_MAX / parts ? a.n - t : GROUPS_MAX / parts;
             const dim3 grid((unsigned)m, (unsigned)parts);
-            if (vec == WIDE)
-                k_append<DT, WIDE><<<grid, THREADS, 0, stream>>>(a, size, t, group, parts);
-            else if (vec == 4)
-                k_append<DT, 4><<<grid, THREADS, 0, stream>>>(a, size, t, group, parts);
-            else
-                k_append<DT, 1><<<grid, THREADS, 0, stream>>>(a, size, t, group, parts);
-            const hipError_t e = hipGetLastError();
+            const auto kern = vec == WIDE ? &k_append<DT, WIDE> : vec == 4 ? &k_append<DT, 4> : &k_append<DT, 1>;
+            const hipError_t e = launch_direct(kern, grid, THREADS, 0, stream, a, size, t, group, parts);
             if (e != hipSuccess) return e;
         }
         return hipSuccess;

@@ -43,7 +43,7 @@ template <>
 struct Mat<AT_BF16> {
     typedef __bf16 Frag __attribute__((ext_vector_type(8)));
     // P is rounded to bf16, off by half a step, 2^-9 of it at most, as the values that it multiplies are.
-    static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
+    [[maybe_unused]] static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
@@ -52,7 +52,7 @@ template <>
 struct Mat<AT_F16> {
     typedef _Float16 Frag __attribute__((ext_vector_type(8)));
     // P times 2^11, at most 2^15 with the slack of its maximum: below 2^-14 steps are 2^-24, off by 2^-36 of the largest at most.
-    static constexpr float SHIFT = 11.0f, SLACK = 4.0f;
+    [[maybe_unused]] static constexpr float SHIFT = 11.0f, SLACK = 4.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
     }
@@ -60,7 +60,7 @@ struct Mat<AT_F16> {
 template <>
 struct Mat<AT_F32> {
     typedef float Frag __attribute__((ext_vector_type(4)));
-    static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
+    [[maybe_unused]] static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
@@ -75,6 +75,7 @@ struct Plan {
     int rows;            // of a tile
     int keys;            // of a tile
     int target;          // pieces a head that the keys are cut into, about; 0: whole sequences
+    int round, brief;    // or `round`, a workgroup a CU, where those have `brief` tiles at most
     int slots;           // pieces a head, at most
     int direct;          // rows of the cache are whole aligned 16 bytes
     int run;             // moves whose rows lie in one page: all of a wave's, 1, or 0 where those of one need not
@@ -82,12 +83,13 @@ struct Plan {
     float* stats;        // [slot][head][row][2]: maximum and sum
 };
 constexpr int LEAST_TILES = 2;   // of a piece
+constexpr int CUS = 256;
 
-// What a sequence has to do: tiles of rows, and the key tiles [lo, hi) that any of them sees.
+// What a sequence has to do: tiles of rows, and the key tiles that one of them sees at most.
 struct Task {
     int first, count, length;   // new tokens; positions in the cache
     int64_t position;           // of the first new token
-    int row_tiles, lo, hi;
+    int row_tiles, seen;
 };
 __device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int b) {
     Task t;
@@ -98,12 +100,16 @@ __device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int 
     t.position = l - s.count;
     t.length = (int)(l < 0 ? 0 : l < room ? l : room);
     t.row_tiles = (int)(((uint32_t)s.count * p.group.d + p.rows - 1) / p.rows);   // fewer than 2^31 rows, tiles of at most 256
-    int64_t lo = a.window > 0 ? t.position - a.window + 1 : 0;
-    lo = lo < 0 ? 0 : lo < t.length ? lo : t.length;
-    t.lo = (int)(lo / p.keys);
-    t.hi = (t.length + p.keys - 1) / p.keys;
+    t.seen = (t.length + p.keys - 1) / p.keys;
+    if (a.window > 0) {   // the window of the first of a tile's tokens, and the others
+        const int64_t w = (a.window + p.rows + p.keys - 1) / p.keys + 1;
+        if (w < t.seen) t.seen = (int)w;
+    }
     return t;
 }
+
+// A value that all lanes have, as the compiler cannot tell.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // Sums of a wave's lanes up to each one, by moves within the vector unit.
 template <int CTRL, int ROWS>
@@ -149,17 +155,32 @@ __device__ __forceinline__ double wave_sum(double v) {
     return __builtin_bit_cast(double, (int64_t)((uint64_t)high << 32 | low));
 }
 
+__device__ __forceinline__ double work_of(const Task& t) { return (double)t.row_tiles * (double)t.seen; }
+__device__ __forceinline__ int pieces_of(const Task& t, int tiles) {
+    const int n = (int)((uint32_t)(t.seen + tiles - 1) / (uint32_t)tiles);   // below 2^31
+    return n < 1 ? 1 : n;
+}
+
 // Key tiles of a piece, of all sequences' row tiles times their key tiles: whole numbers, which 64 bits add exactly in
 // any order, so that both kernels find the same.  More than the quotient, as the workspace has room for `target` pieces
 // and one for each tile of rows.
 __device__ __forceinline__ int piece_tiles(double work, const Plan& p) {
-    const double each = work / (double)p.target;
+    const double each = work / (double)(work <= (double)p.round * p.brief ? p.round : p.target);
     return each < (double)LEAST_TILES ? LEAST_TILES : each < 0x1p30 ? (int)each + 1 : 1 << 30;
 }
-__device__ __forceinline__ double work_of(const Task& t) { return (double)t.row_tiles * (double)(t.hi - t.lo); }
-__device__ __forceinline__ int pieces_of(const Task& t, int tiles) {
-    const int n = (int)((uint32_t)(t.hi - t.lo + tiles - 1) / (uint32_t)tiles);   // below 2^31
-    return n < 1 ? 1 : n;
+// The same by a wave whose lanes have a sequence each.  Pieces of a sequence are rounded up, so that there may be more
+// than run at once, which would take brief work twice as long: their length goes up until there are not.
+__device__ __forceinline__ int piece_tiles(const Task& t, const Plan& p) {
+    const double work = wave_sum(work_of(t));
+    const int tiles = uniform(piece_tiles(work, p));
+    if (work > (double)p.round * p.brief) return tiles;
+    int longer = tiles;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        if (__builtin_amdgcn_readlane(wave_scan(t.row_tiles * pieces_of(t, longer)), 63) <= p.round) return longer;
+        longer = std::min(longer + (longer + 7) / 8, 1 << 30);
+    }
+    return tiles;
 }
 
 // A piece's place: a sequence, and the piece's number among those of the sequence.
@@ -173,7 +194,7 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, in
     if (batch <= 64) {   // a lane a sequence, each wave for itself
         Task t = {};
         if (lane < batch) t = task_of(a, p, lane);
-        const int tiles = p.target ? piece_tiles(wave_sum(work_of(t)), p) : 1 << 30;
+        const int tiles = p.target ? piece_tiles(t, p) : 1 << 30;
         const int n = t.row_tiles * pieces_of(t, tiles), upto = wave_scan(n);
         if (FIRST_OF) return {b, __builtin_amdgcn_readlane(upto - n, b), tiles};
         const uint64_t past = __ballot(upto > slot && lane < batch);
@@ -225,12 +246,13 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, in
     return {scratch[WAVES], scratch[WAVES + 1], tiles};
 }
 
-template <int DT_, int DP_, int ROW_WAVES_, int KEY_WAVES_>
+// DP: the values that a head has room for in LDS, a power of two; USED: those that products are made of.
+template <int DT_, int DP_, int USED_, int ROW_WAVES_, int KEY_WAVES_>
 struct Shape {
-    static constexpr int DT = DT_, DP = DP_;
+    static constexpr int DT = DT_, DP = DP_, USED = USED_;
     // Heads above 128 are halved by columns of the output: two waves compute the same weights, each for its half of the
     // values, as one wave's registers do not hold the queries and all of the output.
-    static constexpr int COL_WAVES = DP > 128 ? 2 : 1, COLS = DP / COL_WAVES;
+    static constexpr int COL_WAVES = DP > 128 ? 2 : 1, COLS = USED / COL_WAVES;
     static constexpr int ROW_WAVES = ROW_WAVES_, KEY_WAVES = KEY_WAVES_, WAVES = ROW_WAVES * KEY_WAVES * COL_WAVES;
     static constexpr int THREADS = WAVES * 64;
     static constexpr int SIZE = sizeof(typename Elem<DT>::T), VEC = 16 / SIZE;
@@ -277,8 +299,6 @@ __device__ __forceinline__ float halves(float v, F&& f) {
     const uint32_t low = r[0], high = r[1];
     return f(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
 }
-// A value that all lanes have, as the compiler cannot tell.
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <class T>
 __device__ __forceinline__ bool is_finite(T v) {
@@ -288,7 +308,7 @@ __device__ __forceinline__ bool is_finite(T v) {
 template <class S>
 __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a, Plan p) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host needs its launch stub only, and does not know all of the device's instructions
-    constexpr int DT = S::DT, DP = S::DP, RW = S::ROW_WAVES, KW = S::KEY_WAVES;
+    constexpr int DT = S::DT, DP = S::DP, USED = S::USED, RW = S::ROW_WAVES, KW = S::KEY_WAVES;
     using T = typename Elem<DT>::T;
     using M = Mat<DT>;
     using Frag = typename M::Frag;
@@ -324,8 +344,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int hi = hi64 < 0 ? 0 : (int)hi64;
     int tile = (int)((lo < hi ? lo : 0) / KEYS), tile_end = lo < hi ? (hi + KEYS - 1) / KEYS : 0;
     {
-        const int64_t from = (int64_t)task.lo + (int64_t)piece * tiles, to = from + tiles;
-        if (tile < from) tile = (int)from;
+        const int64_t from = tile + (int64_t)piece * tiles, to = from + tiles;
+        tile = from < tile_end ? (int)from : tile_end;
         if (tile_end > to) tile_end = (int)to;
     }
 
@@ -369,6 +389,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     // in bytes; those of tokens are below 2^27 where moves go directly
     const uint64_t k_page = (uint64_t)a.c.k_page * S::SIZE, v_page = (uint64_t)a.c.v_page * S::SIZE;
     const uint32_t k_token = (uint32_t)a.c.k_token * S::SIZE, v_token = (uint32_t)a.c.v_token * S::SIZE;
+    const uint32_t bytes = dim * S::SIZE;   // past them, zeros lie in LDS already
     auto stage = [&](int t, char* to, const Ids& ids, const Bad& bad) {
         char* to_k = to + wave * MOVES * 1024;
         char* to_v = to_k + S::TILE;
@@ -382,13 +403,13 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                 asm("" : "+s"(low), "+s"(high));   // or each move's lanes would keep an address of their own
                 return reinterpret_cast<const char*>((uint64_t)high << 32 | low);
             };
-            if (__builtin_expect(p.run && dim == DP && hi - t * KEYS >= KEYS && !bad.any(), 1)) {
+            if (__builtin_expect(p.run && (USED < DP || dim == DP) && hi - t * KEYS >= KEYS && !bad.any(), 1)) {
                 // all rows of a move are there, in one page
                 auto move = [&](int q, const char* k, const char* v) {
                     const int row = row0_ + q * MOVE_ROWS + lane_row;
                     const uint32_t ck = (lane_chunk ^ key_swizzle<CHUNKS>(row)) * 16, cv = (lane_chunk ^ value_swizzle<CHUNKS, S::SIZE>(row)) * 16;
-                    __builtin_amdgcn_global_load_lds(k + (k_lane + ck), to_k + q * 1024, 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds(v + (v_lane + cv), to_v + q * 1024, 16, 0, 0);
+                    if (USED == DP || ck < bytes) __builtin_amdgcn_global_load_lds(k + (k_lane + ck), to_k + q * 1024, 16, 0, 0);
+                    if (USED == DP || cv < bytes) __builtin_amdgcn_global_load_lds(v + (v_lane + cv), to_v + q * 1024, 16, 0, 0);
                 };
                 if (p.run > 1) {
                     const int pos = t * KEYS + row0_;
@@ -410,7 +431,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                     }
                 }
             } else {
-                // row by row, with zeros for those that are not there (past dim, zeros lie in LDS already)
+                // row by row, with zeros for those that are not there
 #pragma unroll 1
                 for (int i = 0; i < MOVES * MOVE_ROWS; ++i) {
                     const int q = i / MOVE_ROWS, row = row0_ + i, pos = t * KEYS + row;
@@ -420,8 +441,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                     if (pos < hi && id < pages) {
                         const char* k = address(k_head, k_page, k_token, id, pos, at);
                         const char* v = address(v_head, v_page, v_token, id, pos, at);
-                        if ((int)ck < dim * S::SIZE) __builtin_amdgcn_global_load_lds(k + ck, to_k + q * 1024, 16, 0, 0);
-                        if ((int)cv < dim * S::SIZE) __builtin_amdgcn_global_load_lds(v + cv, to_v + q * 1024, 16, 0, 0);
+                        if (ck < bytes) __builtin_amdgcn_global_load_lds(k + ck, to_k + q * 1024, 16, 0, 0);
+                        if (cv < bytes) __builtin_amdgcn_global_load_lds(v + cv, to_v + q * 1024, 16, 0, 0);
                     } else {
                         *reinterpret_cast<float4v*>(to_k + q * 1024 + lane * 16) = float4v{};
                         *reinterpret_cast<float4v*>(to_v + q * 1024 + lane * 16) = float4v{};
@@ -471,11 +492,11 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     // Whether some row of this workgroup does not see all of a tile.
     const int all_limit = limit_of(first_pos), all_low = low_of(last_pos);
     auto partly_seen = [&](int t, const Bad& bad) { return t * KEYS + KEYS - 1 > all_limit || t * KEYS < all_low || bad.any(); };
-    constexpr int STEPS = CHUNKS / 2;
+    constexpr int STEPS = USED / (2 * VEC);
     Frag q[STEPS];
     {
         const T* x = static_cast<const T*>(a.q.p) + (int64_t)token * a.q.token + q_head * a.q.head;
-        if (__builtin_expect(dim == DP, 1)) {   // (rows past the last one repeat it)
+        if (__builtin_expect(dim == USED, 1)) {   // (rows past the last one repeat it)
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 const Pack<T, VEC> w = load_pack<T, VEC>(x + (2 * s + half) * VEC);
@@ -782,8 +803,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
             s_stats[wave][mine][1] = sum;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < rows * (DP / 4); i += S::THREADS) {
-            const int row_ = i / (DP / 4), d = i % (DP / 4) * 4, w0 = row_ / 32 + d / COLS * RW * KW;
+        for (int i = threadIdx.x; i < rows * (USED / 4); i += S::THREADS) {
+            const int row_ = i / (USED / 4), d = i % (USED / 4) * 4, w0 = row_ / 32 + d / COLS * RW * KW;
             float most = -inf;
 #pragma unroll
             for (int w = 0; w < KW; ++w) most = fmaxf(most, s_stats[w * RW + w0][row_ & 31][0]);
@@ -885,12 +906,20 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a, Plan p, int dp) {
 int padded(int64_t dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 // Sizes that a call's plan and its workspace share.  The host knows the rows of a sequence in the mean only:
-//   FEW   up to 32, one wave's: waves split the keys
-//   MANY  256 and more, heads of 128 to 256 bytes: eight waves of rows, which share a tile's moves
-//   SOME  between: four waves of rows, two for heads above 128
+//   FEW   fp32 heads up to 128, up to 32 rows, one wave's: waves split the keys, as the products take longest.  A token of
+//         128 values over 8000 keys of 8 heads, 4 query heads each: 39.8 us, SOME 52.9; bf16, where moves take longest,
+//         22.0 and 20.8
+//   MANY  rows of 128 to 256 bytes, 256 rows and more: eight waves of rows, which share a tile's moves.  bf16, 32 query heads:
+//         512 tokens over 32000 before them 283 us, SOME 308; 8192 tokens 590 and 601.  Not where SOME fills the chip
+//         and MANY does not, and has to cut its keys: 1024 tokens 59 us, SOME 39
+//   SOME  the others: four waves of rows, two for heads above 128
+// Keys are cut where tiles of rows leave some of the 256 CUs empty, and not before: 2048 tokens, 520 tiles, 67 us whole and
+// 128 cut; but up to 768 tiles where each is a sequence, as lengths differ: 64 sequences of up to 16384 keys, 512 tiles, 477 us
+// whole and 416 cut.  Pieces are a workgroup a CU where those have few tiles, or MANY's waves, and otherwise three, which even out: a token
+// over 32000 keys of 8 heads 36.2 us by one a CU, 52.2 by three; 64 sequences of up to 16384 keys 490 and 416.
 enum { FEW, SOME, MANY };
 struct Sizes {
-    int shape, rows, keys, target, dp;
+    int shape, rows, keys, target, round, brief, dp;
     int64_t slots;
 };
 Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int64_t heads, int64_t dim, int type) {
@@ -898,38 +927,43 @@ Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int
     const int64_t G = q_heads / heads, most = batch < n ? batch : n;   // sequences with new tokens, at most
     s.dp = padded(dim);
     const int row = s.dp * elem_size(type);
-    s.shape = n * G <= 32 * most ? FEW : n * G >= 256 * most && row >= 128 && row <= 256 ? MANY : SOME;
+    auto units = [&](int rows) { return std::min<int64_t>(n * G, n * G / rows + most); };   // tiles of rows
+    auto fills = [&](int rows) { return units(rows) * heads >= CUS; };
+    const bool many = n * G >= 256 * most && row >= 128 && row <= 256;
+    s.shape = type == AT_F32 && s.dp <= 128 && n * G <= 32 * most ? FEW : many && (fills(256) || !fills(128)) ? MANY : SOME;
     s.rows = s.shape == FEW ? 32 : s.shape == MANY ? 256 : s.dp > 128 ? 64 : 128;
     s.keys = row <= 512 ? 64 : 32;
-    const int64_t units = std::min<int64_t>(n * G, n * G / s.rows + most);   // tiles of rows
-    const int64_t total = s.shape == FEW ? 2048 : 768;
-    s.target = 0;
-    if (units * heads < total && positions > LEAST_TILES * s.keys) s.target = (int)((total + heads - 1) / heads);
-    s.slots = units + s.target;
+    const int64_t limit = n * G <= s.rows * most ? 3 * CUS : CUS;
+    s.target = units(s.rows) * heads < limit && positions > LEAST_TILES * s.keys ? (int)((3 * CUS + heads - 1) / heads) : 0;
+    s.round = (int)std::max<int64_t>(1, CUS / heads);
+    // an fp32 tile's products take four times as long as a 16-bit one's moves: 700 tokens of 12 heads 112 us, with 16 121
+    s.brief = s.shape == MANY ? 1 << 30 : type == AT_F32 && s.shape == SOME ? 4 : 16;
+    s.slots = units(s.rows) + (s.target ? std::max(s.target, s.round) : 0);
     return s;
 }
 
-template <int DT, int DP, int RW, int KW>
+template <int DT, int DP, int USED, int RW, int KW>
 hipError_t attend(const AttendArgs& a, Plan p, hipStream_t stream) {
-    using S = Shape<DT, DP, RW, KW>;
+    using S = Shape<DT, DP, USED, RW, KW>;
     p.run = a.c.page_size % (S::MOVES * S::MOVE_ROWS) == 0 ? S::MOVES : a.c.page_size % S::MOVE_ROWS == 0;
     static std::atomic<uint64_t> prepared{0};
     hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_attend<S>), -1, S::LDS, prepared);
     if (e != hipSuccess) return e;
     const int64_t groups = (int64_t)p.slots * a.c.heads;
     if (groups > (((int64_t)1 << 32) - 1) / S::THREADS) return hipErrorInvalidValue;
-    k_attend<S><<<(unsigned)groups, S::THREADS, S::LDS, stream>>>(a, p);
-    return hipGetLastError();
+    return launch_direct(&k_attend<S>, dim3((unsigned)groups), S::THREADS, S::LDS, stream, a, p);
 }
 
-template <int DT, int DP>
+template <int DT, int DP, int USED>
 hipError_t attend_rows(const AttendArgs& a, const Plan& p, int shape, hipStream_t stream) {
-    constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), KW = ROW <= 512 ? 2 : 1, RW = DP > 128 ? 2 : 4;
-    if (shape == FEW) return attend<DT, DP, 1, KW>(a, p, stream);
-    if constexpr (ROW >= 128 && ROW <= 256) {
-        if (shape == MANY) return attend<DT, DP, 8, 1>(a, p, stream);
+    constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), RW = DP > 128 ? 2 : 4;
+    if constexpr (DT == AT_F32 && DP <= 128) {
+        if (shape == FEW) return attend<DT, DP, USED, 1, 2>(a, p, stream);
     }
-    return attend<DT, DP, RW, 1>(a, p, stream);
+    if constexpr (ROW >= 128 && ROW <= 256) {
+        if (shape == MANY) return attend<DT, DP, USED, 8, 1>(a, p, stream);
+    }
+    return attend<DT, DP, USED, RW, 1>(a, p, stream);
 }
 
 }  // namespace
@@ -957,34 +991,37 @@ hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStrea
     return with_type((int)a.c.type, [&](auto type) -> hipError_t {
         constexpr int DT = type.value;
         const Sizes s = sizes_of(a.n, a.c.batch, a.c.width * a.c.page_size, a.q_heads, a.c.heads, a.c.dim, DT);
-        const int size = elem_size(DT);
         Plan p;
         p.size = divider(a.c.page_size);
         p.group = divider(a.q_heads / a.c.heads);
         p.rows = s.rows;
         p.keys = s.keys;
         p.target = s.target;
+        p.round = s.round;
+        p.brief = s.brief;
         p.slots = (int)s.slots;
         p.direct = moves_directly(a.c);
         p.run = 0;   // by the launch
         p.sums = static_cast<float*>(workspace);
         p.stats = p.sums + (s.target ? s.slots * a.c.heads * s.rows * s.dp : 0);
         hipError_t e;
-        switch (s.dp) {
-            case 32: e = attend_rows<DT, 32>(a, p, s.shape, stream); break;
-            case 64: e = attend_rows<DT, 64>(a, p, s.shape, stream); break;
-            case 128: e = attend_rows<DT, 128>(a, p, s.shape, stream); break;
-            default: e = attend_rows<DT, 256>(a, p, s.shape, stream); break;
-        }
+        const int64_t dim = a.c.dim;
+        if (dim <= 32)
+            e = attend_rows<DT, 32, 32>(a, p, s.shape, stream);
+        else if (dim <= 64)
+            e = attend_rows<DT, 64, 64>(a, p, s.shape, stream);
+        else if (dim <= 96)
+            e = attend_rows<DT, 128, 96>(a, p, s.shape, stream);
+        else if (dim <= 128)
+            e = attend_rows<DT, 128, 128>(a, p, s.shape, stream);
+        else if (dim <= 192)
+            e = attend_rows<DT, 256, 192>(a, p, s.shape, stream);
+        else
+            e = attend_rows<DT, 256, 256>(a, p, s.shape, stream);
         if (e != hipSuccess || !s.target) return e;
         const dim3 grid((unsigned)a.n, (unsigned)((a.q_heads + 3) / 4));
-        if (s.dp <= 64)
-            k_join<DT, 1><<<grid, 256, 0, stream>>>(a, p, s.dp);
-        else if (s.dp == 128)
-            k_join<DT, 2><<<grid, 256, 0, stream>>>(a, p, s.dp);
-        else
-            k_join<DT, 4><<<grid, 256, 0, stream>>>(a, p, s.dp);
-        return hipGetLastError();
+        const auto join = s.dp <= 64 ? &k_join<DT, 1> : s.dp == 128 ? &k_join<DT, 2> : &k_join<DT, 4>;
+        return launch_direct(join, grid, 256, 0, stream, a, p, s.dp);
     });
 }
 

@@ -317,6 +317,8 @@ at_status at_paged_attention(const at_paged* cache, const void* q, int64_t q_tok
     st = workspace_args(fn, workspace, workspace_bytes,
                         paged_attention_workspace(n, cache->batch, cache->width * cache->page_size, q_heads, cache->heads, cache->dim, type));
     if (st != AT_OK) return st;
+    // positions are below 2^31, so that longer windows see the same
+    window = std::min<int64_t>(window, (int64_t)1 << 32);
     const AttendArgs a{*cache, {q, q_token, q_head}, {out, o_token, o_head}, lse, n, q_heads, scale, window};
     return done(launch_paged_attention(a, workspace, (hipStream_t)stream), fn);
 }

@@ -163,6 +163,18 @@ struct OrthoArgs {
 int64_t ortho_workspace(int64_t batch, int64_t rows, int64_t cols, bool fp16_products);
 hipError_t launch_ortho(const OrthoArgs& a, void* workspace, hipStream_t stream);
 
+// A launch without the compiler's launch stub, which copies every argument once more: the smallest calls are bound by the host.
+template <class T>
+struct Whole {
+    using type = T;
+};
+template <class... A>
+hipError_t launch_direct(void (*kern)(A...), dim3 grid, unsigned threads, size_t lds, hipStream_t stream,
+                         const typename Whole<A>::type&... args) {
+    void* ptrs[] = {const_cast<void*>(static_cast<const void*>(&args))...};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kern), grid, dim3(threads), ptrs, lds, stream);
+}
+
 // Rows of heads by token: element [token][head][0] is at p + token * token_ld + head * head_ld.
 template <class P>
 struct Heads {

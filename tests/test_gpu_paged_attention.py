@@ -46,6 +46,14 @@ def test_head_sizes(P, R, kind, dim):
     check(P, R, R.Batch(kind, [70, 1, 33], [0, 5, 200], 4, 2, dim, page=16, seed=dim + 1))
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim", [72, 80, 88, 96, 104, 120, 160, 176, 192, 208])
+def test_padded_heads_in_whole_tiles(P, R, kind, dim):
+    """Heads that leave part of their padding unused, over keys of which every query sees whole tiles."""
+    check(P, R, R.Batch(kind, [300, 70], [700, 5], 4, 2, dim, page=16, seed=dim))
+    check(P, R, R.Batch(kind, [40, 1], [900, 640], 4, 2, dim, page=64, seed=dim + 1), window=500)
+
+
 @pytest.mark.parametrize("kind,dim", [("f32", 255), ("bf16", 255), ("f16", 132)])
 def test_large_heads_of_odd_rows_are_refused(P, R, kind, dim):
     for new in ([1], [70]):
@@ -101,6 +109,22 @@ def test_windows(P, R, kind, window):
         torch.cuda.synchronize()
         R.close(x.lse, want[1], want[3], "lse")
         R.close(x.out, want[0], want[2], "out")
+
+
+@pytest.mark.parametrize("window", [64, 1000, 3000, 2 ** 63 - 1])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_windows_of_cut_keys(P, R, kind, window):
+    """Pieces start where the window of their rows does."""
+    for new, ctx, heads in (([1, 1], [6000, 2500], 4), ([40], [5000], 4), ([300, 20], [4000, 100], 2)):
+        check(P, R, R.Batch(kind, new, ctx, heads, 2, 80 if kind == "f32" else 128, page=24, seed=len(new)), window=window)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new,ctx,heads,kv", [([500, 260, 500], [0, 30, 900], 16, 8), ([600], [0], 32, 16), ([1200], [300], 4, 4),
+                                              ([64] * 5, [100, 0, 2000, 5, 300], 16, 4), ([2100], [0], 8, 8)])
+def test_row_tiles(P, R, kind, new, ctx, heads, kv):
+    """Tiles of rows of every size, with keys cut and whole."""
+    check(P, R, R.Batch(kind, new, ctx, heads, kv, 64, page=16, seed=len(new)))
 
 
 @pytest.mark.parametrize("ctx", [0, 1, 31, 32, 33, 63, 64, 127, 128, 129, 511, 512, 513, 2047, 5000])
