@@ -438,14 +438,20 @@ hipError_t launch_adjust(const AdjustArgs& a, hipStream_t stream) {
     return with_type(a.type, [&](auto type) -> hipError_t {
         constexpr int DT = type.value, VEC = DT == AT_F32 ? 4 : 8;
         constexpr int64_t WIDE = 512 * 2 * VEC;   // columns of a long segment
+        // a wave a row (4000 rows of 500 bf16 15.7 us, 31.4 by workgroups of four)
         if (a.vocab <= 64 * VEC) return adjust<DT, 64, 1, 4>(a, 1, stream);
-        const int64_t all = a.n * ((a.vocab + WIDE - 1) / WIDE), marks = a.past_len + a.n_bias;
-        if (a.vocab >= 16384 && all >= 512 && marks <= MOST_SLOTS / 4 * 3 && a.n_bias <= LISTED) {
+        const int64_t segments = (a.vocab + WIDE - 1) / WIDE, all = a.n * segments, marks = a.past_len + a.n_bias;
+        // The table's own time has to be made up by several segments of many rows (bf16, 131072 columns: 512
+        // rows with pasts of 2000 tokens 101 us and 112 by segments, with 8192 256 rows 61 and 67, 128 rows 41 and 37; of
+        // 32000 columns 1024 rows 57 and 67, 2000 rows 174 and 172).  Tables are three quarters full at most.
+        if (segments >= 4 && all >= 4096 && marks <= MOST_SLOTS / 4 * 3 && a.n_bias <= LISTED) {
             int slots = 64;
             while (slots < MOST_SLOTS && slots < 2 * marks) slots *= 2;
             return adjust_long<DT>(a, slots, stream);
         }
-        if (all < 1024) return adjust<DT, 256, 1, 8>(a, 1, stream);
+        // Small workgroups where there are few, and for short rows whose past they hold (bf16: 16 rows of 131072 columns 8.5
+        // and 9.0 us, 32 rows 22 and 14; 2000 rows of 12000 columns 55 and 65, of 32000 columns 138 and 126).
+        if (all < 384 || (segments <= 2 && a.past_len <= 2048)) return adjust<DT, 256, 1, 8>(a, 1, stream);
         return adjust<DT, 512, 2, 16>(a, (all + 511) / 512, stream);
     });
 }

@@ -82,7 +82,7 @@ struct Plan {
     float* sums;         // [slot][head][row][dim padded]
     float* stats;        // [slot][head][row][2]: maximum and sum
 };
-constexpr int LEAST_TILES = 2;   // of a piece
+constexpr int LEAST_TILES = 1;   // of a piece
 constexpr int CUS = 256;
 
 // What a sequence has to do: tiles of rows, and the key tiles that one of them sees at most.

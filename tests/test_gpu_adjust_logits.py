@@ -168,9 +168,25 @@ def test_long_rows(P):
             if not few:
                 c.a["past"][:] = np.random.default_rng(1).permutation(131072)[:past]
             c.check(P)
-    # half a million columns and more: several pieces of the largest size
     Case("f32", 9, 300001, past=500, biases=30, masks=2, seed=17).check(P)
     Case("bf16", 5, 1100003, past=500, biases=30, masks=2, seed=18, valid=True).check(P)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_tables(P, kind):
+    """Many long rows: tables of every filling, none, and a past that no table holds."""
+    V = 16387 if kind == "f32" else 32771
+    Case(kind, 830, V, past=600, biases=256, masks=3, seed=19, valid=True, pad=1).check(P)
+    Case(kind, 830, V, biases=1, seed=20, penalties=()).check(P)
+    c = Case(kind, 830, V, past=12288 + (kind == "f16"), masks=2, seed=21, index="int32", lengths=False)
+    c.a["past"][:] = np.random.default_rng(1).permutation(V)[:c.a["past"].shape[1]]
+    c.check(P)
+
+
+def test_tables_of_pieces(P):
+    """Half a million columns and more: several pieces of the largest size."""
+    Case("f32", 17, 1000001, past=500, biases=30, masks=2, seed=17).check(P)
+    Case("bf16", 31, 1100003, past=500, biases=30, masks=2, seed=18, valid=True).check(P)
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
