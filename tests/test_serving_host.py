@@ -121,7 +121,7 @@ def test_layouts_that_do_not_overlap(P):
 def test_workspace_sizes(P):
     W = P.at_paged_attention_workspace
     assert W(0, 4, 1000, 8, 2, 64) == 0 and W(4, 0, 1000, 8, 2, 64) == 0
-    assert W(1, 1, 100, 8, 2, 64) == 0                      # too short to be cut
+    assert W(1, 1, 64, 8, 2, 64) == 0                       # one tile of keys
     assert W(1, 1, 100000, 8, 2, 64) > 0
     assert W(100000, 1, 100000, 32, 8, 64) == 0             # rows enough
     for bad in ((-1, 1, 1, 2, 1, 8), (1, 1, 1, 3, 2, 8), (1, 1, 1, 2, 0, 8), (1, 1, 1, 2, 1, 300), (1, 1, -1, 2, 1, 8), (1, 1, 1, 2, 1, 8, 5)):
