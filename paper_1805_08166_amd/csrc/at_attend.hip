@@ -251,7 +251,7 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, in
 }
 
 // DP: the values that a head has room for in LDS, a power of two; USED: those that products are made of.
-template <int DT_, int DP_, int USED_, int ROW_WAVES_, int KEY_WAVES_>
+template <int DT_, int DP_, int USED_, int ROW_WAVES_, int KEY_WAVES_, int SUBS_>
 struct Shape {
     static constexpr int DT = DT_, DP = DP_, USED = USED_;
     // Heads above 128 are halved by columns of the output: two waves compute the same weights, each for its half of the
@@ -262,14 +262,14 @@ struct Shape {
     static constexpr int SIZE = sizeof(typename Elem<DT>::T), VEC = 16 / SIZE;
     static constexpr int CHUNKS = DP / VEC;            // of 16 bytes in a row
     static constexpr int ROW = DP * SIZE;              // bytes
-    static constexpr int SUBS = KEY_WAVES > 1 || ROW > 512 ? 1 : 2;   // 32 keys of a wave and tile each
+    static constexpr int SUBS = SUBS_;                 // 32 keys of a wave and tile each
     static constexpr int KEYS = KEY_WAVES * SUBS * 32;
     static constexpr int ROWS = ROW_WAVES * 32;
     static constexpr int TILE = KEYS * ROW;            // bytes of a tile of keys or values
     static constexpr int MOVES = TILE / 1024 / WAVES;  // of a wave, a KB each
     static constexpr int MOVE_ROWS = 64 / CHUNKS;
     static constexpr int IDS = KEYS > 64 ? 2 : 1;      // words of a lane that hold a tile's page numbers
-    static constexpr int WAVES_EU = ROW <= 256 ? 2 : 1;
+    static constexpr int WAVES_EU = ROW <= 256 || (ROW <= 512 && KEYS == 32) ? 2 : 1;
     static constexpr int OUT_LD = COLS + 4;
     static constexpr int JOIN = KEY_WAVES > 1 ? WAVES * 32 * OUT_LD * 4 : 0;
     static constexpr int LDS = 4 * TILE > JOIN ? 4 * TILE : JOIN;
@@ -946,9 +946,9 @@ Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int
     return s;
 }
 
-template <int DT, int DP, int USED, int RW, int KW>
+template <int DT, int DP, int USED, int RW, int KW, int SUBS>
 hipError_t attend(const AttendArgs& a, Plan p, hipStream_t stream) {
-    using S = Shape<DT, DP, USED, RW, KW>;
+    using S = Shape<DT, DP, USED, RW, KW, SUBS>;
     p.run = a.c.page_size % (S::MOVES * S::MOVE_ROWS) == 0 ? S::MOVES : a.c.page_size % S::MOVE_ROWS == 0;
     static std::atomic<uint64_t> prepared{0};
     hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_attend<S>), -1, S::LDS, prepared);
@@ -962,12 +962,15 @@ template <int DT, int DP, int USED>
 hipError_t attend_rows(const AttendArgs& a, const Plan& p, int shape, hipStream_t stream) {
     constexpr int ROW = DP * (int)sizeof(typename Elem<DT>::T), RW = DP > 128 ? 2 : 4;
     if constexpr (DT == AT_F32 && DP <= 128) {
-        if (shape == FEW) return attend<DT, DP, USED, 1, 2>(a, p, stream);
+        if (shape == FEW) return attend<DT, DP, USED, 1, 2, 1>(a, p, stream);
+        if constexpr (DP == 128) {
+            if (p.keys == 32) return attend<DT, DP, USED, RW, 1, 1>(a, p, stream);
+        }
     }
     if constexpr (ROW >= 128 && ROW <= 256) {
-        if (shape == MANY) return attend<DT, DP, USED, 8, 1>(a, p, stream);
+        if (shape == MANY) return attend<DT, DP, USED, 8, 1, 2>(a, p, stream);
     }
-    return attend<DT, DP, USED, RW, 1>(a, p, stream);
+    return attend<DT, DP, USED, RW, 1, ROW <= 512 ? 2 : 1>(a, p, stream);
 }
 
 }  // namespace
@@ -999,7 +1002,11 @@ hipError_t launch_paged_attention(const AttendArgs& a, void* workspace, hipStrea
         p.size = divider(a.c.page_size);
         p.group = divider(a.q_heads / a.c.heads);
         p.rows = s.rows;
-        p.keys = s.keys;
+        // Tiles of 32 keys leave room for two workgroups a CU and waste less at a window's ends, where it cuts off much of what
+        // there is; without one, a prompt's uneven rows go better to one a CU at a time (fp32, 32 heads on 8 of 128: 8000
+        // tokens, window 500, 601 us, 751 by tiles of 64; 2000 tokens without a window 380 and 316).
+        const bool narrow = DT == AT_F32 && s.dp == 128 && s.shape == SOME && a.window > 0 && a.window <= a.c.width * a.c.page_size / 2;
+        p.keys = narrow ? 32 : s.keys;
         p.target = s.target;
         p.round = s.round;
         p.brief = s.brief;

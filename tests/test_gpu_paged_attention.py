@@ -111,6 +111,15 @@ def test_windows(P, R, kind, window):
         R.close(x.out, want[0], want[2], "out")
 
 
+@pytest.mark.parametrize("window", [1, 33, 300])
+@pytest.mark.parametrize("dim", [65, 80, 96, 100, 112, 128])
+def test_narrow_tiles(P, R, dim, window):
+    """fp32 under a window that is short of what there is: tiles of 32 keys, whole ones, cut ones, and pages of every end."""
+    for new, ctx, heads, page in (([200, 90], [400, 700], 4, 16), ([40], [2500], 2, 24), ([700], [0], 12, 7)):
+        x = R.Batch("f32", new, ctx, heads, 2, dim, page=page, seed=dim + window)
+        check(P, R, x, window=window)
+
+
 @pytest.mark.parametrize("window", [64, 1000, 3000, 2 ** 63 - 1])
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_windows_of_cut_keys(P, R, kind, window):
@@ -231,6 +240,25 @@ def test_not_finite_where_not_seen(P, R, kind, bad):
             elif math.isnan(bad):
                 assert bool(torch.isnan(x.out[rows]).all())
             c[page, off] = clean
+
+
+@pytest.mark.parametrize("kind,dim", [("f32", 80), ("f32", 96), ("bf16", 80), ("bf16", 192), ("f32", 192)])
+def test_not_finite_in_padded_heads(P, R, kind, dim):
+    import torch
+    for new, ctx, at, window in (([70], [900], 905, 100), ([300], [400], 500, 64), ([5], [600], 602, 0)):
+        x = R.Batch(kind, new, ctx, 4, 2, dim, page=16, seed=12)
+        page, off = x.where(0, at, at + 1)
+        want = R.attention64(x, 0.125, window)
+        x.v_cache[page, off, :, dim - 3:] = math.inf
+        x.attend(P, scale=0.125, window=window)
+        torch.cuda.synchronize()
+        pos = torch.arange(ctx[0], ctx[0] + new[0], device=DEV)
+        sees = (pos >= at) & ((pos - at < window) if window else True)
+        rows = torch.zeros(x.n, dtype=torch.bool, device=DEV)
+        rows[x.tokens(0)] = sees
+        R.close(x.out[~rows], want[0][~rows], want[2][~rows], f"{at}")
+        R.close(x.out[rows][..., :dim - 3], want[0][rows][..., :dim - 3], want[2][rows][..., :dim - 3], "other columns")
+        assert not bool(torch.isfinite(x.out[rows][..., dim - 3:]).any())
 
 
 def test_infinite_queries_and_large_scores(P, R):
