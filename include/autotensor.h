@@ -614,7 +614,7 @@ at_status at_paged_append(const at_paged* cache, const void* k, int64_t k_token,
  * Query head h goes with cache head h / (q_heads / heads).  A token that sees
  * nothing gets zeros, and -inf for lse.  NaN and infinities reach the tokens that
  * see them, whose outputs are then not finite, and no others.
- * q, out: device [n][q_heads][dim] of the cache's type; lse: device float
+ * q, out: device [n][q_heads][dim] of the cache's type, out may be q; lse: device float
  * [n][q_heads], or NULL.  scale must be positive and finite.  q_heads is a multiple of the
  * cache's heads.  AT_E_UNSUPPORTED for heads above 128 values whose rows in the cache are not whole
  * 16 bytes at 16-byte aligned addresses, and for 2^31 query heads of all tokens.

@@ -333,7 +333,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const Task task = task_of(a, p, b);
     const int pieces = pieces_of(task, tiles), piece = in_task % pieces;
     const int row_tile = task.row_tiles - 1 - in_task / pieces;   // a prompt's longest first
-    if (row_tile < 0) return;                                     // starts that do not go up
+    if (in_task < 0 || row_tile < 0) return;                      // starts that do not go up
     if (lane == 0) s_odd[wave] = 0;
 
     // Rows of this workgroup, and the keys that they see.

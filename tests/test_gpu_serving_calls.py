@@ -1,0 +1,147 @@
+"""How the serving operators are called: in place, two at once, as captured steps, many
+sequences, and what autograd hears of it."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def P():
+    import torch
+    torch.cuda.set_device(0)
+    import paper_1805_08166_amd
+    return paper_1805_08166_amd
+
+
+@pytest.fixture(scope="module")
+def R():
+    import paged_reference
+    return paged_reference
+
+
+def test_outputs_are_marked_as_written(P, R):
+    import torch
+    x = R.Batch("bf16", [3, 1], [5, 40], 4, 2, 64, page=16)
+    where = (x.k_cache, x.v_cache, x.table, x.starts, x.lengths)
+    k, v, freqs = x.randn(4, 2, 64), x.randn(4, 2, 64), torch.ones(32, dtype=torch.float64, device=DEV)
+    logits, out = torch.zeros(2, 9, device=DEV), torch.zeros(2, 9, device=DEV)
+    past = torch.zeros(2, 3, dtype=torch.int64, device=DEV)
+    f = torch.ones(2, device=DEV)
+
+    def bumped(call, outs, ins):
+        before = [t._version for t in outs], [t._version for t in ins]
+        call()
+        assert all(t._version > w for t, w in zip(outs, before[0]))
+        assert [t._version for t in ins] == before[1]
+
+    bumped(lambda: P.at_paged_append(k, v, *where, q=x.q, q_out=x.out, freqs=freqs), [x.k_cache, x.v_cache, x.out], [k, v, x.q, x.table])
+    bumped(lambda: P.at_paged_append(k, v, *where), [x.k_cache, x.v_cache], [k, v, x.out])
+    bumped(lambda: P.at_paged_attention(x.q, *where, x.out, lse=x.lse), [x.out, x.lse], [x.q, x.k_cache, x.v_cache])
+    bumped(lambda: P.at_paged_attention(x.q, *where, x.out), [x.out], [x.lse])
+    bumped(lambda: P.at_adjust_logits(logits, out, tokens=past, frequency=f), [out], [logits, past, f])
+
+
+@pytest.mark.parametrize("kind,dim", [("bf16", 128), ("bf16", 256), ("f32", 80), ("f16", 40)])
+@pytest.mark.parametrize("new,ctx", [([1, 1], [900, 3]), ([200, 40], [0, 700]), ([9], [20])])
+def test_queries_in_place(P, R, kind, dim, new, ctx):
+    import torch
+    for window in (0, 7):
+        x = R.Batch(kind, new, ctx, 4, 2, dim, page=16, seed=dim)
+        x.attend(P, window=window)
+        out, lse = x.out.clone(), x.lse.clone()
+        P.at_paged_attention(x.q, x.k_cache, x.v_cache, x.table, x.starts, x.lengths, x.q, lse=x.lse, window=window)
+        assert torch.equal(x.q, out) and torch.equal(x.lse, lse)
+
+
+def test_many_sequences(P, R):
+    """More sequences than a wave has lanes, of prompts and of single tokens, with pieces of each."""
+    import torch
+    for kind, many, new, ctx, heads, dim in (("bf16", 70, 260, 0, 1, 64), ("bf16", 65, 3, 300, 2, 128), ("f32", 90, 1, 700, 2, 64),
+                                             ("f32", 66, 40, 500, 1, 100)):
+        print(f"[gpu-serving] {kind} {many} x {new}", flush=True)
+        x = R.Batch(kind, [new] * many, np.random.default_rng(0).integers(0, ctx + 1, many), heads, 1, dim, page=16, seed=many)
+        for window in (0, 150):
+            want = R.attention64(x, 0.125, window)
+            x.attend(P, scale=0.125, window=window)
+            torch.cuda.synchronize()
+            R.close(x.lse, want[1], want[3], "lse")
+            R.close(x.out, want[0], want[2], "out")
+
+
+def test_two_at_once(P, R):
+    """Calls on two streams, each with pieces in a workspace of its own."""
+    import torch
+    xs = [R.Batch("bf16", [1], [ctx], 8, 2, 128, page=16, seed=ctx) for ctx in (9000, 7000)]
+    want = []
+    for x in xs:
+        x.attend(P)
+        want.append((x.out.clone(), x.lse.clone()))
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, s in zip(xs, streams):
+            x.attend(P, stream=s)
+    torch.cuda.synchronize()
+    for x, (out, lse) in zip(xs, want):
+        assert torch.equal(x.out, out) and torch.equal(x.lse, lse)
+
+
+def test_captured_steps(P, R):
+    """A step of append, attention and changes to logits, captured once and replayed as sequences grow, beside eager calls."""
+    import torch
+    B, H, K, D, V, size = 5, 8, 2, 64, 300, 16
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=DEV).bfloat16()  # noqa: E731
+    table = torch.randperm(B * 8, generator=gen, device=DEV).int().reshape(B, 8)
+    starts = torch.arange(B + 1, dtype=torch.int32, device=DEV)
+    freqs = torch.logspace(0, -3, D // 2, dtype=torch.float64, device=DEV)
+    weight = rand(H * D, V)
+    mask = torch.randint(-2 ** 31, 2 ** 31 - 1, (1, (V + 31) // 32), generator=gen, device=DEV).int()
+    rows = torch.zeros(B, dtype=torch.int32, device=DEV)
+    penalty = torch.full((B,), 1.5, device=DEV)
+
+    class State:
+        def __init__(self):
+            self.k_cache, self.v_cache = (torch.zeros(B * 8, size, K, D, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+            self.lengths = torch.zeros(B, dtype=torch.int32, device=DEV)
+            self.past = torch.full((B, 128), -1, dtype=torch.int64, device=DEV)
+            self.qkv = torch.zeros(B, H + 2 * K, D, device=DEV, dtype=torch.bfloat16)
+            self.out = torch.zeros(B, H, D, device=DEV, dtype=torch.bfloat16)
+            self.logits = torch.zeros(B, V, device=DEV)
+
+        def step(self):
+            q, k, v = self.qkv.split([H, K, K], 1)
+            where = (self.k_cache, self.v_cache, table, starts, self.lengths)
+            P.at_paged_append(k, v, *where, q=q, q_out=self.out, freqs=freqs)
+            P.at_paged_attention(self.out, *where, self.out)
+            torch.matmul(self.out.reshape(B, H * D).float(), weight.float(), out=self.logits)
+            P.at_adjust_logits(self.logits, self.logits, tokens=self.past, lengths=self.lengths, repetition=penalty, mask=mask, mask_rows=rows)
+
+    eager, captured = State(), State()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured.step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.step()
+    for c in (captured.k_cache, captured.v_cache):
+        c.zero_()
+    for n in range(120):
+        qkv = rand(B, H + 2 * K, D)
+        for s in (eager, captured):
+            s.qkv.copy_(qkv)
+            s.lengths.add_(1)
+        eager.step()
+        graph.replay()
+        assert torch.equal(eager.logits, captured.logits) and torch.equal(eager.out, captured.out), n
+        assert bool(torch.isfinite(eager.logits).any(1).all()) and bool((eager.logits == -math.inf).any())
+        token = eager.logits.argmax(1)
+        for s in (eager, captured):
+            s.past[:, n] = token
+    assert torch.equal(eager.k_cache, captured.k_cache) and torch.equal(eager.v_cache, captured.v_cache)
