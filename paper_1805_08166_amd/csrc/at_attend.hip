@@ -104,7 +104,7 @@ __device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int 
     t.position = l - s.count;
     t.length = (int)(l < 0 ? 0 : l < room ? l : room);
     t.row_tiles = (int)(((uint32_t)s.count * p.group.d + p.rows - 1) / p.rows);   // fewer than 2^31 rows, tiles of at most 256
-    t.seen = (t.length + p.keys - 1) / p.keys;
+    t.seen = (int)(((uint32_t)t.length + p.keys - 1) / p.keys);
     if (a.window > 0) {   // the window of the first of a tile's tokens, and the others
         const int64_t w = (a.window + p.rows + p.keys - 1) / p.keys + 1;
         if (w < t.seen) t.seen = (int)w;
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     lo = lo < 0 ? 0 : lo;
     hi64 = hi64 < task.length ? hi64 : task.length;
     const int hi = hi64 < 0 ? 0 : (int)hi64;
-    int tile = (int)((lo < hi ? lo : 0) / KEYS), tile_end = lo < hi ? (hi + KEYS - 1) / KEYS : 0;
+    int tile = (int)((lo < hi ? lo : 0) / KEYS), tile_end = lo < hi ? (int)(((uint32_t)hi + KEYS - 1) / KEYS) : 0;
     {
         const int64_t from = tile + (int64_t)piece * tiles, to = from + tiles;
         tile = from < tile_end ? (int)from : tile_end;
