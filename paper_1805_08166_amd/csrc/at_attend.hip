@@ -46,7 +46,7 @@ struct Mat;
 template <>
 struct Mat<AT_BF16> {
     typedef __bf16 Frag __attribute__((ext_vector_type(8)));
-    // P is rounded to bf16, off by half a step, 2^-9 of it at most, as the values that it multiplies are.
+    // P is rounded to bf16, off by half a step, 2^-8 of it at most, as the values that it multiplies are.
     [[maybe_unused]] static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -268,7 +268,6 @@ struct Shape {
     static constexpr int TILE = KEYS * ROW;            // bytes of a tile of keys or values
     static constexpr int MOVES = TILE / 1024 / WAVES;  // of a wave, a KB each
     static constexpr int MOVE_ROWS = 64 / CHUNKS;
-    static constexpr int IDS = KEYS > 64 ? 2 : 1;      // words of a lane that hold a tile's page numbers
     static constexpr int WAVES_EU = ROW <= 256 || (ROW <= 512 && KEYS == 32) ? 2 : 1;
     static constexpr int OUT_LD = COLS + 4;
     static constexpr int JOIN = KEY_WAVES > 1 ? WAVES * 32 * OUT_LD * 4 : 0;
@@ -357,32 +356,13 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int32_t* table = a.c.table + b * a.c.table_ld;
     const uint32_t pages = (uint32_t)a.c.pages;
     const int used_pages = hi > 0 ? (int)divided((uint32_t)hi - 1, p.size) + 1 : 0;   // with positions below hi
-    struct Ids {
-        int v[S::IDS];
-    };
-    struct Bad {   // those that are not there
-        uint64_t v[S::IDS];
-        __device__ bool any() const { return S::IDS > 1 ? (v[0] | v[S::IDS - 1]) != 0 : v[0] != 0; }
-    };
+    static_assert(KEYS <= 64, "a lane has a page number of a tile");
     auto look_up = [&](int t) {
-        Ids r;
-        const int first = (int)divided((uint32_t)(t * KEYS), p.size);
-#pragma unroll
-        for (int i = 0; i < S::IDS; ++i) {
-            const int at = first + i * 64 + lane;
-            r.v[i] = at < used_pages ? table[at] : 0;
-        }
-        return r;
+        const int at = (int)divided((uint32_t)(t * KEYS), p.size) + lane;
+        return at < used_pages ? table[at] : 0;
     };
-    auto bad_of = [&](const Ids& ids) {   // (lanes past the last page have number 0)
-        Bad r;
-#pragma unroll
-        for (int i = 0; i < S::IDS; ++i) r.v[i] = __ballot((uint32_t)ids.v[i] >= pages);
-        return r;
-    };
-    auto id_of = [&](const Ids& ids, uint32_t at) {   // the `at`-th of a tile's page numbers
-        return (uint32_t)__builtin_amdgcn_readlane(S::IDS > 1 && at >= 64 ? ids.v[S::IDS - 1] : ids.v[0], at & 63);
-    };
+    auto bad_of = [&](int ids) { return __ballot((uint32_t)ids >= pages); };   // those that are not there (lanes past the last page have number 0)
+    auto id_of = [&](int ids, uint32_t at) { return (uint32_t)__builtin_amdgcn_readlane(ids, at); };   // the `at`-th of a tile's
     // A tile into LDS, a KB a move.
     constexpr int MOVES = S::MOVES, MOVE_ROWS = S::MOVE_ROWS;
     const int dim = (int)a.c.dim;
@@ -394,7 +374,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const uint64_t k_page = (uint64_t)a.c.k_page * S::SIZE, v_page = (uint64_t)a.c.v_page * S::SIZE;
     const uint32_t k_token = (uint32_t)a.c.k_token * S::SIZE, v_token = (uint32_t)a.c.v_token * S::SIZE;
     const uint32_t bytes = dim * S::SIZE;   // past them, zeros lie in LDS already
-    auto stage = [&](int t, char* to, const Ids& ids, const Bad& bad) {
+    auto stage = [&](int t, char* to, int ids, uint64_t bad) {
         char* to_k = to + wave * MOVES * 1024;
         char* to_v = to_k + S::TILE;
         const int first = (int)divided((uint32_t)(t * KEYS), p.size);
@@ -407,7 +387,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                 asm("" : "+s"(low), "+s"(high));   // or each move's lanes would keep an address of their own
                 return reinterpret_cast<const char*>((uint64_t)high << 32 | low);
             };
-            if (__builtin_expect(p.run && (USED < DP || dim == DP) && hi - t * KEYS >= KEYS && !bad.any(), 1)) {
+            if (__builtin_expect(p.run && (USED < DP || dim == DP) && hi - t * KEYS >= KEYS && !bad, 1)) {
                 // all rows of a move are there, in one page
                 auto move = [&](int q, const char* k, const char* v) {
                     const int row = row0_ + q * MOVE_ROWS + lane_row;
@@ -476,8 +456,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
             }
         }
     };
-    Ids next = {};           // of the next tile, and those of them that are not there
-    Bad bad_next = {};
+    int next = 0;            // page numbers of the next tile, and those of them that are not there
+    uint64_t bad_next = 0;
     if (tile < tile_end) next = look_up(tile);
     // This lane's row: its queries, and the positions that it sees.
     const int row = rw * 32 + mine;
@@ -495,7 +475,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int limit_min = limit_of(wave_from), limit_max = limit_of(wave_to), low_max = low_of(wave_to);
     // Whether some row of this workgroup does not see all of a tile.
     const int all_limit = limit_of(first_pos), all_low = low_of(last_pos);
-    auto partly_seen = [&](int t, const Bad& bad) { return t * KEYS + KEYS - 1 > all_limit || t * KEYS < all_low || bad.any(); };
+    auto partly_seen = [&](int t, uint64_t bad) { return t * KEYS + KEYS - 1 > all_limit || t * KEYS < all_low || bad; };
     constexpr int STEPS = USED / (2 * VEC);
     Frag q[STEPS];
     {
@@ -541,7 +521,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int tile0 = tile;   // the first one
     // Products of a tile with this wave's rows, while the next one moves into the other buffer: the two lie apart, or the
     // compiler would wait for the moves before it reads.
-    auto step = [&](const char* __restrict__ from, char* __restrict__ to, const Bad& bad) {
+    auto step = [&](const char* __restrict__ from, char* __restrict__ to, uint64_t bad) {
         if (tile + 1 < tile_end) {
             bad_next = bad_of(next);
             stage(tile + 1, to, next, bad_next);
@@ -596,14 +576,14 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
         };
         read_values(0);
         __builtin_amdgcn_sched_barrier(ORDERED);
-        if (__builtin_expect(key0 + SUBS * 32 - 1 > limit_min || key0 < low_max || bad.any(), 0)) {
+        if (__builtin_expect(key0 + SUBS * 32 - 1 > limit_min || key0 < low_max || bad, 0)) {
             uint32_t gone[SUBS] = {};   // keys whose page is not there
-            if (bad.any()) {
+            if (bad) {
                 const uint32_t first = divided((uint32_t)(tile * KEYS), p.size);
 #pragma unroll
                 for (int u = 0; u < SUBS; ++u) {
                     const uint32_t at = divided((uint32_t)(key0 + u * 32 + mine), p.size) - first;
-                    gone[u] = (uint32_t)__ballot((S::IDS > 1 && at >= 64 ? bad.v[S::IDS - 1] : bad.v[0]) >> (at & 63) & 1);
+                    gone[u] = (uint32_t)__ballot(bad >> at & 1);
                 }
             }
 #pragma unroll
@@ -691,7 +671,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     for (; tile < tile_end; ++tile) {
         // this tile has landed, and everyone is done with the last one
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        const Bad bad = bad_next;
+        const uint64_t bad = bad_next;
         if (__builtin_expect(partly_seen(tile, bad), 0)) {
             // A NaN or an infinity among the values must not reach, as 0 times it, a row that does not see it: it is
             // left out here, by the lane that moved it, and added at the end where it is seen.
