@@ -132,7 +132,7 @@ __global__ __launch_bounds__(THREADS) void k_append(AppendArgs a, Divider size, 
     }
     __syncthreads();
     const int dim = (int)a.c.dim, heads = (int)a.c.heads, rows = (int)a.q_heads + 2 * heads;
-    const int lane = threadIdx.x % group, per = THREADS / group;
+    const int lane = threadIdx.x % group, per = blockDim.x / group;
     const int turned = pairs / VEC;                                                // pieces of turned pairs
     const int pieces = turned + (dim - a.rot + 2 * VEC - 1) / (2 * VEC);
     for (int row = blockIdx.y * per + threadIdx.x / group; row < rows; row += per * parts) {
@@ -208,12 +208,16 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t stream) {
         // tokens that fill the chip take a workgroup each, which computes its angles once (48 heads of 128 bf16: 512 tokens
         // 6.9 us, 6.5 in parts; 1000 tokens 9.7 and 11.2)
         const int parts = a.n >= 768 ? 1 : whole;
+        // and fewer threads where its heads are few (36864 tokens: 10 heads of 128 bf16 67 us with 128 threads, 90 with 256; 48
+        // heads, pairs (j, j + 64), 179 with 192, 187 with 256, side by side 198 with both; 80 heads 344 with 128, 324 with 256)
+        const int lanes = rows * group;
+        const unsigned threads = parts > 1 || lanes > 384 ? THREADS : lanes > 192 ? 192 : 128;   // 128 pairs at most
         const Divider size = divider(a.c.page_size);
         for (int64_t t = 0; t < a.n; t += GROUPS_MAX / parts) {
             const int64_t m = a.n - t < GROUPS_MAX / parts ? a.n - t : GROUPS_MAX / parts;
             const dim3 grid((unsigned)m, (unsigned)parts);
             const auto kern = vec == WIDE ? &k_append<DT, WIDE> : vec == 4 ? &k_append<DT, 4> : &k_append<DT, 1>;
-            const hipError_t e = launch_direct(kern, grid, THREADS, 0, stream, a, size, t, group, parts);
+            const hipError_t e = launch_direct(kern, grid, threads, 0, stream, a, size, t, group, parts);
             if (e != hipSuccess) return e;
         }
         return hipSuccess;

@@ -106,6 +106,13 @@ def test_many_tokens(P, R):
     check(P, R, R.Batch("f16", [5], [8], 300, 100, 16, seed=4), 8)
 
 
+@pytest.mark.parametrize("kind,heads,kv,dim,rot", [("bf16", 4, 2, 256, 256), ("f32", 2, 1, 256, 256), ("bf16", 12, 4, 128, 64),
+                                                   ("bf16", 32, 8, 128, 128), ("f16", 64, 8, 80, 80), ("f32", 1, 1, 6, 6)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_workgroups_of_every_size(P, R, kind, heads, kv, dim, rot, norm):
+    check(P, R, R.Batch(kind, [800, 3], [9, 70], heads, kv, dim, page=24, seed=dim + heads), rot, norm=norm)
+
+
 def test_without_queries(P, R):
     check(P, R, R.Batch("bf16", [4, 9], [1, 60], 8, 8, 64, seed=5), 64, with_q=False)
 
