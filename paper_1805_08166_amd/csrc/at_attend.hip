@@ -39,6 +39,13 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LN2 = 0.69314718055994530942f;
+// scale log2(e), bounded: the maximum's weight must not be 0 times infinity.  Where the bound counts, scores within 2^-120 of the
+// maximum only have weights that it changes.
+__device__ __forceinline__ float exponent_scale(float scale) { return fminf(scale * LOG2E, 0x1.fffffep127f); }
+// From a row's maximum, and its weights' sum times 2^shift.  The scale itself, as scale log2(e) may leave fp32 where lse does not.
+__device__ __forceinline__ float lse_of(float top, float sum, float scale, float shift) {
+    return sum == 0.0f ? -__builtin_inff() : top * scale + (__log2f(sum) - shift) * LN2;
+}
 
 // Element types: fragments of 16 bytes and their products.
 template <int DT>
@@ -512,7 +519,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     for (int d = 0; d < DTILES; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
-    const float inf = __builtin_inff(), scale = a.scale * LOG2E;
+    const float inf = __builtin_inff(), scale = exponent_scale(a.scale);
     float top = -inf, sum = 0.0f;   // about the row's maximum score, and this lane's part of its sum
     // Weights are 2^((s - top) scale + SHIFT).  Near zero that is one fma with the scaled top, whose rounding, 2^-19 at most,
     // all of a row's weights share.  Far from it the rounding would take weights out of their range, and the distance is taken
@@ -777,7 +784,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                 if (d + e < dim) y[e] = rounded<T>(v[e] * f);
         }
         if (d == 0 && a.lse)
-            a.lse[token_ * a.q_heads + head_] = sum_ == 0.0f ? -inf : (top_ * scale - M::SHIFT + __log2f(sum_)) * LN2;
+            a.lse[token_ * a.q_heads + head_] = lse_of(top_, sum_, a.scale, M::SHIFT);
     };
     if constexpr (KW == 1) {
         if (!real) return;
@@ -835,7 +842,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a, Plan p, int dp) {
     const Task task = task_of(a, p, b);
     const int pieces = uniform(pieces_of(task, place.tiles));
     if (pieces == 1 || token < task.first || token >= task.first + task.count) return;
-    const float inf = __builtin_inff(), scale = a.scale * LOG2E;
+    const float inf = __builtin_inff(), scale = exponent_scale(a.scale);
     const int dim = (int)a.c.dim, heads = (int)a.c.heads, q_head = blockIdx.y * 4 + wave;
     if (q_head >= a.q_heads) return;
     const int G = p.group.d, head = (int)divided((uint32_t)q_head, p.group), r = (token - task.first) * G + q_head - head * G;
@@ -898,7 +905,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a, Plan p, int dp) {
             if (lane * COLS + c < dim) y[c] = rounded<T>(v[c] * over);
     }
     if (lane == 0 && a.lse)
-        a.lse[(int64_t)token * a.q_heads + q_head] = sum == 0.0f ? -inf : (top * scale - Mat<DT>::SHIFT + __log2f(sum)) * LN2;
+        a.lse[(int64_t)token * a.q_heads + q_head] = lse_of(top, sum, a.scale, Mat<DT>::SHIFT);
 }
 
 int padded(int64_t dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }

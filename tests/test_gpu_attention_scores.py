@@ -101,3 +101,27 @@ def test_large_scores_that_differ(P, R, kind, dim):
         x.attend(P, scale=2.0 ** -8)
         torch.cuda.synchronize()
         check(R, x, lambda b, L, m: 2.0 ** 22 + 0.5 * steps[b].double()[None], 0.0, "differ")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_largest_scales(P, R, kind):
+    """A scale up to fp32's largest: equal scores weigh the same, others nothing."""
+    import torch
+    top = torch.finfo(torch.float32).max
+    for scale in (top, 2.5e38, 2.0 ** 127):
+        for new, ctx in CALLS:
+            print(f"[gpu-scores] {kind} scale {scale} new {new} ctx {ctx}", flush=True)
+            x = R.Batch(kind, new, ctx, 4, 2, 64, page=16, seed=3)
+            x.q.zero_()
+            x.attend(P, scale=scale)
+            torch.cuda.synchronize()
+            check(R, x, lambda b, L, m: torch.zeros(1, L, device=DEV, dtype=torch.float64), 0.0, "zeros")
+            if kind == "f16":   # whose products do not come near 2^-120
+                continue
+            x.q.fill_(2.0 ** -63)
+            for b in range(x.batch):
+                page, off = x.where(b)
+                x.k_cache[page, off] = torch.where(torch.arange(len(page), device=DEV) % 2 == 0, 2.0 ** -63, -2.0 ** -63).to(x.q.dtype)[:, None, None].expand(-1, 2, 64)
+            x.attend(P, scale=scale)
+            torch.cuda.synchronize()
+            check(R, x, lambda b, L, m: 2.0 ** -120 * scale * torch.where(torch.arange(L, device=DEV) % 2 == 0, 1.0, -1.0)[None].double(), 0.0, "tiny")
