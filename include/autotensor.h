@@ -569,6 +569,7 @@ at_status at_orthogonalize(const void* x, int xtype, int64_t xbatch, int64_t ldx
  * lies in place p % page_size of page table[b][p / page_size].  starts goes up;
  * a sequence may have no new tokens; tokens from starts[batch] on (and before
  * starts[0]) belong to none, and what a call writes for tokens is left as it was for them.
+ * Where starts goes past n, the tokens that the call has keep their positions.
  * Whatever these arrays hold, nothing outside the caches and the table is touched: pages
  * outside [0, pages) and positions past width * page_size or below 0 are not there.
  * All pointers are device; k and v may be NULL where there are no pages.

@@ -108,7 +108,7 @@ __device__ __forceinline__ Task task_of(const AttendArgs& a, const Plan& p, int 
     t.first = s.first;
     t.count = s.count;
     const int64_t room = a.c.width * a.c.page_size, l = a.c.lengths[b];
-    t.position = l - s.count;
+    t.position = l - ((int64_t)a.c.starts[b + 1] - s.first);   // also where the call has fewer tokens than starts name
     t.length = (int)(l < 0 ? 0 : l < room ? l : room);
     t.row_tiles = (int)(((uint32_t)s.count * p.group.d + p.rows - 1) / p.rows);   // fewer than 2^31 rows, tiles of at most 256
     t.seen = (int)(((uint32_t)t.length + p.keys - 1) / p.keys);
@@ -198,7 +198,7 @@ __device__ __forceinline__ int piece_tiles(const Task& t, const Plan& p) {
 struct Place {
     int b, number, tiles;   // b < 0: none
 };
-// Where piece `slot` lies, or (b >= 0) how many pieces lie before sequence b's, as -number.  All threads get the answer.
+// Where piece `slot` lies, or (FIRST_OF) how many pieces lie before sequence b's, as its number.  All threads get the answer.
 template <int THREADS, bool FIRST_OF>
 __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, int slot, int b, int* scratch) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, batch = (int)a.c.batch;

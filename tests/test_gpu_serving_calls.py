@@ -145,3 +145,29 @@ def test_captured_steps(P, R):
         for s in (eager, captured):
             s.past[:, n] = token
     assert torch.equal(eager.k_cache, captured.k_cache) and torch.equal(eager.v_cache, captured.v_cache)
+
+
+@pytest.mark.parametrize("kind,dim", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("new,ctx,fewer", [([5, 1], [30, 900], 1), ([9], [40], 4), ([200, 90], [50, 700], 33), ([300, 1, 1], [0, 20, 5000], 150),
+                                           ([40], [6000], 25)])
+def test_fewer_tokens_than_starts_name(P, R, kind, dim, new, ctx, fewer):
+    """Buffers that end before the last sequence's new tokens do: tokens keep their positions, in the cache and in what they see."""
+    import torch
+    for window in (0, 20):
+        x = R.Batch(kind, new, ctx, 4, 2, dim, page=16, seed=fewer)
+        want = R.attention64(x, 0.125, window)
+        n, keep = x.n - fewer, (x.k_cache.clone(), x.v_cache.clone())
+        places = [x.where(b, int(x.len[b] - x.new[b])) for b in range(x.batch)]
+        page, off = (torch.cat(p) for p in zip(*places))
+        k, v = (c[page, off] for c in keep)
+        for c in (x.k_cache, x.v_cache):
+            c[page, off] = math.nan
+        where = (x.k_cache, x.v_cache, x.table, x.starts, x.lengths)
+        P.at_paged_append(k[:n], v[:n], *where)
+        for c, whole in zip((x.k_cache, x.v_cache), keep):
+            assert torch.equal(c[page, off][:n], whole[page, off][:n]) and bool(torch.isnan(c[page, off][n:]).all())
+        P.at_paged_attention(x.q[:n], *where, x.out[:n], scale=0.125, window=window, lse=x.lse[:n])
+        torch.cuda.synchronize()
+        R.close(x.out[:n], want[0][:n], want[2][:n], "out")
+        R.close(x.lse[:n], want[1][:n], want[3][:n], "lse")
+        assert bool((x.out[n:] == 77).all()) and bool((x.lse[n:] == 77).all())
