@@ -316,7 +316,7 @@ __device__ __forceinline__ bool is_finite(T v) {
 }
 
 template <class S>
-__global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a, Plan p) {
+__global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a, Plan p, int slot0) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host needs its launch stub only, and does not know all of the device's instructions
     constexpr int DT = S::DT, DP = S::DP, USED = S::USED, RW = S::ROW_WAVES, KW = S::KEY_WAVES;
     using T = typename Elem<DT>::T;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     __shared__ __attribute__((aligned(16))) float s_fix[S::WAVES][COLS];   // values of a key that are not finite
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, mine = lane & 31;
     const int rw = wave % RW, kw = wave / RW % KW, col0 = wave / (RW * KW) * COLS;
-    const int heads = (int)a.c.heads, head = blockIdx.x % heads, slot = blockIdx.x / heads;
+    const int heads = (int)a.c.heads, head = blockIdx.x % heads, slot = slot0 + (int)(blockIdx.x / heads);
 
     // Which sequence, tile of rows and piece of keys.
     const Place place = place_of<S::THREADS, false>(a, p, slot, 0, s_scratch);
@@ -954,9 +954,12 @@ hipError_t attend(const AttendArgs& a, Plan p, hipStream_t stream) {
     static std::atomic<uint64_t> prepared{0};
     hipError_t e = prepare_kernel(reinterpret_cast<const void*>(&k_attend<S>), -1, S::LDS, prepared);
     if (e != hipSuccess) return e;
-    const int64_t groups = (int64_t)p.slots * a.c.heads;
-    if (groups > (((int64_t)1 << 32) - 1) / S::THREADS) return hipErrorInvalidValue;
-    return launch_direct(&k_attend<S>, dim3((unsigned)groups), S::THREADS, S::LDS, stream, a, p);
+    const int64_t most = (((int64_t)1 << 32) - 1) / S::THREADS / a.c.heads;   // a launch holds fewer than 2^32 threads
+    for (int64_t slot = 0; slot < p.slots; slot += most) {
+        e = launch_direct(&k_attend<S>, dim3((unsigned)(std::min(most, p.slots - slot) * a.c.heads)), S::THREADS, S::LDS, stream, a, p, (int)slot);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <int DT, int DP, int USED>

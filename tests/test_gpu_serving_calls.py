@@ -171,3 +171,22 @@ def test_fewer_tokens_than_starts_name(P, R, kind, dim, new, ctx, fewer):
         R.close(x.out[:n], want[0][:n], want[2][:n], "out")
         R.close(x.lse[:n], want[1][:n], want[3][:n], "lse")
         assert bool((x.out[n:] == 77).all()) and bool((x.lse[n:] == 77).all())
+
+
+def test_more_workgroups_than_a_launch_holds(P):
+    """2^32 threads and more, by 65535 heads of 257 sequences: each token sees one key, whose value it gets."""
+    import torch
+    B, H, D = 257, 65535, 8
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    k_cache, v_cache, q = (torch.randn(B, H, D, generator=gen, device=DEV).bfloat16() for _ in range(3))
+    table = torch.randperm(B, generator=gen, device=DEV).int()[:, None].contiguous()
+    starts = torch.arange(B + 1, dtype=torch.int32, device=DEV)
+    lengths = torch.ones(B, dtype=torch.int32, device=DEV)
+    out, lse = torch.full_like(q, 77.0), torch.full((B, H), 77.0, device=DEV)
+    P.at_paged_attention(q, k_cache[:, None], v_cache[:, None], table, starts, lengths, out, scale=1.0, lse=lse)
+    torch.cuda.synchronize()
+    page = table[:, 0].long()
+    assert torch.equal(out, v_cache[page])
+    products = q.float() * k_cache[page].float()   # exact
+    # sums of eight products, and the maximum's scaling, in fp32
+    assert bool(((lse - products.double().sum(2)).abs() <= 2.0 ** -24 * (12 * products.abs().sum(2) + 4)).all())
