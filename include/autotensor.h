@@ -597,7 +597,7 @@ typedef struct {
  * interleaved; elements from rot on stay.  Angles are 64-bit, the rest fp32,
  * rounded once.  Values are copied.
  * k, v: device [n][heads][dim]; q, q_out: device [n][q_heads][dim], or q NULL
- * for none; q_out may be q.  freqs: device [rot / 2] double, in radians a
+ * for none; q_out may be q, with its strides.  freqs: device [rot / 2] double, in radians a
  * position (base, stretching and the like are in them).  A token whose position is not there
  * is not stored; its query is turned all the same.  Two tokens of a call must not share a place of a
  * page: where they do, it holds values of either.
@@ -615,7 +615,7 @@ at_status at_paged_append(const at_paged* cache, const void* k, int64_t k_token,
  * Query head h goes with cache head h / (q_heads / heads).  A token that sees
  * nothing gets zeros, and -inf for lse.  NaN and infinities reach the tokens that
  * see them, whose outputs are then not finite, and no others.
- * q, out: device [n][q_heads][dim] of the cache's type, out may be q; lse: device float
+ * q, out: device [n][q_heads][dim] of the cache's type, out may be q, with its strides; lse: device float
  * [n][q_heads], or NULL.  scale must be positive and finite.  q_heads is a multiple of the
  * cache's heads.  AT_E_UNSUPPORTED for heads above 128 values whose rows in the cache are not whole
  * 16 bytes at 16-byte aligned addresses, and for 2^31 query heads of all tokens.

@@ -94,6 +94,12 @@ bool apart(int64_t dim, Axis a, Axis b, Axis c) {
     return true;
 }
 
+// Whether n tokens of `heads` heads that start at one address lie there with different strides: outputs in the place of
+// other tokens' inputs.
+bool elsewhere(const void* in, int64_t in_token, int64_t in_head, const void* out, int64_t out_token, int64_t out_head, int64_t n, int64_t heads) {
+    return in == out && ((n > 1 && in_token != out_token) || (heads > 1 && in_head != out_head));
+}
+
 at_status paged_args(const char* fn, const at_paged* c) {
     if (!c) return refuse(AT_E_INVALID, fn, "NULL cache");
     if (!type_ok((int)c->type) || c->type != (int)c->type) return refuse(AT_E_INVALID, fn, "unknown element type");
@@ -275,6 +281,7 @@ at_status at_paged_append(const at_paged* cache, const void* k, int64_t k_token,
     if (!aligned_t(k, type) || !aligned_t(v, type) || !aligned_t(q, type) || !aligned_t(q_out, type) ||
         !aligned_t(k_weight, type) || !aligned_t(q_weight, type) || !aligned(freqs, 8))
         return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
+    if (q_heads && elsewhere(q, q_token, q_head, q_out, o_token, o_head, n, q_heads)) return refuse(AT_E_INVALID, fn, "in place with another stride");
     const AppendArgs a{*cache, {k, k_token, k_head}, {v, v_token, v_head}, {q, q_token, q_head}, {q_out, o_token, o_head}, n, q_heads,
                        k_weight, q_weight, eps, freqs, (int)rot, interleaved != 0, rot_scale};
     return done(launch_paged_append(a, (hipStream_t)stream), fn);
@@ -312,6 +319,7 @@ at_status at_paged_attention(const at_paged* cache, const void* q, int64_t q_tok
     const int type = (int)cache->type;
     if (!aligned_t(q, type) || !aligned_t(out, type) || !aligned(lse, 4))
         return refuse(AT_E_INVALID, fn, "a buffer is not aligned to its elements");
+    if (elsewhere(q, q_token, q_head, out, o_token, o_head, n, q_heads)) return refuse(AT_E_INVALID, fn, "in place with another stride");
     if (!paged_attention_takes(*cache))
         return refuse(AT_E_UNSUPPORTED, fn, "heads above 128 values need a cache of whole, 16-byte aligned 16 bytes");
     st = workspace_args(fn, workspace, workspace_bytes,

@@ -142,3 +142,11 @@ def test_binding_checks(P):
         P.at_paged_attention(k, c, c, table, starts, lengths, k)
     with pytest.raises(ValueError, match="device"):
         P.at_adjust_logits(torch.zeros(2, 5), torch.zeros(2, 5))
+
+
+@pytest.mark.parametrize("call,args", [(append, dict(o_token=40)), (append, dict(o_token=8, o_head=40)), (append, dict(n=1, o_head=16)),
+                                       (attend, dict(o_token=40)), (attend, dict(o_token=8, o_head=40)), (attend, dict(n=1, o_head=16))])
+def test_in_place_with_other_strides_is_refused(P, call, args):
+    """Outputs that start where the queries do and lie apart otherwise would replace other tokens' queries."""
+    assert call(P, **args) == INVALID
+    assert "stride" in P.lib().at_last_error().decode()
