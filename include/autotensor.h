@@ -618,7 +618,8 @@ at_status at_paged_append(const at_paged* cache, const void* k, int64_t k_token,
  * q, out: device [n][q_heads][dim] of the cache's type, out may be q, with its strides; lse: device float
  * [n][q_heads], or NULL.  scale must be positive and finite.  q_heads is a multiple of the
  * cache's heads.  AT_E_UNSUPPORTED for heads above 128 values whose rows in the cache are not whole
- * 16 bytes at 16-byte aligned addresses, and for 2^31 query heads of all tokens.
+ * 16 bytes at 16-byte aligned addresses, or lie 2^25 elements and more apart in a page, and for
+ * 2^31 query heads of all tokens.
  * Products of 16-bit types run on the matrix cores in that type with fp32 sums,
  * for which the weights exp(s_j - max) are rounded to it; fp32 in fp32.
  * Long sequences may be cut into pieces, joined in order: the same call gives the same bits, a

@@ -984,8 +984,10 @@ namespace {
 bool moves_directly(const at_paged& c) {
     const int size = elem_size((int)c.type);
     uintptr_t bits = reinterpret_cast<uintptr_t>(c.k) | reinterpret_cast<uintptr_t>(c.v);
-    for (int64_t d : {c.dim, c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head}) bits |= (uintptr_t)(d * size);
-    return bits % 16 == 0 && (c.k_token | c.v_token) < (int64_t)1 << 25;
+    const int64_t page = c.pages > 1, token = c.page_size > 1, head = c.heads > 1;   // no distance counts along an axis of one
+    for (int64_t d : {c.dim, page * c.k_page, token * c.k_token, head * c.k_head, page * c.v_page, token * c.v_token, head * c.v_head})
+        bits |= (uintptr_t)(d * size);
+    return bits % 16 == 0 && token * (c.k_token | c.v_token) < (int64_t)1 << 25;
 }
 }  // namespace
 

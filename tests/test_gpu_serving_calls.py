@@ -190,3 +190,23 @@ def test_more_workgroups_than_a_launch_holds(P):
     products = q.float() * k_cache[page].float()   # exact
     # sums of eight products, and the maximum's scaling, in fp32
     assert bool(((lse - products.double().sum(2)).abs() <= 2.0 ** -24 * (12 * products.abs().sum(2) + 4)).all())
+
+
+def test_size_one_axes_have_any_stride(P, R):
+    """One token in place whose output has another distance between tokens; one head, page or place at odd distances."""
+    import torch
+    for dim in (64, 192):
+        x = R.Batch("bf16", [1], [15], 4, 1, dim, page=16, seed=dim)
+        want = R.attention64(x, 0.125)
+        big = torch.zeros(4 * dim + 8, dtype=torch.bfloat16, device=DEV)
+        q, out = big.as_strided((1, 4, dim), (4 * dim, dim, 1)), big.as_strided((1, 4, dim), (4 * dim + 3, dim, 1))
+        q.copy_(x.q)
+        odd = [c.as_strided((x.pages, 16, 1, dim), (16 * dim, dim, 7, 1)) for c in (x.k_cache, x.v_cache)]
+        P.at_paged_attention(q, *odd, x.table, x.starts, x.lengths, out, scale=0.125, lse=x.lse)
+        R.close(out, want[0], want[2], "out")
+        k, v = x.randn(1, 1, dim), x.randn(1, 1, dim)
+        freqs = torch.linspace(1, 0.01, dim // 2, dtype=torch.float64, device=DEV)
+        q.copy_(x.q)
+        for q_, o_ in ((x.q, x.out), (q, out)):
+            P.at_paged_append(k, v, *odd, x.table, x.starts, x.lengths, q=q_, q_out=o_, freqs=freqs)
+        assert torch.equal(out, x.out)

@@ -150,3 +150,16 @@ def test_in_place_with_other_strides_is_refused(P, call, args):
     """Outputs that start where the queries do and lie apart otherwise would replace other tokens' queries."""
     assert call(P, **args) == INVALID
     assert "stride" in P.lib().at_last_error().decode()
+
+
+def test_rows_of_one_entry_are_whole_whatever_the_stride(P):
+    """Distances along axes of one head, page or place do not count for whole 16 bytes: such a call goes on to its workspace."""
+    wide = dict(c_dim=136, c_k_token=136, c_v_token=136, c_k_page=2176, c_v_page=2176, q_head=136, q_token=544, o_head=136, o_token=544,
+                c_width=4096, c_table_ld=4096, ws=None)
+    one = dict(wide, c_heads=1, c_k_head=7, c_v_head=7)
+    assert attend(P, **one) == INVALID and "workspace" in P.lib().at_last_error().decode()
+    assert attend(P, **{**one, "c_pages": 1, "c_k_page": 3}) == INVALID
+    assert attend(P, **{**one, "c_page_size": 1, "c_width": 65536, "c_table_ld": 65536, "c_k_token": 5, "c_v_token": 5}) == INVALID
+    assert attend(P, **{**one, "c_page_size": 1, "c_width": 65536, "c_table_ld": 65536, "c_k_token": 1 << 26}) == INVALID
+    assert attend(P, **{**one, "c_k_token": 1 << 26}) == UNSUPPORTED
+    assert attend(P, **dict(wide, c_heads=2, c_k_head=7, c_v_head=136)) == UNSUPPORTED
