@@ -167,7 +167,26 @@ __global__ __launch_bounds__(THREADS) void k_append(AppendArgs a, Divider size, 
         float norm = 1.0f;
         if (weight) {   // all lanes of a head have the same weight pointer
             for (int o = group >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-            norm = 1.0f / sqrtf(sum / (float)dim + a.eps);
+            const float mean = sum / (float)dim + a.eps;
+            norm = 1.0f / sqrtf(mean);
+            if (!(mean >= 0x1p-80f && mean <= 0x1p120f)) {
+                // squares, or their sum, that fp32 does not hold: normed in 64 bits, then as if their norm were 1
+                double whole = 0.0;
+#pragma unroll
+                for (int it = 0; it < ROUNDS; ++it)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) whole += (double)r[it].a[e] * r[it].a[e] + (double)r[it].b[e] * r[it].b[e];
+                for (int o = group >> 1; o > 0; o >>= 1) whole += __shfl_xor(whole, o);
+                whole = 1.0 / sqrt(whole / dim + (double)a.eps);
+#pragma unroll
+                for (int it = 0; it < ROUNDS; ++it)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        r[it].a[e] = (float)(r[it].a[e] * whole);
+                        r[it].b[e] = (float)(r[it].b[e] * whole);
+                    }
+                norm = 1.0f;
+            }
         }
 #pragma unroll
         for (int it = 0; it < ROUNDS; ++it) {
