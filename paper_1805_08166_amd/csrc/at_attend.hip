@@ -85,7 +85,7 @@ struct Plan {
     Divider group;       // G, query heads of a cache head
     int rows;            // of a tile
     int keys;            // of a tile
-    int target;          // pieces a head that the keys are cut into, about; 0: whole sequences
+    int target;          // pieces a head that the keys are cut into, about; 0: none is cut
     int round, brief;    // or `round`, a workgroup a CU, where those have `brief` tiles at most
     int slots;           // pieces a head, at most
     int direct;          // rows of the cache are whole aligned 16 bytes
@@ -198,14 +198,27 @@ __device__ __forceinline__ int piece_tiles(const Task& t, const Plan& p) {
 struct Place {
     int b, number, tiles;   // b < 0: none
 };
-// Where piece `slot` lies, or (FIRST_OF) how many pieces lie before sequence b's, as its number.  All threads get the answer.
+// Where no sequence is cut: b has places from (rows before it) / ROWS + b on, as many as it has tiles at most, so that a search
+// finds it.  Adding up all sequences in each workgroup would take the square of their number: 32768 of a token each 63 ms.
+template <int ROWS>
+__device__ __forceinline__ int place_before(const AttendArgs& a, const Plan& p, int b) {
+    const int s = a.c.starts[b], n = (int)a.n;
+    return (int)((uint32_t)(s < 0 ? 0 : s < n ? s : n) * p.group.d / ROWS) + b;
+}
+template <int ROWS>
+__device__ __forceinline__ Place whole_place_of(const AttendArgs& a, const Plan& p, int slot) {
+    const int batch = (int)a.c.batch, b = last_upto(batch, slot, [&](int i) { return place_before<ROWS>(a, p, i); });
+    if (b < 0 || b >= batch) return {-1, 0, 0};
+    return {b, slot - place_before<ROWS>(a, p, b), 1 << 30};
+}
+// Where piece `slot` of sequences that are cut lies, or (FIRST_OF) how many pieces lie before sequence b's, as its number.  All threads get the answer.
 template <int THREADS, bool FIRST_OF>
 __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, int slot, int b, int* scratch) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, batch = (int)a.c.batch;
     if (batch <= 64) {   // a lane a sequence, each wave for itself
         Task t = {};
         if (lane < batch) t = task_of(a, p, lane);
-        const int tiles = p.target ? piece_tiles(t, p) : 1 << 30;
+        const int tiles = piece_tiles(t, p);
         const int n = t.row_tiles * pieces_of(t, tiles), upto = wave_scan(n);
         if (FIRST_OF) return {b, __builtin_amdgcn_readlane(upto - n, b), tiles};
         const uint64_t past = __ballot(upto > slot && lane < batch);
@@ -216,19 +229,16 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, in
     // a run of sequences a thread
     const int each = (batch + THREADS - 1) / THREADS, b0 = threadIdx.x * each, b1 = b0 + each < batch ? b0 + each : batch;
     constexpr int WAVES = THREADS / 64;
-    int tiles = 1 << 30;
-    if (p.target) {
-        double work = 0.0;
-        for (int i = b0; i < b1; ++i) work += work_of(task_of(a, p, i));
-        work = wave_sum(work);
-        double* sums = reinterpret_cast<double*>(scratch);
-        if (lane == 0) sums[wave] = work;
-        __syncthreads();
-        work = 0.0;
-        for (int w = 0; w < WAVES; ++w) work += sums[w];
-        __syncthreads();
-        tiles = piece_tiles(work, p);
-    }
+    double work = 0.0;
+    for (int i = b0; i < b1; ++i) work += work_of(task_of(a, p, i));
+    work = wave_sum(work);
+    double* sums = reinterpret_cast<double*>(scratch);
+    if (lane == 0) sums[wave] = work;
+    __syncthreads();
+    work = 0.0;
+    for (int w = 0; w < WAVES; ++w) work += sums[w];
+    __syncthreads();
+    const int tiles = piece_tiles(work, p);
     int here = 0;
     for (int i = b0; i < b1; ++i) {
         const Task t = task_of(a, p, i);
@@ -333,7 +343,11 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
     const int heads = (int)a.c.heads, head = blockIdx.x % heads, slot = slot0 + (int)(blockIdx.x / heads);
 
     // Which sequence, tile of rows and piece of keys.
-    const Place place = place_of<S::THREADS, false>(a, p, slot, 0, s_scratch);
+    Place place;
+    if (__builtin_expect(p.target, 0))
+        place = place_of<S::THREADS, false>(a, p, slot, 0, s_scratch);
+    else
+        place = whole_place_of<S::ROWS>(a, p, slot);
     const int b = uniform(place.b), in_task = uniform(place.number), tiles = uniform(place.tiles);
     if (b < 0) return;
     const Task task = task_of(a, p, b);
@@ -943,7 +957,7 @@ Sizes sizes_of(int64_t n, int64_t batch, int64_t positions, int64_t q_heads, int
     s.round = (int)std::max<int64_t>(1, CUS / heads);
     // an fp32 tile's products take four times as long as a 16-bit one's moves: 700 tokens of 12 heads 112 us, with 16 121
     s.brief = s.shape == MANY ? 1 << 30 : type == AT_F32 && s.shape == SOME ? 4 : 16;
-    s.slots = units(s.rows) + (s.target ? std::max(s.target, s.round) : 0);
+    s.slots = s.target ? units(s.rows) + std::max(s.target, s.round) : n * G / s.rows + batch;
     return s;
 }
 

@@ -32,21 +32,26 @@ __device__ __forceinline__ Span span_of(const int32_t* starts, int b, int n) {
     return {lo, hi > lo ? hi - lo : 0};
 }
 
-// The last b of 0 .. batch with starts[b] <= i, or -1: 64 places are looked at a step,
+// The last b of 0 .. batch with of(b) <= i, or -1, where of goes up: 64 places are looked at a step,
 // by the lanes of a wave, which all get the answer.
-__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, int i) {
+template <class F>
+__device__ __forceinline__ int last_upto(int batch, int i, F&& of) {
     const int lane = threadIdx.x & 63;
     int lo = 0, hi = batch;   // it is in [lo, hi], or none is
     while (true) {
         const int step = (hi - lo) / 64 + 1;
         const int64_t at = lo + (int64_t)lane * step;
-        const uint64_t below = __ballot(at <= hi && starts[at <= hi ? at : hi] <= i);
+        const uint64_t below = __ballot(at <= hi && of((int)(at <= hi ? at : hi)) <= i);
         const int found = below == ~0ull ? 64 : __builtin_ctzll(~below);   // the first `found` places are at most i
         if (found == 0) return lo - 1;                                      // in the first step only: lo is 0
         lo += (found - 1) * step;
         if (step == 1) return lo;
         hi = hi < lo + step - 1 ? hi : lo + step - 1;
     }
+}
+// The sequence that token i belongs to, if it is in 0 .. batch - 1.
+__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, int i) {
+    return last_upto(batch, i, [&](int b) { return starts[b]; });
 }
 
 }  // namespace at

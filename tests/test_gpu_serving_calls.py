@@ -210,3 +210,40 @@ def test_size_one_axes_have_any_stride(P, R):
         for q_, o_ in ((x.q, x.out), (q, out)):
             P.at_paged_append(k, v, *odd, x.table, x.starts, x.lengths, q=q_, q_out=o_, freqs=freqs)
         assert torch.equal(out, x.out)
+
+
+def test_a_quarter_of_a_million_sequences(P):
+    """The time of a call goes with the number of its sequences, not with the square, which would be a second here; some have no new
+    token, and some two."""
+    import torch
+    B, H, D = 1 << 18, 2, 16
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    new = torch.randint(0, 3, (B,), generator=gen, device=DEV)
+    starts = torch.cat([torch.zeros(1, device=DEV, dtype=torch.int64), new.cumsum(0)]).int()
+    n = int(starts[-1])
+    k_cache, v_cache = (torch.randn(B, 2, H, D, generator=gen, device=DEV).bfloat16() for _ in range(2))
+    table = torch.randperm(B, generator=gen, device=DEV).int()[:, None].contiguous()
+    q = torch.randn(n, H, D, generator=gen, device=DEV).bfloat16()
+    out, lse = torch.full_like(q, 77.0), torch.full((n, H), 77.0, device=DEV)
+    call = lambda: P.at_paged_attention(q, k_cache, v_cache, table, starts, new.int(), out, scale=0.25, lse=lse)  # noqa: E731
+    call()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    call()
+    end.record()
+    torch.cuda.synchronize()
+    b = torch.repeat_interleave(torch.arange(B, device=DEV), new)
+    page, second = table[b, 0].long(), (torch.arange(n, device=DEV) > starts[b])[:, None, None]
+    k, v = k_cache[page].double(), v_cache[page].double()                       # [n, 2, H, D]
+    s = 0.25 * (q.double()[:, None] * k).sum(3)
+    size = 0.25 * (q.double()[:, None] * k).abs().sum(3).amax(1)
+    s[:, 1] = torch.where(second[..., 0], s[:, 1], torch.full_like(s[:, 1], -math.inf))
+    want_lse = torch.logsumexp(s, 1)
+    p = torch.exp(s - want_lse[:, None])[..., None]
+    want, big, u = (p * v).sum(1), (p * v.abs()).sum(1), 2.0 ** -24
+    # scores of 16 products, twice in a weight, whose rounding to bf16 is 2^-8 and the result's again
+    assert bool(((out.double() - want).abs() <= big * (48 * u * size[..., None] + 40 * u + 2.0 ** -8) + want.abs() * 2.0 ** -8 * (1 + 2 ** -6)).all())
+    assert bool(((lse.double() - want_lse).abs() <= 24 * u * size + 20 * u + 4 * u * want_lse.abs()).all())
+    took = begin.elapsed_time(end)
+    print(f"[gpu-serving] {took:.2f} ms", flush=True)
+    assert took < 100.0
