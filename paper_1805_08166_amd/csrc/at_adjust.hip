@@ -23,7 +23,7 @@ namespace {
 
 // Of a column's word: whether the token is in the prompt, whether it has a bias; the rest is how often it is in the answer.
 constexpr uint32_t IN_PROMPT = 1u << 31, BIASED = 1u << 30, COUNT = BIASED - 1;
-constexpr int LISTED = 256;   // biases of a segment that LDS lists; with more, the list in memory is searched
+constexpr int LISTED = 256;   // biases of a segment that LDS lists; with more, the list in memory is read once more
 
 constexpr int MOST_SLOTS = 16384;            // of a table in LDS
 constexpr uint32_t NOWHERE = 0x7fffffffu;   // in the place of a token that is none
@@ -31,9 +31,11 @@ constexpr uint32_t NOWHERE = 0x7fffffffu;   // in the place of a token that is n
 // Waits for the workgroup's LDS, not for what is on its way to and from memory.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// PACKS packs of 16 bytes of logits a thread and segment; HELD of the past's tokens a thread in registers.
-template <int DT, int THREADS, int PACKS, int HELD>
-__global__ __launch_bounds__(THREADS) void k_adjust(AdjustArgs a, int64_t row0, int groups, int run) {
+// PACKS packs of 16 bytes of logits a thread and segment; HELD of the past's tokens a thread in registers; MANY: rows have more
+// biases than LISTED, whose last ones take registers that other calls do without.  Two workgroups of 512 threads to a CU need four waves a
+// SIMD (512 rows of 131072 bf16, 300 biases: 153 us, with three waves 262).
+template <int DT, int THREADS, int PACKS, int HELD, bool MANY>
+__global__ __launch_bounds__(THREADS, 4) void k_adjust(AdjustArgs a, int64_t row0, int groups, int run) {
     using T = typename Elem<DT>::T;
     constexpr int VEC = 16 / sizeof(T), SEGMENT = THREADS * PACKS * VEC;
     static_assert(SEGMENT <= 65536, "columns of the list are 16-bit");
@@ -162,26 +164,52 @@ __global__ __launch_bounds__(THREADS) void k_adjust(AdjustArgs a, int64_t row0, 
             const uint32_t changes = s_changes, biases = s_biases;
             // the other turn's were read before this barrier, and are used again after the next one
             if (threadIdx.x < 2) s_many[(i & 1) ^ 1][threadIdx.x] = 0;
-            for (uint32_t n = threadIdx.x; n < changes; n += THREADS) {
-                const uint32_t c = s_list[n], w = s_words[c], times = w & COUNT;
-                s_words[c] = 0;   // for the next segment
+            // word w of column c, and the place of its last bias in the row's list
+            auto change = [&](uint32_t c, uint32_t w, int64_t last) {
+                const uint32_t times = w & COUNT;
                 float z = (float)s_x[c];
-                if (z == -__builtin_inff()) continue;
+                if (z == -__builtin_inff()) return;
                 if (use_r && (w & ~BIASED)) z = z > 0.0f ? z / r : z * r;
                 if (use_f && times) z = z - f * (float)times;
                 if (use_q && times) z = z - q;
-                if (w & BIASED) {   // the last one in the row's list
-                    int64_t k = -1;
-                    if (biases <= LISTED) {
-                        for (uint32_t b = 0; b < biases; ++b)
-                            if (s_bias[b][0] == c && (int64_t)s_bias[b][1] > k) k = s_bias[b][1];
-                    } else {
-                        for (k = a.n_bias - 1; bias_token(k) != first + c; --k) {
-                        }
-                    }
-                    z = z + a.bias[row * a.bias_ld + k];
-                }
+                if (w & BIASED) z = z + a.bias[row * a.bias_ld + last];
                 s_x[c] = rounded<T>(z);
+            };
+            if (!MANY || __builtin_expect(biases <= LISTED, 1)) {
+                for (uint32_t n = threadIdx.x; n < changes; n += THREADS) {
+                    const uint32_t c = s_list[n], w = s_words[c];
+                    s_words[c] = 0;   // for the next segment
+                    int64_t last = -1;
+                    if (w & BIASED)
+                        for (uint32_t b = 0; b < biases; ++b)
+                            if (s_bias[b][0] == c && (int64_t)s_bias[b][1] > last) last = s_bias[b][1];
+                    change(c, w, last);
+                }
+            } else if constexpr (MANY) {
+                // The words go to registers, and their columns' places in LDS take the last bias: a search of the row's list for
+                // each column would take the square of its length (32768 biases of as many columns 8.5 ms).
+                constexpr int EACH = SEGMENT / THREADS;
+                uint32_t word[EACH];
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    const uint32_t n = i * THREADS + threadIdx.x;
+                    word[i] = n < changes ? s_words[s_list[n]] : 0;
+                    if (n < changes) s_words[s_list[n]] = 0;
+                }
+                lds_barrier();
+                for (int64_t k = threadIdx.x; k < a.n_bias; k += THREADS) {
+                    const uint32_t c = bias_token(k) - first;
+                    if (c < cols) atomicMax(&s_words[c], (uint32_t)k + 1);
+                }
+                lds_barrier();
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    const uint32_t n = i * THREADS + threadIdx.x;
+                    if (n >= changes) continue;
+                    const uint32_t c = s_list[n], last = s_words[c];
+                    s_words[c] = 0;
+                    change(c, word[i], (int64_t)last - 1);
+                }
             }
             lds_barrier();
 #pragma unroll
@@ -406,8 +434,8 @@ hipError_t adjust(const AdjustArgs& a, int64_t run, hipStream_t stream) {
     const int64_t fit = (((int64_t)1 << 32) - 1) / THREADS / groups, most = fit > 0 ? fit : 1;
     for (int64_t row = 0; row < a.n; row += most) {
         const int64_t m = a.n - row < most ? a.n - row : most;
-        const hipError_t e = launch_direct(&k_adjust<DT, THREADS, PACKS, HELD>, dim3((unsigned)(m * groups)), THREADS, 0, stream, a,
-                                           row, (int)groups, (int)run);
+        const auto kern = a.n_bias > LISTED ? &k_adjust<DT, THREADS, PACKS, HELD, true> : &k_adjust<DT, THREADS, PACKS, HELD, false>;
+        const hipError_t e = launch_direct(kern, dim3((unsigned)(m * groups)), THREADS, 0, stream, a, row, (int)groups, (int)run);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
