@@ -613,8 +613,11 @@ at_status at_paged_append(const at_paged* cache, const void* k, int64_t k_token,
  * positions j <= p, with window > 0 only j > p - window:
  *   s_j = scale * q . k_j,  out = sum_j exp(s_j - lse) v_j,  lse = log sum_j exp(s_j)
  * Query head h goes with cache head h / (q_heads / heads).  A token that sees
- * nothing gets zeros, and -inf for lse.  NaN and infinities reach the tokens that
- * see them, whose outputs are then not finite, and no others.
+ * nothing, or whose scores are all -inf, gets zeros, and -inf for lse.  NaN and infinities
+ * reach the tokens that see them, and no others: a key whose score is -inf weighs nothing, any other
+ * score or value that is not finite leaves outputs that are not.
+ * Scores, and sums of weights times values before they are divided, are fp32: products q . k
+ * that it does not hold, and values above 2^119 over the number of keys, count as infinite.
  * q, out: device [n][q_heads][dim] of the cache's type, out may be q, with its strides; lse: device float
  * [n][q_heads], or NULL.  scale must be positive and finite.  q_heads is a multiple of the
  * cache's heads.  AT_E_UNSUPPORTED for heads above 128 values whose rows in the cache are not whole

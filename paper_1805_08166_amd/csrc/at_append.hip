@@ -10,8 +10,9 @@
 // taken by a group of lanes, each with VEC pairs: 16 bytes of each half of
 // the pairs, or 32 in a row where pairs lie side by side.
 // Bound by HBM: every value is read once and written once.  36864 tokens of 32 query and 8 + 8 other heads of 128
-// bf16: 196 us, 4.6 TB/s, of 5.3 that a copy reaches; one token 3.9 us, what its four dependent loads take.  A head's
-// values read ahead, while the position is looked up, took 260 us.
+// bf16: 172 us, 5.3 TB/s, what a copy reaches; one token 3.9 us, what its four dependent loads take.  An order of the loop's loads that
+// the compiler chose for the same statements without the norm in 64 bits took 196, and so with 5 to 8 waves a SIMD; there a head's
+// values read ahead, while the position is looked up, took 260.
 #include "at_paged.h"
 
 namespace at {
@@ -225,10 +226,10 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t stream) {
         while (group < pieces && group < 64) group *= 2;
         const int rows = (int)a.q_heads + 2 * (int)a.c.heads, per = THREADS / group, whole = (rows + per - 1) / per;
         // tokens that fill the chip take a workgroup each, which computes its angles once (48 heads of 128 bf16: 512 tokens
-        // 6.9 us, 6.5 in parts; 1000 tokens 9.7 and 11.2)
+        // 5.9 us, 5.8 in parts; 1000 tokens 8.1 and 9.3)
         const int parts = a.n >= 768 ? 1 : whole;
-        // and fewer threads where its heads are few (36864 tokens: 10 heads of 128 bf16 67 us with 128 threads, 90 with 256; 48
-        // heads, pairs (j, j + 64), 179 with 192, 187 with 256, side by side 198 with both; 80 heads 344 with 128, 324 with 256)
+        // and fewer threads where its heads are few (36864 tokens: 10 heads of 128 bf16 61 us with 128 threads, 83 with 256; 48
+        // heads, normed, 178 with 192, 188 with 256, otherwise 169 with both; 80 heads 293 with 128, 282 with 256)
         const int lanes = rows * group;
         const unsigned threads = parts > 1 || lanes > 384 ? THREADS : lanes > 192 ? 192 : 128;   // 128 pairs at most
         const Divider size = divider(a.c.page_size);

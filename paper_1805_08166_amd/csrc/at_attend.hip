@@ -22,9 +22,11 @@
 // out in a row and cut into pieces of equal length, which leave their sums in the
 // workspace for a joining launch that adds them in order.
 //
-// Bound by the matrix cores for prompts (8192 tokens of 32 heads on 8 of 128 bf16 585 us, 940 TF/s; 512 tokens with 32000
-// before them 284 us, 955 TF/s), by HBM for tokens of many long sequences (64 of up to 16385 keys 417 us, 5.2 TB/s), by
+// Bound by the matrix cores for prompts (8192 tokens of 32 heads on 8 of 128 bf16 582 us, 945 TF/s; 512 tokens with 32000
+// before them 281 us, 962 TF/s), by HBM for tokens of many long sequences (64 of up to 16385 keys 418 us, 5.2 TB/s), by
 // latency for a single one (4097 keys: 12 us and 4.6 to join).
+//
+// Scores, and sums before they are divided, are fp32: with weights of up to 2^8, values above 2^119 over the number of keys overflow.
 #include <algorithm>
 #include <atomic>
 
@@ -53,7 +55,7 @@ struct Mat;
 template <>
 struct Mat<AT_BF16> {
     typedef __bf16 Frag __attribute__((ext_vector_type(8)));
-    // P is rounded to bf16, off by half a step, 2^-8 of it at most, as the values that it multiplies are.
+    // P, at most 2^8 with the slack of its maximum, is rounded to bf16, off by half a step, 2^-8 of it at most, as the values that it multiplies are.
     [[maybe_unused]] static constexpr float SHIFT = 0.0f, SLACK = 8.0f;
     static __device__ __forceinline__ float16v mma(Frag a, Frag b, float16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -436,7 +438,9 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_EU) void k_attend(AttendArgs a
                     }
                 }
             } else {
-                // row by row, with zeros for those that are not there
+                // row by row, with zeros for those that are not there.  All tiles of heads of 1 to 31, 33 to 63, 97 to 127
+                // and 193 to 255 values come here too, and all of pages that end within a move: 64 sequences of up to 16384 keys 885 us
+                // with heads of 112 bf16 and 884 with pages of 1, 415 with 128 and 16.
 #pragma unroll 1
                 for (int i = 0; i < MOVES * MOVE_ROWS; ++i) {
                     const int q = i / MOVE_ROWS, row = row0_ + i, pos = t * KEYS + row;
